@@ -1,5 +1,6 @@
-"""Build librkrotor.so (the solver) and librkcalib.so (measured GPU ceilings for the
-benchmark), HIP for gfx950, in-tree with hipcc."""
+"""Build librkrotor.so (the solver), librkblock.so (operators of the blocks that a schedule
+runs) and librkcalib.so (measured GPU ceilings for the benchmark), HIP for gfx950, in-tree
+with hipcc."""
 from __future__ import annotations
 
 import os
@@ -14,6 +15,8 @@ LIB = os.path.join(PKG, "librkrotor.so")
 SOURCES = ["rk_api.hip", "rk_kernels.hip", "rk_tile.hip", "rk_host.cpp"]
 CALIB_LIB = os.path.join(PKG, "librkcalib.so")
 CALIB_SOURCES = ["rk_calib.hip"]
+BLOCK_LIB = os.path.join(PKG, "librkblock.so")
+BLOCK_SOURCES = ["rkb_norm.hip", "rkb_ckpt.hip", "rkb_gemm.hip"]
 ARCH = "gfx950"
 
 HIPCC_FLAGS = [
@@ -49,7 +52,8 @@ def _compile(sources, out: str, verbose: bool) -> str:
 
 
 def build(verbose: bool = False) -> str:
-    """Both libraries; returns the solver's path."""
+    """All three libraries; returns the solver's path."""
+    _compile(BLOCK_SOURCES, BLOCK_LIB, verbose)
     _compile(CALIB_SOURCES, CALIB_LIB, verbose)
     return _compile(SOURCES, LIB, verbose)
 

@@ -1,0 +1,160 @@
+// Shared by the kernels of librkblock (rk_block.h): types, 16-byte row chunks, sums over
+// lanes, and the arithmetic of the 8-bit checkpoints.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "rk_block.h"
+
+namespace rkb {
+
+using bf16 = __bf16;
+using f16 = _Float16;
+template <class T, int N>
+using vec = T __attribute__((ext_vector_type(N)));
+using f32x4 = vec<float, 4>;
+using f32x8 = vec<float, 8>;
+using u32x4 = vec<uint32_t, 4>;
+
+constexpr int WAVE = 64;
+constexpr int GROUP = RKB_GROUP;
+
+template <class T>
+constexpr int CHUNK = 16 / sizeof(T);  // elements of a 16-byte chunk
+
+// Largest power of two 2^e at which a group's codes may pass 63 (see rk_block.h): above it
+// 64 * 2^e is no finite value of T.
+template <class T>
+inline constexpr int CODE_TOP_EXP = 121;  // bf16 and f32: 64 * 2^122 = 2^128
+template <>
+inline constexpr int CODE_TOP_EXP<f16> = 9;  // 64 * 2^10 = 65536
+
+// Chunk of a row, `left` of whose elements exist (any number; the others read as 0).  The
+// pointer has the alignment of T only: global loads take any address on gfx950.
+template <class T>
+__device__ inline void load_chunk(const T *p, int64_t left, float (&v)[CHUNK<T>])
+{
+    constexpr int N = CHUNK<T>;
+    if (left >= N) {
+        vec<T, N> t;
+        __builtin_memcpy(&t, p, 16);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = (float)t[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = i < left ? (float)p[i] : 0.0f;
+    }
+}
+
+template <class T>
+__device__ inline void store_chunk(T *p, int64_t left, const float (&v)[CHUNK<T>])
+{
+    constexpr int N = CHUNK<T>;
+    if (left >= N) {
+        vec<T, N> t;
+#pragma unroll
+        for (int i = 0; i < N; ++i) t[i] = (T)v[i];
+        __builtin_memcpy(p, &t, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (i < left) p[i] = (T)v[i];
+    }
+}
+
+// Eight columns: one chunk of a 16-bit type, two of a 32-bit one.
+template <class T>
+__device__ inline void load8(const T *p, int64_t left, float (&v)[8])
+{
+    constexpr int N = CHUNK<T>;
+#pragma unroll
+    for (int k = 0; k < 8; k += N) {
+        float c[N];
+        load_chunk<T>(p + k, left - k, c);
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[k + i] = c[i];
+    }
+}
+
+template <class T>
+__device__ inline void store8(T *p, int64_t left, const float (&v)[8])
+{
+    constexpr int N = CHUNK<T>;
+#pragma unroll
+    for (int k = 0; k < 8; k += N) {
+        float c[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) c[i] = v[k + i];
+        store_chunk<T>(p + k, left - k, c);
+    }
+}
+
+__device__ inline float two_to(int e)  // 2^e for -126 <= e <= 127
+{
+    return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+// Exponent of a group's step from max|x|: the least e >= -126 with top <= 127 * 2^e.  With
+// top = m * 2^k, 1 <= m < 2, that is k - 6 for m <= 127/64 (its fraction bits 0x7e0000), else k - 5.
+__device__ inline int step_exp(float top)
+{
+    const uint32_t b = __float_as_uint(top);
+    const int e = (int)(b >> 23) - 127 - ((b & 0x7fffffu) <= 0x7e0000u ? 6 : 5);
+    return max(e, -126);
+}
+
+__device__ inline bool finite(float top)  // top >= 0 or NaN
+{
+    return __float_as_uint(top) < 0x7f800000u;
+}
+
+// max(a, |b|) that keeps NaN: bit patterns of non-negative floats are ordered as the
+// floats, infinity and then NaN above them.
+__device__ inline uint32_t max_bits(uint32_t a, float b)
+{
+    return max(a, __float_as_uint(b) & 0x7fffffffu);
+}
+
+__device__ inline int code_of(float x, float inv_step, float limit)
+{
+    return (int)fminf(fmaxf(rintf(x * inv_step), -limit), limit);
+}
+
+// The value that stands for a group's stored exponent byte: its step, or NaN.
+__device__ inline float step_of(uint8_t exp_byte)
+{
+    return exp_byte == 255 ? __uint_as_float(0x7fc00000u) : two_to((int)exp_byte - 127);
+}
+
+// Sum over groups of LANES neighbouring lanes (LANES a power of two up to 64), in every lane.
+template <int LANES>
+__device__ inline float lane_sum(float v)
+{
+#pragma unroll
+    for (int d = 1; d < LANES; d *= 2) v += __shfl_xor(v, d);
+    return v;
+}
+
+inline bool good_dtype(int dtype) { return dtype == RKB_F32 || dtype == RKB_F16 || dtype == RKB_BF16; }
+inline bool good_dtype16(int dtype) { return dtype == RKB_F16 || dtype == RKB_BF16; }
+inline int dtype_size(int dtype) { return dtype == RKB_F32 ? 4 : 2; }
+
+inline bool good_size(int64_t rows, int64_t cols)
+{
+    return rows >= 0 && rows <= RKB_MAX_ROWS && cols >= 1 && cols <= RKB_MAX_COLS;
+}
+
+// A matrix argument: present, aligned to its type, with rows that do not overlap (a stride is not read for one row).
+inline bool good_matrix(const void *p, int64_t rows, int64_t cols, int64_t stride, int size)
+{
+    if (rows == 0) return true;
+    return p && (uintptr_t)p % size == 0 && (rows == 1 || (stride >= cols && stride <= ((int64_t)1 << 40)));
+}
+
+inline int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+inline int64_t code_ld(int64_t cols) { return round_up(cols, GROUP); }
+
+inline int launched() { return hipGetLastError() == hipSuccess ? RKB_OK : RKB_E_DEVICE; }
+
+}  // namespace rkb

@@ -1,0 +1,118 @@
+"""librkblock's C ABI on a host without a GPU: exports, constants, workspace sizes, and the
+refusal of bad arguments before any device call."""
+import ctypes as C
+import os
+import re
+
+import pytest
+import torch
+
+from paper_2307_01236_amd import block as bk
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = open(os.path.join(ROOT, "include", "rk_block.h")).read()
+P = 1 << 20  # a pointer-like number that is never read: the calls below refuse first
+
+
+def test_exports_every_declared_symbol():
+    text = re.sub(r"/\*.*?\*/", "", HEADER, flags=re.S)
+    names = set(re.findall(r"\b(rkb_[a-z0-9_]+)\s*\(", text))
+    assert names == set(bk.EXPORTS)
+    for n in names:
+        assert hasattr(bk.load(), n), n
+
+
+def test_constants_match_header():
+    for name in ("RKB_OK", "RKB_E_INVAL", "RKB_E_NOMEM", "RKB_E_DEVICE", "RKB_F32", "RKB_F16", "RKB_BF16", "RKB_SILU",
+                 "RKB_GELU", "RKB_KEEP_NONE", "RKB_KEEP_FULL", "RKB_KEEP_8BIT",
+                 "RKB_KEEP_16BIT"):
+        m = re.search(rf"\b{name}\s*=\s*(-?\d+)", HEADER)
+        assert m and int(m.group(1)) == getattr(bk, name), name
+    assert f"#define RKB_MAX_NORM_COLS {bk.RKB_MAX_NORM_COLS} " in HEADER
+    assert f"#define RKB_GROUP {bk.RKB_GROUP} " in HEADER
+    assert "#define RKB_MAX_ROWS ((int64_t)1 << 30)" in HEADER and bk.RKB_MAX_ROWS == 1 << 30
+    assert "#define RKB_MAX_COLS ((int64_t)1 << 24)" in HEADER and bk.RKB_MAX_COLS == 1 << 24
+
+
+def test_strerror():
+    assert bk.rkb_strerror(0) == "ok" and "invalid" in bk.rkb_strerror(-1) and bk.rkb_strerror(77) == "unknown error"
+
+
+# A valid argument list of each call (not run), and per call replacements that make it invalid.
+NORM_FWD = dict(dtype=bk.RKB_BF16, wdtype=bk.RKB_BF16, rows=4, cols=64, x=P, xs=64, w=P, b=P, eps=1e-5, y=P, ys=64, mean=P,
+                rstd=P, stream=None)
+NORM_BWD = dict(dtype=bk.RKB_BF16, wdtype=bk.RKB_BF16, rows=4, cols=64, dy=P, dys=64, x=P, xs=64, codes=None, exps=None,
+                mean=P, rstd=P, w=P, dx=P, dxs=64, dw=P, db=P, ws=P, wsb=1 << 20, stream=None)
+SAVE = dict(dtype=bk.RKB_F16, rows=4, cols=64, x=P, xs=64, codes=P, exps=P, stream=None)
+LOAD = dict(dtype=bk.RKB_F16, rows=4, cols=64, codes=P, exps=P, x=P, xs=64, stream=None)
+WGRAD = dict(dtype=bk.RKB_F16, rows=4, n=32, k=64, dy=P, dys=32, x=None, xs=64, codes=P, exps=P, dw=P, dws=64, ws=P,
+             wsb=1 << 24, stream=None)
+FWD = dict(dtype=bk.RKB_F16, act=0, keep=2, rows=4, d=64, f=32, x=P, xs=64, wg=P, wgs=64, wu=P, wus=64, h=P, hs=32, g=P, u=P,
+           ge=P, ue=P, ws=P, wsb=1 << 24, stream=None)
+BWD = dict(dtype=bk.RKB_F16, act=0, keep=2, rows=4, d=64, f=32, dh=P, dhs=32, x=P, xs=64, wg=P, wgs=64, wu=P, wus=64, g=P,
+           u=P, ge=P, ue=P, dx=P, dxs=64, dwg=P, dwu=P, dws=64, h=P, hs=32, ws=P, wsb=1 << 24, stream=None)
+CALLS = dict(rkb_layer_norm_fwd=NORM_FWD, rkb_layer_norm_bwd=NORM_BWD, rkb_ckpt8_save=SAVE, rkb_ckpt8_load=LOAD,
+             rkb_weight_grad=WGRAD, rkb_gated_fwd=FWD, rkb_gated_bwd=BWD)
+COMMON = [dict(dtype=3), dict(dtype=-1), dict(rows=-1), dict(rows=(1 << 30) + 1)]
+REFUSED = dict(
+    rkb_layer_norm_fwd=COMMON + [dict(cols=0), dict(cols=16385), dict(x=None), dict(y=None), dict(x=P + 1), dict(xs=63),
+                                 dict(ys=63), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")),
+                                 dict(wdtype=bk.RKB_F16), dict(w=P + 1), dict(mean=P + 2)],
+    rkb_layer_norm_bwd=COMMON + [dict(cols=0), dict(cols=16385), dict(dy=None), dict(x=None), dict(dx=None), dict(dys=63),
+                                 dict(codes=P), dict(exps=P), dict(x=None, codes=P), dict(x=None, codes=P + 8, exps=P),
+                                 dict(mean=None), dict(rstd=None), dict(ws=None), dict(ws=P + 16), dict(wdtype=bk.RKB_F16)],
+    rkb_ckpt8_save=COMMON + [dict(cols=0), dict(cols=(1 << 24) + 1), dict(x=None), dict(xs=63), dict(codes=None),
+                             dict(exps=None), dict(codes=P + 8), dict(x=P + 1)],
+    rkb_ckpt8_load=COMMON + [dict(cols=0), dict(x=None), dict(xs=63), dict(codes=None), dict(exps=None), dict(codes=P + 8)],
+    rkb_weight_grad=COMMON + [dict(dtype=bk.RKB_F32), dict(n=0), dict(k=0), dict(dy=None), dict(dys=31), dict(dw=None),
+                              dict(dws=63), dict(x=P), dict(codes=None), dict(exps=None), dict(codes=None, exps=None),
+                              dict(codes=P + 4), dict(ws=None), dict(ws=P + 8)],
+    rkb_gated_fwd=COMMON + [dict(dtype=bk.RKB_F32), dict(act=2), dict(act=-1), dict(keep=4), dict(keep=3), dict(keep=-1), dict(d=0),
+                            dict(f=0), dict(x=None), dict(wg=None), dict(wu=None), dict(h=None), dict(xs=63), dict(wgs=63),
+                            dict(wus=63), dict(hs=31), dict(g=None), dict(ge=None), dict(u=P + 8), dict(keep=1),
+                            dict(keep=0)],
+    rkb_gated_bwd=COMMON + [dict(dtype=bk.RKB_F32), dict(act=2), dict(keep=4), dict(keep=3), dict(d=0), dict(f=0), dict(dh=None),
+                            dict(x=None), dict(wg=None), dict(wu=None), dict(dhs=31), dict(xs=63), dict(g=None),
+                            dict(ue=None), dict(keep=1), dict(keep=0), dict(dwg=None), dict(dwu=None), dict(dws=63),
+                            dict(dxs=63), dict(hs=31), dict(ws=None), dict(ws=P + 64)],
+)
+
+
+@pytest.mark.parametrize("name", sorted(CALLS))
+def test_bad_arguments_are_refused(name):
+    fn = getattr(bk.load(), name)
+    for change in REFUSED[name]:
+        args = {**CALLS[name], **change}
+        assert fn(*args.values()) == bk.RKB_E_INVAL, change
+
+
+def test_short_workspaces_are_refused():
+    lib, n = bk.load(), C.c_size_t(0)
+    for name, ask in (("rkb_layer_norm_bwd", (bk.RKB_BF16, 4, 64)), ("rkb_weight_grad", (bk.RKB_F16, 4, 32, 64, 1)),
+                      ("rkb_gated_bwd", (bk.RKB_F16, 2, 4, 64, 32))):
+        assert getattr(lib, name + "_workspace")(*ask, C.byref(n)) == bk.RKB_OK and n.value > 0
+        args = {**CALLS[name], "wsb": n.value - 1}
+        assert getattr(lib, name)(*args.values()) == bk.RKB_E_NOMEM
+        assert getattr(lib, name + "_workspace")(*ask, None) == bk.RKB_E_INVAL
+    assert lib.rkb_gated_fwd_workspace(bk.RKB_F16, 4, 64, 32, C.byref(n)) == bk.RKB_OK
+    assert lib.rkb_gated_bwd_workspace(bk.RKB_F16, 5, 4, 64, 32, C.byref(n)) == bk.RKB_E_INVAL
+
+
+def test_no_rows_need_no_pointers():
+    """Nothing to compute and nothing to clear: no device call is made."""
+    none = dict(x=None, y=None, h=None, codes=None, exps=None, mean=None, rstd=None, w=None, b=None, rows=0)
+    for name, args in (("rkb_layer_norm_fwd", NORM_FWD), ("rkb_ckpt8_save", SAVE), ("rkb_ckpt8_load", LOAD),
+                       ("rkb_gated_fwd", FWD)):
+        args = {**args, **{k: v for k, v in none.items() if k in args}}
+        assert getattr(bk.load(), name)(*args.values()) == bk.RKB_OK, name
+
+
+def test_the_binding_refuses_host_tensors_and_other_types():
+    x = torch.zeros(4, 64, dtype=torch.bfloat16)
+    for call in (lambda: bk.rkb_layer_norm_fwd(x), lambda: bk.rkb_ckpt8_save(x), lambda: bk.rkb_gated_fwd(x, x, x),
+                 lambda: bk.rkb_layer_norm_fwd(torch.zeros(4, 64, dtype=torch.float64)), lambda: bk.rkb_ckpt8_load(x),
+                 lambda: bk.rkb_gated_fwd(x, x, x, act="relu"), lambda: bk.rkb_gated_fwd(x, x, x, keep="some"),
+                 lambda: bk.rkb_weight_grad(x.float(), x)):
+        with pytest.raises(bk.RKBError) as e:
+            call()
+        assert e.value.code == bk.RKB_E_INVAL
