@@ -23,7 +23,10 @@
  * the host or kept between calls, and no call records anything but kernels, so all may be
  * captured into a HIP graph.  Calls that need scratch memory take a caller's workspace, 256-byte
  * aligned, of at least the bytes that the matching ..._workspace call reports; its contents
- * matter only while the call's kernels run.  Results do not depend on what ran before or
+ * matter only while the call's kernels run.  Products read their operands (x, dy, wg, wu) in 16-byte
+ * chunks; `aligned` of a ..._workspace call says that each of them starts at a multiple of 16 bytes and
+ * has a row stride that is a multiple of 8 elements and at most 2^22 (wg and wu the same stride), and 0 asks for
+ * room for copies that are.  Results do not depend on what ran before or
  * beside: every sum has a fixed order.  Calls are thread-safe.  Nothing is thrown across the
  * ABI.
  */
@@ -95,8 +98,9 @@ int rkb_ckpt8_load(int dtype, int64_t rows, int64_t cols, const int8_t *codes, c
 /*
  * Weight gradient of y = x W^T: dw [n, k] = dy^T x, summed over rows; dy [rows, n], x [rows, k], given as it
  * was or as its checkpoint, as above.  dtype: RKB_F16 or RKB_BF16.  rows == 0 gives zeros.
+ * ckpt of the workspace call: whether x is given as its checkpoint.
  */
-int rkb_weight_grad_workspace(int dtype, int64_t rows, int64_t n, int64_t k, int ckpt, size_t *bytes);
+int rkb_weight_grad_workspace(int dtype, int64_t rows, int64_t n, int64_t k, int ckpt, int aligned, size_t *bytes);
 int rkb_weight_grad(int dtype, int64_t rows, int64_t n, int64_t k, const void *dy, int64_t dy_stride,
                     const void *x, int64_t x_stride, const int8_t *codes, const uint8_t *exps, void *dw,
                     int64_t dw_stride, void *workspace, size_t ws_bytes, void *stream);
@@ -111,7 +115,7 @@ int rkb_weight_grad(int dtype, int64_t rows, int64_t n, int64_t k, const void *d
  *   RKB_KEEP_8BIT  g, u receive the codes and ge, ue the exps of the checkpoints of g and u, taken
  *                  from the 32-bit sums (as of type RKB_F32)
  */
-int rkb_gated_fwd_workspace(int dtype, int64_t rows, int64_t d, int64_t f, size_t *bytes);
+int rkb_gated_fwd_workspace(int dtype, int64_t rows, int64_t d, int64_t f, int aligned, size_t *bytes);
 int rkb_gated_fwd(int dtype, int act, int keep, int64_t rows, int64_t d, int64_t f, const void *x,
                   int64_t x_stride, const void *wg, int64_t wg_stride, const void *wu, int64_t wu_stride, void *h,
                   int64_t h_stride, void *g, void *u, uint8_t *ge, uint8_t *ue, void *workspace,
@@ -125,7 +129,7 @@ int rkb_gated_fwd(int dtype, int act, int keep, int64_t rows, int64_t d, int64_t
  * both of dwg and dwu may be NULL.  h: NULL, or [rows, f] of dtype, receives act(g) u of the same g and u, for the weight
  * gradient of the layer that follows.  rows == 0 gives zero weight gradients.
  */
-int rkb_gated_bwd_workspace(int dtype, int keep, int64_t rows, int64_t d, int64_t f, size_t *bytes);
+int rkb_gated_bwd_workspace(int dtype, int keep, int64_t rows, int64_t d, int64_t f, int aligned, size_t *bytes);
 int rkb_gated_bwd(int dtype, int act, int keep, int64_t rows, int64_t d, int64_t f, const void *dh,
                   int64_t dh_stride, const void *x, int64_t x_stride, const void *wg, int64_t wg_stride,
                   const void *wu, int64_t wu_stride, const void *g, const void *u, const uint8_t *ge,

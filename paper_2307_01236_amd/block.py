@@ -58,11 +58,11 @@ def load():
         lib.rkb_layer_norm_bwd.argtypes = [i, i, l, l, p, l, p, l, p, p, p, p, p, p, l, p, p, p, sz, p]
         lib.rkb_ckpt8_save.argtypes = [i, l, l, p, l, p, p, p]
         lib.rkb_ckpt8_load.argtypes = [i, l, l, p, p, p, l, p]
-        lib.rkb_weight_grad_workspace.argtypes = [i, l, l, l, i, szp]
+        lib.rkb_weight_grad_workspace.argtypes = [i, l, l, l, i, i, szp]
         lib.rkb_weight_grad.argtypes = [i, l, l, l, p, l, p, l, p, p, p, l, p, sz, p]
-        lib.rkb_gated_fwd_workspace.argtypes = [i, l, l, l, szp]
+        lib.rkb_gated_fwd_workspace.argtypes = [i, l, l, l, i, szp]
         lib.rkb_gated_fwd.argtypes = [i, i, i, l, l, l] + [p, l] * 4 + [p] * 4 + [p, sz, p]
-        lib.rkb_gated_bwd_workspace.argtypes = [i, i, l, l, l, szp]
+        lib.rkb_gated_bwd_workspace.argtypes = [i, i, l, l, l, i, szp]
         lib.rkb_gated_bwd.argtypes = [i, i, i, l, l, l] + [p, l] * 4 + [p] * 4 + [p, l, p, p, l, p, l, p, sz, p]
         lib.rkb_strerror.argtypes = [i]
         lib.rkb_strerror.restype = C.c_char_p
@@ -188,6 +188,16 @@ def _workspace(query, device, where: str, *args):
     return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
 
 
+def _aligned(p: int, stride: int) -> bool:
+    return p % 16 == 0 and stride % 8 == 0 and stride <= 1 << 22
+
+
+def _plain(mats) -> bool:
+    """Whether x, wg and wu need no aligned copies (rk_block.h)."""
+    xp, xs, wgp, wgs, wup, wus = mats
+    return _aligned(xp, xs) and _aligned(wgp, wgs) and _aligned(wup, wus) and wgs == wus
+
+
 def _space(ws):
     return (ws.data_ptr(), ws.numel()) if ws is not None else (None, 0)
 
@@ -290,7 +300,8 @@ def rkb_weight_grad(dy, x) -> torch.Tensor:
     xp, xs, codes, exps = _kept(x, where, dy.dtype, dy.device, rows, k)
     with _on(dy.device) as stream:
         dw = torch.empty(n, k, dtype=dy.dtype, device=dy.device)
-        ws = _workspace(lib.rkb_weight_grad_workspace, dy.device, where, dt, rows, n, k, codes is not None)
+        aligned = _aligned(p, stride) and (codes is not None or _aligned(xp, xs))
+        ws = _workspace(lib.rkb_weight_grad_workspace, dy.device, where, dt, rows, n, k, codes is not None, aligned)
         _check(lib.rkb_weight_grad(dt, rows, n, k, p, stride, xp, xs, codes, exps, dw.data_ptr(), k, *_space(ws), stream),
                where)
     return dw
@@ -325,7 +336,7 @@ def rkb_gated_fwd(x, wg, wu, act: str = "silu", keep: str = "none"):
         elif keep == "8bit":
             kept = tuple(Ckpt8(*_new_ckpt(rows, f, x.device), shape, torch.float32) for _ in range(2))
             ptrs = tuple(c.codes.data_ptr() for c in kept) + tuple(c.exps.data_ptr() for c in kept)
-        ws = _workspace(lib.rkb_gated_fwd_workspace, x.device, where, dt, rows, d, f)
+        ws = _workspace(lib.rkb_gated_fwd_workspace, x.device, where, dt, rows, d, f, _plain(mats))
         _check(lib.rkb_gated_fwd(dt, _ACT[act], _KEEP[keep], rows, d, f, *mats, h.data_ptr(), f, *ptrs, *_space(ws),
                                  stream), where)
     return h, kept
@@ -357,7 +368,7 @@ def rkb_gated_bwd(dh, x, wg, wu, act: str = "silu", kept=None, want_h: bool = Fa
         dwg = torch.empty(f, d, dtype=x.dtype, device=x.device)
         dwu = torch.empty_like(dwg)
         h = torch.empty(dh.shape, dtype=x.dtype, device=x.device) if want_h else None
-        ws = _workspace(lib.rkb_gated_bwd_workspace, x.device, where, dt, keep, rows, d, f)
+        ws = _workspace(lib.rkb_gated_bwd_workspace, x.device, where, dt, keep, rows, d, f, _plain(mats))
         _check(lib.rkb_gated_bwd(dt, _ACT[act], keep, rows, d, f, dhp, dhs, *mats, *ptrs, dx.data_ptr(), d, dwg.data_ptr(),
                                  dwu.data_ptr(), d, h.data_ptr() if want_h else None, f, *_space(ws), stream), where)
     return dx, dwg, dwu, h

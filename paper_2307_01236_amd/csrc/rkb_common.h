@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "rk_block.h"
 
@@ -47,6 +48,16 @@ __device__ inline void load_chunk(const T *p, int64_t left, float (&v)[CHUNK<T>]
     }
 }
 
+// A 32-bit result before it is rounded to T.  The compiler may fold a product into its rounding to
+// f16 in one place and not in another (one rounding or two); here it is two everywhere, so that what
+// is made again is bit for bit what it was.
+template <class T>
+__device__ inline float settled(float v)
+{
+    if constexpr (std::is_same_v<T, f16>) asm("" : "+v"(v));
+    return v;
+}
+
 template <class T>
 __device__ inline void store_chunk(T *p, int64_t left, const float (&v)[CHUNK<T>])
 {
@@ -54,12 +65,12 @@ __device__ inline void store_chunk(T *p, int64_t left, const float (&v)[CHUNK<T>
     if (left >= N) {
         vec<T, N> t;
 #pragma unroll
-        for (int i = 0; i < N; ++i) t[i] = (T)v[i];
+        for (int i = 0; i < N; ++i) t[i] = (T)settled<T>(v[i]);
         __builtin_memcpy(p, &t, 16);
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i)
-            if (i < left) p[i] = (T)v[i];
+            if (i < left) p[i] = (T)settled<T>(v[i]);
     }
 }
 

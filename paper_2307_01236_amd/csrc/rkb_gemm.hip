@@ -3,7 +3,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "rkb_common.h"
+#include "rkb_tile.h"
 
 namespace rkb {
 namespace {
@@ -25,30 +25,24 @@ __device__ inline void activate(float g, float &value, float &slope)
     }
 }
 
-// ------------------------------------------------------------------ matrix units
-
-template <class T>
-using frag = vec<T, 8>;
-
-__device__ inline f32x4 mma(frag<bf16> a, frag<bf16> b, f32x4 c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-}
-__device__ inline f32x4 mma(frag<f16> a, frag<f16> b, f32x4 c)
-{
-    return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
-}
-
 // ------------------------------------------------------------------ what becomes of a product
 //
-// A wave hands out its results in units of 16 rows by 32 columns: lane l has the 8 columns
-// from 8 (l / 16) of row l % 16.  A unit's columns are one checkpoint group, held by 4 lanes.
+// A wave hands out its results in units of 16 rows by 32 columns: lane l has 8 neighbouring columns of
+// row l % 16.  A unit's columns are one checkpoint group, held by the lanes l, l + 16, l + 32 and l + 48.
 // Units reach past the matrix's edge; `row` and `col` are compared with its size here.
 
 template <class T>
 struct out_matrix {
     T *p;
     int64_t stride, rows, cols;
+    // The same into rows whose columns go on to a multiple of 8: those past the end become 0.
+    __device__ void put_padded(int64_t row, int64_t col, float (&v)[8]) const
+    {
+        if (row >= rows || col >= cols) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = col + i < cols ? v[i] : 0.0f;
+        store8<T>(p + row * stride + col, 8, v);
+    }
     __device__ void put(int64_t row, int64_t col, const float (&v)[8]) const
     {
         if (p && row < rows && col < cols) store8<T>(p + row * stride + col, cols - col, v);
@@ -140,96 +134,116 @@ struct epi_gated_bwd {
         float d[8], a[8], b[8], c[8];
         load8<T>(dh + row * dhs + col, dg.cols - col, d);
         gated_grads<T, ACT>(gv, uv, d, a, b, c);
-        dg.put(row, col, a);
-        du.put(row, col, b);
+        dg.put_padded(row, col, a);
+        du.put_padded(row, col, b);
         h.put(row, col, c);
     }
 };
 
+constexpr size_t WS_ALIGN = 256;
+
 // ------------------------------------------------------------------ products
 
-// Element (r, k) of an operand lies at p + r * row + k * red.
-template <class T>
-struct operand {
-    const T *p;
-    int64_t row, red;
-};
-
-// C[m, n] = sum over k < K of A(m, k) B(n, k).  SUMS of the epilogue = 1: the sum of `parts` products with operand
-// pairs (a[i], b[i]); 2: the products a[0] b[0] and a[0] b[1] side by side.  gridDim.z = 2 runs two
-// problems, the second with a[1] (and b[0]), where parts = 1.
-template <class T>
-struct problem {
-    operand<T> a[2], b[2];
-    int64_t M, N, K;
-    int parts;
-};
-
-constexpr int ST = 64, SK = 32, SPAD = 8;  // tile side, depth, and LDS padding in elements
-
-template <class T>
-__device__ inline void stage(T (&to)[ST][SK + SPAD], const operand<T> &from, int64_t r0, int64_t rows, int64_t k0, int64_t K)
+template <class T, class EPI, int TM, int TN, int WM, int WN, bool ANEAR, bool BNEAR>
+int launch_product(product pr, const EPI &epi, hipStream_t st)
 {
-    const bool k_near = from.red == 1;  // neighbouring lanes read neighbouring addresses
-#pragma unroll
-    for (int i = 0; i < ST * SK / 256; ++i) {
-        const int e = i * 256 + threadIdx.x;
-        const int r = k_near ? e / SK : e % ST, k = k_near ? e % SK : e / ST;
-        const bool in = r0 + r < rows && k0 + k < K;
-        to[r][k] = in ? from.p[(r0 + r) * from.row + (k0 + k) * from.red] : (T)0.0f;
-    }
-}
-
-template <class T, class EPI>
-__global__ __launch_bounds__(256) void k_simple(problem<T> pr, EPI epi)
-{
-    constexpr int SUMS = EPI::SUMS;
-    __shared__ T as[ST][SK + SPAD], bs[SUMS][ST][SK + SPAD];
-    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE;
-    const int64_t m0 = (int64_t)blockIdx.y * ST, n0 = (int64_t)blockIdx.x * ST;
-    const int which = blockIdx.z;
-    f32x4 acc[SUMS][4] = {};
-    for (int part = 0; part < pr.parts; ++part) {
-        for (int64_t k0 = 0; k0 < pr.K; k0 += SK) {
-            __syncthreads();
-            stage<T>(as, pr.a[part + which], m0, pr.M, k0, pr.K);
-#pragma unroll
-            for (int s = 0; s < SUMS; ++s) stage<T>(bs[s], pr.b[SUMS == 2 ? s : part], n0, pr.N, k0, pr.K);
-            __syncthreads();
-            const int r = lane % 16, k = lane / 16 * 8;
-            const frag<T> fa = *(const frag<T> *)&as[wave * 16 + r][k];
-#pragma unroll
-            for (int s = 0; s < SUMS; ++s)
-#pragma unroll
-                for (int f = 0; f < 4; ++f) {
-                    // fragment f of a unit holds its columns 8 q + 4 (f % 2) + i, q = 0..3, i = 0..3
-                    const int n = f / 2 * 32 + r / 4 * 8 + f % 2 * 4 + r % 4;
-                    acc[s][f] = mma(*(const frag<T> *)&bs[s][n][k], fa, acc[s][f]);
-                }
-        }
-    }
-#pragma unroll
-    for (int unit = 0; unit < 2; ++unit) {
-        const int64_t row = m0 + wave * 16 + lane % 16, col = n0 + unit * 32 + lane / 16 * 8;
-        float v[SUMS][8];
-#pragma unroll
-        for (int s = 0; s < SUMS; ++s)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[s][i] = acc[s][unit * 2 + i / 4][i % 4];
-        if constexpr (SUMS == 1)
-            epi(which, row, col, v[0]);
-        else
-            epi(which, row, col, v[0], v[1]);
-    }
-}
-
-template <class T, class EPI>
-int run_problem(const problem<T> &pr, int problems, const EPI &epi, hipStream_t st)
-{
-    const dim3 grid((uint32_t)((pr.N + ST - 1) / ST), (uint32_t)((pr.M + ST - 1) / ST), problems);
-    hipLaunchKernelGGL((k_simple<T, EPI>), grid, dim3(256), 0, st, pr, epi);
+    pr.tiles_m = (int)((pr.M + TM - 1) / TM);
+    pr.tiles_n = (int)((pr.N + TN / EPI::SUMS - 1) / (TN / EPI::SUMS));
+    pr.splits = 1;
+    pr.split_stages = (int)((pr.K + DEPTH - 1) / DEPTH) * pr.parts;
+    const int64_t total = (int64_t)pr.tiles_m * pr.tiles_n * pr.problems * pr.splits;
+    hipLaunchKernelGGL((k_product<T, EPI, TM, TN, WM, WN, ANEAR, BNEAR>), dim3((uint32_t)total), dim3(WM * WN * WAVE), 0, st,
+                       pr, epi);
     return launched();
 }
+
+template <class T, bool ANEAR, bool BNEAR, class EPI>
+int run_product(const product &pr, const EPI &epi, hipStream_t st)
+{
+    return launch_product<T, EPI, 128, 128, 2, 2, ANEAR, BNEAR>(pr, epi, st);
+}
+
+// ------------------------------------------------------------------ operands
+//
+// The products copy 16 bytes at a time from 16-byte aligned rows of a multiple of 8 columns.  A matrix that is laid
+// out otherwise is copied into the workspace once, its rows ending in zeros: one more pass
+// over that matrix, against the many that its product makes.
+
+constexpr int64_t STRIDE_LIMIT = (int64_t)1 << 22;  // 256 rows' offsets stay in 32 bits
+
+struct matrix {
+    const void *p;
+    int64_t stride, rows, cols;
+    bool aligned() const
+    {
+        return cols % 8 == 0 && (uintptr_t)p % 16 == 0 && (rows <= 1 || (stride % 8 == 0 && stride <= STRIDE_LIMIT));
+    }
+};
+
+size_t padded_bytes(int64_t rows, int64_t cols) { return (size_t)round_up(rows * round_up(cols, 8) * 2, WS_ALIGN); }
+
+struct pad_job {
+    const uint16_t *from;
+    uint16_t *to;
+    int64_t stride, rows;
+    int cols, chunks;
+};
+struct pad_jobs {
+    pad_job job[3];
+};
+
+__global__ __launch_bounds__(256) void k_pad(pad_jobs jobs)
+{
+    const pad_job j = jobs.job[blockIdx.y];
+    const int64_t all = j.rows * j.chunks;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const int64_t r = i / j.chunks;
+        const int c = (int)(i - r * j.chunks) * 8, left = j.cols - c;
+        const uint16_t *from = j.from + r * j.stride + c;
+        vec<uint16_t, 8> v;
+        if (left >= 8) {
+            __builtin_memcpy(&v, from, 16);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = e < left ? from[e] : (uint16_t)0;
+        }
+        *(vec<uint16_t, 8> *)(j.to + i * 8) = v;
+    }
+}
+
+// Takes scratch memory in order, and replaces matrices that are not aligned by copies in it.
+struct workspace_taker {
+    char *at, *end;
+    pad_jobs jobs;
+    int n_jobs = 0;
+
+    workspace_taker(void *ws, size_t bytes) : at((char *)ws), end((char *)ws + bytes) {}
+    void *take(size_t bytes)
+    {
+        char *p = at;
+        at += bytes;
+        return p;
+    }
+    bool fits() const { return at <= end; }
+    void align(matrix &m, bool force = false)
+    {
+        if (m.rows <= 1) m.stride = round_up(m.cols, 8);
+        if (m.rows == 0 || (m.aligned() && !force)) return;
+        const int64_t ld = round_up(m.cols, 8);
+        void *to = take(padded_bytes(m.rows, m.cols));
+        jobs.job[n_jobs++] = pad_job{(const uint16_t *)m.p, (uint16_t *)to, m.stride, m.rows, (int)m.cols, (int)(ld / 8)};
+        m.p = to;
+        m.stride = ld;
+    }
+    int run(hipStream_t st)
+    {
+        if (!n_jobs) return RKB_OK;
+        int64_t most = 0;
+        for (int i = 0; i < n_jobs; ++i) most = std::max(most, jobs.job[i].rows * jobs.job[i].chunks);
+        hipLaunchKernelGGL(k_pad, dim3((uint32_t)std::min<int64_t>((most + 255) / 256, 4096), n_jobs), dim3(256), 0, st, jobs);
+        return launched();
+    }
+};
 
 // ------------------------------------------------------------------ the backward pass's elementwise step
 
@@ -261,14 +275,11 @@ __global__ __launch_bounds__(256) void k_gated_grads(const T *__restrict__ dh, i
         }
         load8<T>(dh + row * dhs + col, cols - col, d);
         gated_grads<T, ACT>(gv, uv, d, a, b, c);
-        dg.put(row, col, a);
-        du.put(row, col, b);
+        dg.put_padded(row, col, a);
+        du.put_padded(row, col, b);
         h.put(row, col, c);
     }
 }
-
-constexpr size_t WS_ALIGN = 256;
-size_t padded_bytes(int64_t rows, int64_t cols) { return (size_t)round_up(rows * cols * 2, WS_ALIGN); }
 
 bool good_workspace(const void *ws) { return ws && (uintptr_t)ws % WS_ALIGN == 0; }
 
@@ -292,20 +303,15 @@ int with_kept(int keep, F go)
     return go(std::integral_constant<int, RKB_KEEP_8BIT>());
 }
 
-int load_ckpt(int dtype, int64_t rows, int64_t cols, const int8_t *codes, const uint8_t *exps, void *to, void *stream)
-{
-    return rkb_ckpt8_load(dtype, rows, cols, codes, exps, to, cols, stream);
-}
-
 }  // namespace
 }  // namespace rkb
 
 using namespace rkb;
 
-extern "C" int rkb_weight_grad_workspace(int dtype, int64_t rows, int64_t n, int64_t k, int ckpt, size_t *bytes)
+extern "C" int rkb_weight_grad_workspace(int dtype, int64_t rows, int64_t n, int64_t k, int ckpt, int aligned, size_t *bytes)
 {
     if (!bytes || !good_dtype16(dtype) || !good_size(rows, n) || !good_size(rows, k)) return RKB_E_INVAL;
-    *bytes = ckpt ? padded_bytes(rows, k) : 0;
+    *bytes = (ckpt || k % 8 || !aligned ? padded_bytes(rows, k) : 0) + (n % 8 || !aligned ? padded_bytes(rows, n) : 0);
     return RKB_OK;
 }
 
@@ -313,25 +319,31 @@ extern "C" int rkb_weight_grad(int dtype, int64_t rows, int64_t n, int64_t k, co
                                const void *x, int64_t x_stride, const int8_t *codes, const uint8_t *exps, void *dw,
                                int64_t dw_stride, void *workspace, size_t ws_bytes, void *stream)
 {
-    size_t need = 0;
     const bool ckpt = codes != nullptr;
-    int rc = rkb_weight_grad_workspace(dtype, rows, n, k, ckpt, &need);
-    if (rc != RKB_OK) return rc;
-    if (!good_matrix(dy, rows, n, dy_stride, 2) || !good_matrix(dw, n, k, dw_stride, 2)) return RKB_E_INVAL;
+    if (!good_dtype16(dtype) || !good_size(rows, n) || !good_size(rows, k) || !good_matrix(dy, rows, n, dy_stride, 2) ||
+        !good_matrix(dw, n, k, dw_stride, 2))
+        return RKB_E_INVAL;
     if (rows > 0 && (ckpt ? (x || !exps || (uintptr_t)codes % 16) : (exps || !good_matrix(x, rows, k, x_stride, 2))))
         return RKB_E_INVAL;
-    if (need && !good_workspace(workspace)) return RKB_E_INVAL;
-    if (ws_bytes < need) return RKB_E_NOMEM;
+    const hipStream_t st = (hipStream_t)stream;
+    workspace_taker ws(workspace, ws_bytes);
+    matrix a{dy, dy_stride, rows, n}, b{x, x_stride, rows, k};
     if (ckpt && rows > 0) {
-        rc = load_ckpt(dtype, rows, k, codes, exps, workspace, stream);
-        if (rc != RKB_OK) return rc;
-        x = workspace;
-        x_stride = k;
+        b.p = ws.take(padded_bytes(rows, k));
+        b.stride = round_up(k, 8);
+    } else {
+        ws.align(b);
     }
+    ws.align(a);
+    if (ws.at != workspace && !good_workspace(workspace)) return RKB_E_INVAL;
+    if (!ws.fits()) return RKB_E_NOMEM;
+    int rc = ws.run(st);
+    if (rc == RKB_OK && ckpt && rows > 0) rc = rkb_ckpt8_load(dtype, rows, k, codes, exps, (void *)b.p, b.stride, stream);
+    if (rc != RKB_OK) return rc;
     return with_type16(dtype, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        problem<T> pr{{{(const T *)dy, 1, dy_stride}}, {{(const T *)x, 1, x_stride}}, n, k, rows, 1};
-        return run_problem<T>(pr, 1, epi_store<T>{{{(T *)dw, dw_stride, n, k}}}, (hipStream_t)stream);
+        const product pr{{(const char *)a.p, nullptr}, {(const char *)b.p, nullptr}, a.stride, b.stride, round_up(n, 8), round_up(k, 8), rows, 1, 1};
+        return run_product<T, false, false>(pr, epi_store<T>{{{(T *)dw, dw_stride, n, k}}}, st);
     });
 }
 
@@ -352,12 +364,32 @@ static bool good_kept(int keep, int64_t rows, const void *g, const void *u, cons
     return ge && ue && (uintptr_t)g % 16 == 0 && (uintptr_t)u % 16 == 0;
 }
 
-extern "C" int rkb_gated_fwd_workspace(int dtype, int64_t rows, int64_t d, int64_t f, size_t *bytes)
+extern "C" int rkb_gated_fwd_workspace(int dtype, int64_t rows, int64_t d, int64_t f, int aligned, size_t *bytes)
 {
     if (!bytes || !good_gated(dtype, RKB_SILU, RKB_KEEP_NONE, rows, d, f)) return RKB_E_INVAL;
-    *bytes = 0;
+    *bytes = d % 8 || !aligned ? padded_bytes(rows, d) + 2 * padded_bytes(f, d) : 0;
     return RKB_OK;
 }
+
+// x, wg and wu as the products take them.
+struct gated_operands {
+    matrix x, wg, wu;
+    void align(workspace_taker &ws)
+    {
+        ws.align(x);
+        ws.align(wg);
+        ws.align(wu);
+        // a launch's pairs share their strides
+        if (wg.stride != wu.stride) {
+            if (wg.stride != round_up(wg.cols, 8)) ws.align(wg, true);
+            if (wu.stride != round_up(wu.cols, 8)) ws.align(wu, true);
+        }
+    }
+    product sums(int64_t rows, int64_t d, int64_t f) const  // g and u
+    {
+        return product{{(const char *)x.p, nullptr}, {(const char *)wg.p, (const char *)wu.p}, x.stride, wg.stride, rows, f, round_up(d, 8), 1, 1};
+    }
+};
 
 extern "C" int rkb_gated_fwd(int dtype, int act, int keep, int64_t rows, int64_t d, int64_t f, const void *x,
                              int64_t x_stride, const void *wg, int64_t wg_stride, const void *wu, int64_t wu_stride, void *h,
@@ -369,13 +401,20 @@ extern "C" int rkb_gated_fwd(int dtype, int act, int keep, int64_t rows, int64_t
         !good_kept(keep, rows, g, u, ge, ue))
         return RKB_E_INVAL;
     if (rows == 0) return RKB_OK;
+    const hipStream_t st = (hipStream_t)stream;
+    workspace_taker ws(workspace, ws_bytes);
+    gated_operands in{{x, x_stride, rows, d}, {wg, wg_stride, f, d}, {wu, wu_stride, f, d}};
+    in.align(ws);
+    if (ws.at != workspace && !good_workspace(workspace)) return RKB_E_INVAL;
+    if (!ws.fits()) return RKB_E_NOMEM;
+    const int rc = ws.run(st);
+    if (rc != RKB_OK) return rc;
     return with_type16(dtype, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        const problem<T> pr{{{(const T *)x, x_stride, 1}}, {{(const T *)wg, wg_stride, 1}, {(const T *)wu, wu_stride, 1}}, rows, f, d, 1};
         return with_act(act, [&](auto a) {
             auto go = [&](auto kind) {
-                epi_gated_fwd<T, a(), kind()> epi{{(T *)h, h_stride, rows, f}, g, u, ge, ue};
-                return run_problem<T>(pr, 1, epi, (hipStream_t)stream);
+                const epi_gated_fwd<T, a(), kind()> epi{{(T *)h, h_stride, rows, f}, g, u, ge, ue};
+                return run_product<T, true, true>(in.sums(rows, d, f), epi, st);
             };
             if (keep == RKB_KEEP_NONE) return go(std::integral_constant<int, RKB_KEEP_NONE>());
             return with_kept(keep, go);
@@ -383,10 +422,10 @@ extern "C" int rkb_gated_fwd(int dtype, int act, int keep, int64_t rows, int64_t
     });
 }
 
-extern "C" int rkb_gated_bwd_workspace(int dtype, int keep, int64_t rows, int64_t d, int64_t f, size_t *bytes)
+extern "C" int rkb_gated_bwd_workspace(int dtype, int keep, int64_t rows, int64_t d, int64_t f, int aligned, size_t *bytes)
 {
     if (!bytes || !good_gated(dtype, RKB_SILU, keep, rows, d, f)) return RKB_E_INVAL;
-    *bytes = 2 * padded_bytes(rows, f);
+    *bytes = 2 * padded_bytes(rows, f) + (d % 8 || !aligned ? padded_bytes(rows, d) + 2 * padded_bytes(f, d) : 0);
     return RKB_OK;
 }
 
@@ -396,29 +435,29 @@ extern "C" int rkb_gated_bwd(int dtype, int act, int keep, int64_t rows, int64_t
                              const uint8_t *ue, void *dx, int64_t dx_stride, void *dwg, void *dwu, int64_t dw_stride, void *h,
                              int64_t h_stride, void *workspace, size_t ws_bytes, void *stream)
 {
-    size_t need = 0;
-    if (rkb_gated_bwd_workspace(dtype, keep, rows, d, f, &need) != RKB_OK || !good_gated(dtype, act, keep, rows, d, f))
-        return RKB_E_INVAL;
-    if (!good_matrix(dh, rows, f, dh_stride, 2) || !good_matrix(x, rows, d, x_stride, 2) ||
-        !good_matrix(wg, f, d, wg_stride, 2) || !good_matrix(wu, f, d, wu_stride, 2) || !good_kept(keep, rows, g, u, ge, ue) ||
-        (dx && !good_matrix(dx, rows, d, dx_stride, 2)) || (!dwg != !dwu) ||
+    if (!good_gated(dtype, act, keep, rows, d, f) || !good_matrix(dh, rows, f, dh_stride, 2) ||
+        !good_matrix(x, rows, d, x_stride, 2) || !good_matrix(wg, f, d, wg_stride, 2) || !good_matrix(wu, f, d, wu_stride, 2) ||
+        !good_kept(keep, rows, g, u, ge, ue) || (dx && !good_matrix(dx, rows, d, dx_stride, 2)) || (!dwg != !dwu) ||
         (dwg && (!good_matrix(dwg, f, d, dw_stride, 2) || !good_matrix(dwu, f, d, dw_stride, 2))) ||
         (h && !good_matrix(h, rows, f, h_stride, 2)))
         return RKB_E_INVAL;
-    if (need && !good_workspace(workspace)) return RKB_E_INVAL;
-    if (ws_bytes < need) return RKB_E_NOMEM;
     const hipStream_t st = (hipStream_t)stream;
+    workspace_taker ws(workspace, ws_bytes);
+    const int64_t ld = round_up(f, 8);
+    void *dg = ws.take(padded_bytes(rows, f)), *du = ws.take(padded_bytes(rows, f));
+    gated_operands in{{x, x_stride, rows, d}, {wg, wg_stride, f, d}, {wu, wu_stride, f, d}};
+    if (rows > 0) in.align(ws);
+    if (ws.at != workspace && !good_workspace(workspace)) return RKB_E_INVAL;
+    if (!ws.fits()) return RKB_E_NOMEM;
+    int rc = ws.run(st);
+    if (rc != RKB_OK) return rc;
     return with_type16(dtype, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        T *dg = (T *)workspace, *du = (T *)((char *)workspace + padded_bytes(rows, f));
-        const out_matrix<T> og{dg, f, rows, f}, ou{du, f, rows, f}, oh{(T *)h, h_stride, rows, f};
-        int rc = RKB_OK;
+        const out_matrix<T> og{(T *)dg, ld, rows, f}, ou{(T *)du, ld, rows, f}, oh{(T *)h, h_stride, rows, f};
         if (rows > 0)
             rc = with_act(act, [&](auto a) {
-                if (keep == RKB_KEEP_NONE) {
-                    const problem<T> pr{{{(const T *)x, x_stride, 1}}, {{(const T *)wg, wg_stride, 1}, {(const T *)wu, wu_stride, 1}}, rows, f, d, 1};
-                    return run_problem<T>(pr, 1, epi_gated_bwd<T, a()>{(const T *)dh, dh_stride, og, ou, oh}, st);
-                }
+                if (keep == RKB_KEEP_NONE)
+                    return run_product<T, true, true>(in.sums(rows, d, f), epi_gated_bwd<T, a()>{(const T *)dh, dh_stride, og, ou, oh}, st);
                 const dim3 grid((uint32_t)((f + 2047) / 2048), (uint32_t)std::min<int64_t>(rows, 32768));
                 auto go = [&](auto kind) {
                     hipLaunchKernelGGL((k_gated_grads<T, a(), kind()>), grid, dim3(256), 0, st, (const T *)dh, dh_stride, g, u,
@@ -428,12 +467,12 @@ extern "C" int rkb_gated_bwd(int dtype, int act, int keep, int64_t rows, int64_t
                 return with_kept(keep, go);
             });
         if (rc == RKB_OK && dx && rows > 0) {
-            const problem<T> pr{{{dg, f, 1}, {du, f, 1}}, {{(const T *)wg, 1, wg_stride}, {(const T *)wu, 1, wu_stride}}, rows, d, f, 2};
-            rc = run_problem<T>(pr, 1, epi_store<T>{{{(T *)dx, dx_stride, rows, d}}}, st);
+            const product pr{{(const char *)dg, (const char *)du}, {(const char *)in.wg.p, (const char *)in.wu.p}, ld, in.wg.stride, rows, round_up(d, 8), f, 2, 1};
+            rc = run_product<T, true, false>(pr, epi_store<T>{{{(T *)dx, dx_stride, rows, d}}}, st);
         }
         if (rc == RKB_OK && dwg) {
-            const problem<T> pr{{{dg, 1, f}, {du, 1, f}}, {{(const T *)x, 1, x_stride}}, f, d, rows, 1};
-            rc = run_problem<T>(pr, 2, epi_store<T>{{{(T *)dwg, dw_stride, f, d}, {(T *)dwu, dw_stride, f, d}}}, st);
+            const product pr{{(const char *)dg, (const char *)du}, {(const char *)in.x.p, nullptr}, ld, in.x.stride, ld, round_up(d, 8), rows, 1, 2};
+            rc = run_product<T, false, false>(pr, epi_store<T>{{{(T *)dwg, dw_stride, f, d}, {(T *)dwu, dw_stride, f, d}}}, st);
         }
         return rc;
     });

@@ -88,14 +88,14 @@ def test_bad_arguments_are_refused(name):
 
 def test_short_workspaces_are_refused():
     lib, n = bk.load(), C.c_size_t(0)
-    for name, ask in (("rkb_layer_norm_bwd", (bk.RKB_BF16, 4, 64)), ("rkb_weight_grad", (bk.RKB_F16, 4, 32, 64, 1)),
-                      ("rkb_gated_bwd", (bk.RKB_F16, 2, 4, 64, 32))):
+    for name, ask in (("rkb_layer_norm_bwd", (bk.RKB_BF16, 4, 64)), ("rkb_weight_grad", (bk.RKB_F16, 4, 32, 64, 1, 1)),
+                      ("rkb_gated_bwd", (bk.RKB_F16, 2, 4, 64, 32, 1))):
         assert getattr(lib, name + "_workspace")(*ask, C.byref(n)) == bk.RKB_OK and n.value > 0
         args = {**CALLS[name], "wsb": n.value - 1}
         assert getattr(lib, name)(*args.values()) == bk.RKB_E_NOMEM
         assert getattr(lib, name + "_workspace")(*ask, None) == bk.RKB_E_INVAL
-    assert lib.rkb_gated_fwd_workspace(bk.RKB_F16, 4, 64, 32, C.byref(n)) == bk.RKB_OK
-    assert lib.rkb_gated_bwd_workspace(bk.RKB_F16, 5, 4, 64, 32, C.byref(n)) == bk.RKB_E_INVAL
+    assert lib.rkb_gated_fwd_workspace(bk.RKB_F16, 4, 64, 32, 1, C.byref(n)) == bk.RKB_OK
+    assert lib.rkb_gated_bwd_workspace(bk.RKB_F16, 5, 4, 64, 32, 1, C.byref(n)) == bk.RKB_E_INVAL
 
 
 def test_no_rows_need_no_pointers():
