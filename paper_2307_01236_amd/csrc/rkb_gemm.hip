@@ -78,6 +78,17 @@ struct epi_store {
     __device__ void operator()(int which, int64_t row, int64_t col, const float (&v)[8]) const { c[which].put(row, col, v); }
 };
 
+// A split's partial sums, in 32 bits.
+struct epi_part {
+    static constexpr int SUMS = 1;
+    float *p;
+    int64_t rows, cols, ld;  // ld: cols rounded up to 8
+    __device__ void operator()(int which, int64_t row, int64_t col, const float (&v)[8]) const
+    {
+        if (row < rows && col < cols) store8<float>(p + ((int64_t)which * rows + row) * ld + col, 8, v);
+    }
+};
+
 // h = act(g) u, and g and u in the form that the backward pass will read.
 template <class T, int ACT, int KEEP>
 struct epi_gated_fwd {
@@ -141,26 +152,238 @@ struct epi_gated_bwd {
 };
 
 constexpr size_t WS_ALIGN = 256;
+constexpr int64_t MAX_TILES = (int64_t)1 << 22;  // workgroups of a launch: 512 threads of each in 32 bits
 
 // ------------------------------------------------------------------ products
 
-template <class T, class EPI, int TM, int TN, int WM, int WN, bool ANEAR, bool BNEAR>
-int launch_product(product pr, const EPI &epi, hipStream_t st)
+// How a product is cut: the tile, and how many workgroups share the stages of one tile (splits).
+struct cut {
+    int tm, tn, splits;
+    double us;  // what the choice expects it to take
+};
+
+// The tiles, with the microseconds of one stage in a workgroup that runs nearly alone and on a full chip
+// (where the clock is lower and L2 shared), and of a tile's start and end, fitted to measured products
+// of 64 to 8192 rows (bf16).  Small tiles pay more per product and fill the chip sooner: at 8192 x 4096 x 11264 the
+// gated forward takes 1140 us by 256 x 256, 1237 by 192 x 256, 1533 by 128 x 256 and 1368 by 128 x 128; at 1024 x 1280 x 5120
+// it takes 36.7, 30.7, 43.7 and 37.5; at 512 x 1024 x 4096, 27.3, 22.0, 16.7 and 12.4.
+struct tile_kind {
+    int tm, tn, slots;  // slots: workgroups that 256 compute units hold at once
+    double alone, busy, ends;
+};
+constexpr tile_kind TILES[] = {
+    {256, 256, 256, 1.05, 1.68, 5.0},
+    {192, 256, 256, 0.82, 1.29, 4.5},
+    {128, 256, 256, 0.66, 1.07, 4.0},
+    {128, 128, 512, 0.50, 0.97, 3.0},
+};
+constexpr double JOIN_FIXED = 4.0, JOIN_BYTES = 4.5e6;  // microseconds, bytes a microsecond
+
+// The cut that these figures expect to be fastest.  Splits share a long K among workgroups where the tiles alone do
+// not fill the chip, at the price of 32-bit partial sums written and read once: dw of 512 x 512 over 16384
+// rows takes 174 us whole and 25 in 16 splits, of 2048 x 2048 over 2048 rows 28 whole and 34 in 2.
+cut choose_cut(int64_t M, int64_t N, int64_t K, int parts, int problems, int sums, bool near)
+{
+    const int64_t stages = std::max<int64_t>(1, (K + DEPTH - 1) / DEPTH * parts);
+    cut best{256, 256, 1, 1e30};
+    for (const tile_kind &t : TILES) {
+        if (t.tm == 192 && !near) continue;
+        const int64_t tiles = (M + t.tm - 1) / t.tm * ((N + t.tn / sums - 1) / (t.tn / sums)) * problems;
+        for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+            if (splits > 1 && (sums == 2 || splits * 4 > stages || splits * tiles > 2 * t.slots)) break;
+            const int64_t groups = tiles * splits, rounds = groups / t.slots, rest = groups % t.slots;
+            const double each = (double)((stages + splits - 1) / splits);
+            double us = rounds * (each * t.busy + t.ends);
+            if (rest) us += each * (t.alone + (t.busy - t.alone) * rest / t.slots) + t.ends;
+            if (splits > 1) us += JOIN_FIXED + 2.0 * 4.0 * splits * problems * (double)M * N / JOIN_BYTES;
+            if (us < best.us) best = cut{t.tm, t.tn, splits, us};
+        }
+    }
+    return best;
+}
+
+size_t split_bytes(const cut &c, int64_t M, int64_t N, int problems)
+{
+    return c.splits == 1 ? 0 : (size_t)round_up((int64_t)c.splits * problems * M * round_up(N, 8) * 4, WS_ALIGN);
+}
+
+template <class T, bool ANEAR, bool BNEAR, int PARTS, int TM, int TN, int WM, int WN, class EPI>
+int launch_product(product pr, const cut &c, const EPI &epi, hipStream_t st)
 {
     pr.tiles_m = (int)((pr.M + TM - 1) / TM);
     pr.tiles_n = (int)((pr.N + TN / EPI::SUMS - 1) / (TN / EPI::SUMS));
-    pr.splits = 1;
-    pr.split_stages = (int)((pr.K + DEPTH - 1) / DEPTH) * pr.parts;
+    const int stages = (int)((pr.K + DEPTH - 1) / DEPTH) * PARTS;
+    pr.splits = c.splits;
+    pr.split_stages = (stages + c.splits - 1) / c.splits;
     const int64_t total = (int64_t)pr.tiles_m * pr.tiles_n * pr.problems * pr.splits;
-    hipLaunchKernelGGL((k_product<T, EPI, TM, TN, WM, WN, ANEAR, BNEAR>), dim3((uint32_t)total), dim3(WM * WN * WAVE), 0, st,
+    if (total > MAX_TILES) return RKB_E_INVAL;
+    hipLaunchKernelGGL((k_product<T, EPI, TM, TN, WM, WN, ANEAR, BNEAR, PARTS>), dim3((uint32_t)total), dim3(WM * WN * WAVE), 0, st,
                        pr, epi);
     return launched();
 }
 
-template <class T, bool ANEAR, bool BNEAR, class EPI>
-int run_product(const product &pr, const EPI &epi, hipStream_t st)
+template <class T, bool ANEAR, bool BNEAR, int PARTS, class EPI>
+int run_product(const product &pr, const cut &c, const EPI &epi, hipStream_t st)
 {
-    return launch_product<T, EPI, 128, 128, 2, 2, ANEAR, BNEAR>(pr, epi, st);
+    if (c.tn == 128) return launch_product<T, ANEAR, BNEAR, PARTS, 128, 128, 2, 2>(pr, c, epi, st);
+    if (c.tm == 128) return launch_product<T, ANEAR, BNEAR, PARTS, 128, 256, 2, 4>(pr, c, epi, st);
+    if constexpr (ANEAR)
+        if (c.tm == 192) return launch_product<T, ANEAR, BNEAR, PARTS, 192, 256, 2, 4>(pr, c, epi, st);
+    return launch_product<T, ANEAR, BNEAR, PARTS, 256, 256, 2, 4>(pr, c, epi, st);
+}
+
+// The splits' partial sums, in their order.
+template <class T>
+__global__ __launch_bounds__(256) void k_join(const float *__restrict__ parts, int splits, int64_t ld, epi_store<T> out)
+{
+    const out_matrix<T> c = out.c[blockIdx.y];
+    const int64_t chunks = ld / 8, all = c.rows * chunks;
+    parts += (int64_t)blockIdx.y * splits * c.rows * ld;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        float v[8] = {};
+        for (int s = 0; s < splits; ++s) {
+            float w[8];
+            load8<float>(parts + (int64_t)s * c.rows * ld + i * 8, 8, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += w[e];
+        }
+        const int64_t row = i / chunks;
+        c.put(row, (i - row * chunks) * 8, v);
+    }
+}
+
+// A product stored as it is; `scratch` has split_bytes.
+template <class T, bool ANEAR, bool BNEAR, int PARTS>
+int store_product(const product &pr, const cut &c, void *scratch, const epi_store<T> &out, hipStream_t st)
+{
+    if (c.splits == 1) return run_product<T, ANEAR, BNEAR, PARTS>(pr, c, out, st);
+    const int64_t rows = out.c[0].rows, cols = out.c[0].cols, ld = round_up(cols, 8);
+    const int rc = run_product<T, ANEAR, BNEAR, PARTS>(pr, c, epi_part{(float *)scratch, rows, cols, ld}, st);
+    if (rc != RKB_OK) return rc;
+    const int64_t blocks = (rows * ld / 8 + 255) / 256;
+    hipLaunchKernelGGL((k_join<T>), dim3((uint32_t)std::min<int64_t>(blocks, 1 << 16), pr.problems), dim3(256), 0, st,
+                       (const float *)scratch, c.splits, ld, out);
+    return launched();
+}
+
+// ------------------------------------------------------------------ few rows
+//
+// g and u of at most 16 MT rows.  Bound by reading wg and wu once: each workgroup takes 16 NB columns of the
+// hidden layer, its waves a share of d each, and a weight goes from memory to the matrix units' registers
+// without a stop in LDS, whatever its alignment, the next steps' loads in flight while the present ones
+// are multiplied.  The waves' sums are joined in LDS in their order.
+
+constexpr int FEW_WAVES = 8, FEW_STEPS = 2;  // steps of 32 k that are loaded together
+
+// 8 neighbouring k of a row, of which `left` exist (the others read as 0).
+template <class T>
+__device__ inline frag<T> load_frag(const T *p, int left)
+{
+    frag<T> v;
+    if (left >= 8) {
+        __builtin_memcpy(&v, p, 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? p[i] : (T)0.0f;
+    }
+    return v;
+}
+
+template <class T, class EPI, int MT, int NB>
+__global__ __launch_bounds__(FEW_WAVES *WAVE) void k_few(product pr, EPI epi)
+{
+    constexpr int F = 2 * NB;  // fragments of weights
+    __shared__ f32x4 part[FEW_WAVES][MT][F][WAVE];
+    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, r = lane % 16, q = lane / 16;
+    const int64_t n0 = (int64_t)blockIdx.x * (16 * NB);
+    const int K = (int)pr.K, steps = (K + 31) / 32, each = (steps + FEW_WAVES - 1) / FEW_WAVES;
+    const int first = wave * each, last = min(steps, first + each);
+    const T *x[MT], *w[F];
+#pragma unroll
+    for (int m = 0; m < MT; ++m) x[m] = (const T *)pr.a[0] + min((int64_t)m * 16 + r, pr.M - 1) * pr.sa + q * 8;
+#pragma unroll
+    for (int f = 0; f < F; ++f)
+        w[f] = (const T *)pr.b[f / NB] + min(n0 + f % NB * 16 + r, pr.N - 1) * (f < NB ? pr.sb : pr.sb2) + q * 8;
+    f32x4 acc[MT][F] = {};
+    frag<T> fw[2][FEW_STEPS][F], fx[2][FEW_STEPS][MT];
+    auto load = [&](int at, int s) {  // steps from s on, past the share's end as zeros
+#pragma unroll
+        for (int i = 0; i < FEW_STEPS; ++i) {
+            const int k = (s + i) * 32, left = s + i < last ? K - k - q * 8 : 0;
+#pragma unroll
+            for (int f = 0; f < F; ++f) fw[at][i][f] = load_frag(w[f] + k, left);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) fx[at][i][m] = load_frag(x[m] + k, left);
+        }
+    };
+    auto multiply = [&](int at) {
+#pragma unroll
+        for (int i = 0; i < FEW_STEPS; ++i)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int f = 0; f < F; ++f) acc[m][f] = mma(fw[at][i][f], fx[at][i][m], acc[m][f]);
+    };
+    load(0, first);
+    for (int s = first; s < last; s += 2 * FEW_STEPS) {
+        load(1, s + FEW_STEPS);
+        multiply(0);
+        load(0, s + 2 * FEW_STEPS);
+        multiply(1);
+    }
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int f = 0; f < F; ++f) part[wave][m][f][lane] = acc[m][f];
+    __syncthreads();
+    if (wave >= MT || q >= 2 * NB) return;
+    // Column n of 16 of a fragment lies in lane n / 4 * 16 + row, element n % 4; this lane takes columns 8 q .. 8 q + 7.
+    float v[2][8];
+#pragma unroll
+    for (int which = 0; which < 2; ++which)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            f32x4 sum = {};
+#pragma unroll
+            for (int from = 0; from < FEW_WAVES; ++from) sum += part[from][wave][which * NB + q / 2][(q % 2 * 2 + h) * 16 + r];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[which][h * 4 + e] = sum[e];
+        }
+    epi(0, wave * 16 + r, n0 + q * 8, v[0], v[1]);
+}
+
+constexpr int FEW_ROWS = 64;
+
+// Whether the few-rows form is expected to beat tiles that take `tiles_us`.  Weights come at the rate of a large read, and
+// with the rows that every workgroup reads again (from L2) at 7.3 TB/s in all, after 3 us of start and end.  At 1024 x 4096, 1
+// and 64 rows take 6.2 and 10.5 us (tiles: 9.7, 10.9); at 4096 x 11264, 33 and 75 (tiles: 41, 43).  What is kept
+// has no say: h, and g and u made again, are the same bits in every form.
+bool few_rows_win(int64_t M, int64_t N, int64_t K, double tiles_us)
+{
+    if (M > FEW_ROWS) return false;
+    const double weights = 4.0 * N * K, again = (double)((N + 15) / 16) * M * K * 2.0;
+    return 3.0 + std::max(weights / 5.5e6, (weights + again) / 7.3e6) < tiles_us;
+}
+
+template <class T, int NB, class EPI>
+int launch_few(const product &pr, const EPI &epi, hipStream_t st)
+{
+    const dim3 grid((uint32_t)((pr.N + 16 * NB - 1) / (16 * NB))), block(FEW_WAVES * WAVE);
+    if (pr.M <= 16)
+        hipLaunchKernelGGL((k_few<T, EPI, 1, NB>), grid, block, 0, st, pr, epi);
+    else if (pr.M <= 32)
+        hipLaunchKernelGGL((k_few<T, EPI, 2, NB>), grid, block, 0, st, pr, epi);
+    else
+        hipLaunchKernelGGL((k_few<T, EPI, 4, NB>), grid, block, 0, st, pr, epi);
+    return launched();
+}
+
+// g and u of a block, by tiles or by the few-rows form (which takes operands of any alignment).  WHOLE: the epilogue needs units
+// of 32 columns (checkpoint groups).
+template <class T, bool WHOLE, class EPI>
+int run_sums(const product &pr, bool few, const cut &c, const EPI &epi, hipStream_t st)
+{
+    return few ? launch_few<T, WHOLE ? 2 : 1>(pr, epi, st) : run_product<T, true, true, 1>(pr, c, epi, st);
 }
 
 // ------------------------------------------------------------------ operands
@@ -311,7 +534,8 @@ using namespace rkb;
 extern "C" int rkb_weight_grad_workspace(int dtype, int64_t rows, int64_t n, int64_t k, int ckpt, int aligned, size_t *bytes)
 {
     if (!bytes || !good_dtype16(dtype) || !good_size(rows, n) || !good_size(rows, k)) return RKB_E_INVAL;
-    *bytes = (ckpt || k % 8 || !aligned ? padded_bytes(rows, k) : 0) + (n % 8 || !aligned ? padded_bytes(rows, n) : 0);
+    *bytes = (ckpt || k % 8 || !aligned ? padded_bytes(rows, k) : 0) + (n % 8 || !aligned ? padded_bytes(rows, n) : 0) +
+             split_bytes(choose_cut(n, k, rows, 1, 1, 1, false), n, k, 1);
     return RKB_OK;
 }
 
@@ -335,6 +559,8 @@ extern "C" int rkb_weight_grad(int dtype, int64_t rows, int64_t n, int64_t k, co
         ws.align(b);
     }
     ws.align(a);
+    const cut c = choose_cut(n, k, rows, 1, 1, 1, false);
+    void *parts = ws.take(split_bytes(c, n, k, 1));
     if (ws.at != workspace && !good_workspace(workspace)) return RKB_E_INVAL;
     if (!ws.fits()) return RKB_E_NOMEM;
     int rc = ws.run(st);
@@ -342,8 +568,8 @@ extern "C" int rkb_weight_grad(int dtype, int64_t rows, int64_t n, int64_t k, co
     if (rc != RKB_OK) return rc;
     return with_type16(dtype, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        const product pr{{(const char *)a.p, nullptr}, {(const char *)b.p, nullptr}, a.stride, b.stride, round_up(n, 8), round_up(k, 8), rows, 1, 1};
-        return run_product<T, false, false>(pr, epi_store<T>{{{(T *)dw, dw_stride, n, k}}}, st);
+        const product pr{{(const char *)a.p, nullptr}, {(const char *)b.p, nullptr}, a.stride, b.stride, b.stride, round_up(n, 8), round_up(k, 8), rows, 1};
+        return store_product<T, false, false, 1>(pr, c, parts, epi_store<T>{{{(T *)dw, dw_stride, n, k}}}, st);
     });
 }
 
@@ -363,6 +589,11 @@ static bool good_kept(int keep, int64_t rows, const void *g, const void *u, cons
     if (keep != RKB_KEEP_8BIT) return !ge && !ue && (uintptr_t)g % size == 0 && (uintptr_t)u % size == 0;
     return ge && ue && (uintptr_t)g % 16 == 0 && (uintptr_t)u % 16 == 0;
 }
+
+// The three products of a gated block: g and u, dx, and dwg and dwu.
+static cut sums_cut(int64_t rows, int64_t d, int64_t f) { return choose_cut(rows, f, d, 1, 1, 2, true); }
+static cut dx_cut(int64_t rows, int64_t d, int64_t f) { return choose_cut(rows, d, f, 2, 1, 1, true); }
+static cut dw_cut(int64_t rows, int64_t d, int64_t f) { return choose_cut(f, d, rows, 1, 2, 1, false); }
 
 extern "C" int rkb_gated_fwd_workspace(int dtype, int64_t rows, int64_t d, int64_t f, int aligned, size_t *bytes)
 {
@@ -387,7 +618,7 @@ struct gated_operands {
     }
     product sums(int64_t rows, int64_t d, int64_t f) const  // g and u
     {
-        return product{{(const char *)x.p, nullptr}, {(const char *)wg.p, (const char *)wu.p}, x.stride, wg.stride, rows, f, round_up(d, 8), 1, 1};
+        return product{{(const char *)x.p, nullptr}, {(const char *)wg.p, (const char *)wu.p}, x.stride, wg.stride, wu.stride, rows, f, d, 1};
     }
 };
 
@@ -404,7 +635,9 @@ extern "C" int rkb_gated_fwd(int dtype, int act, int keep, int64_t rows, int64_t
     const hipStream_t st = (hipStream_t)stream;
     workspace_taker ws(workspace, ws_bytes);
     gated_operands in{{x, x_stride, rows, d}, {wg, wg_stride, f, d}, {wu, wu_stride, f, d}};
-    in.align(ws);
+    const cut c = sums_cut(rows, d, f);
+    const bool few = few_rows_win(rows, f, d, c.us);
+    if (!few) in.align(ws);
     if (ws.at != workspace && !good_workspace(workspace)) return RKB_E_INVAL;
     if (!ws.fits()) return RKB_E_NOMEM;
     const int rc = ws.run(st);
@@ -414,7 +647,7 @@ extern "C" int rkb_gated_fwd(int dtype, int act, int keep, int64_t rows, int64_t
         return with_act(act, [&](auto a) {
             auto go = [&](auto kind) {
                 const epi_gated_fwd<T, a(), kind()> epi{{(T *)h, h_stride, rows, f}, g, u, ge, ue};
-                return run_product<T, true, true>(in.sums(rows, d, f), epi, st);
+                return run_sums<T, kind() == RKB_KEEP_8BIT>(in.sums(rows, d, f), few, c, epi, st);
             };
             if (keep == RKB_KEEP_NONE) return go(std::integral_constant<int, RKB_KEEP_NONE>());
             return with_kept(keep, go);
@@ -425,7 +658,8 @@ extern "C" int rkb_gated_fwd(int dtype, int act, int keep, int64_t rows, int64_t
 extern "C" int rkb_gated_bwd_workspace(int dtype, int keep, int64_t rows, int64_t d, int64_t f, int aligned, size_t *bytes)
 {
     if (!bytes || !good_gated(dtype, RKB_SILU, keep, rows, d, f)) return RKB_E_INVAL;
-    *bytes = 2 * padded_bytes(rows, f) + (d % 8 || !aligned ? padded_bytes(rows, d) + 2 * padded_bytes(f, d) : 0);
+    *bytes = 2 * padded_bytes(rows, f) + (d % 8 || !aligned ? padded_bytes(rows, d) + 2 * padded_bytes(f, d) : 0) +
+             std::max(split_bytes(dx_cut(rows, d, f), rows, d, 1), split_bytes(dw_cut(rows, d, f), f, d, 2));
     return RKB_OK;
 }
 
@@ -447,6 +681,8 @@ extern "C" int rkb_gated_bwd(int dtype, int act, int keep, int64_t rows, int64_t
     void *dg = ws.take(padded_bytes(rows, f)), *du = ws.take(padded_bytes(rows, f));
     gated_operands in{{x, x_stride, rows, d}, {wg, wg_stride, f, d}, {wu, wu_stride, f, d}};
     if (rows > 0) in.align(ws);
+    const cut cx = dx_cut(rows, d, f), cw = dw_cut(rows, d, f);
+    void *parts = ws.take(std::max(split_bytes(cx, rows, d, 1), split_bytes(cw, f, d, 2)));
     if (ws.at != workspace && !good_workspace(workspace)) return RKB_E_INVAL;
     if (!ws.fits()) return RKB_E_NOMEM;
     int rc = ws.run(st);
@@ -456,8 +692,11 @@ extern "C" int rkb_gated_bwd(int dtype, int act, int keep, int64_t rows, int64_t
         const out_matrix<T> og{(T *)dg, ld, rows, f}, ou{(T *)du, ld, rows, f}, oh{(T *)h, h_stride, rows, f};
         if (rows > 0)
             rc = with_act(act, [&](auto a) {
-                if (keep == RKB_KEEP_NONE)
-                    return run_product<T, true, true>(in.sums(rows, d, f), epi_gated_bwd<T, a()>{(const T *)dh, dh_stride, og, ou, oh}, st);
+                if (keep == RKB_KEEP_NONE) {
+                    const epi_gated_bwd<T, a()> epi{(const T *)dh, dh_stride, og, ou, oh};
+                    const cut c = sums_cut(rows, d, f);
+                    return run_sums<T, false>(in.sums(rows, d, f), few_rows_win(rows, f, d, c.us), c, epi, st);
+                }
                 const dim3 grid((uint32_t)((f + 2047) / 2048), (uint32_t)std::min<int64_t>(rows, 32768));
                 auto go = [&](auto kind) {
                     hipLaunchKernelGGL((k_gated_grads<T, a(), kind()>), grid, dim3(256), 0, st, (const T *)dh, dh_stride, g, u,
@@ -467,12 +706,12 @@ extern "C" int rkb_gated_bwd(int dtype, int act, int keep, int64_t rows, int64_t
                 return with_kept(keep, go);
             });
         if (rc == RKB_OK && dx && rows > 0) {
-            const product pr{{(const char *)dg, (const char *)du}, {(const char *)in.wg.p, (const char *)in.wu.p}, ld, in.wg.stride, rows, round_up(d, 8), f, 2, 1};
-            rc = run_product<T, true, false>(pr, epi_store<T>{{{(T *)dx, dx_stride, rows, d}}}, st);
+            const product pr{{(const char *)dg, (const char *)du}, {(const char *)in.wg.p, (const char *)in.wu.p}, ld, in.wg.stride, in.wg.stride, rows, round_up(d, 8), f, 1};
+            rc = store_product<T, true, false, 2>(pr, cx, parts, epi_store<T>{{{(T *)dx, dx_stride, rows, d}}}, st);
         }
         if (rc == RKB_OK && dwg) {
-            const product pr{{(const char *)dg, (const char *)du}, {(const char *)in.x.p, nullptr}, ld, in.x.stride, ld, round_up(d, 8), rows, 1, 2};
-            rc = run_product<T, false, false>(pr, epi_store<T>{{{(T *)dwg, dw_stride, f, d}, {(T *)dwu, dw_stride, f, d}}}, st);
+            const product pr{{(const char *)dg, (const char *)du}, {(const char *)in.x.p, nullptr}, ld, in.x.stride, in.x.stride, ld, round_up(d, 8), rows, 2};
+            rc = store_product<T, false, false, 1>(pr, cw, parts, epi_store<T>{{{(T *)dwg, dw_stride, f, d}, {(T *)dwu, dw_stride, f, d}}}, st);
         }
         return rc;
     });

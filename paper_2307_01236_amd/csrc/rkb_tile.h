@@ -54,7 +54,7 @@ __device__ inline void copy_piece(const void *from, lds_byte *to)
 template <class T, int ROWS, int WAVES, bool NEAR, bool PAIR>
 struct stager {
     static constexpr int PIECES = ROWS * DEPTH * 2 / PIECE, MINE = PIECES / WAVES;
-    static constexpr int BYTES = NEAR ? PIECES * PIECE : PIECES * PIECE_APART;
+    static constexpr int APART = NEAR ? PIECE : PIECE_APART, BYTES = PIECES * APART;
     static_assert(PIECES % WAVES == 0 && sizeof(T) == 2 && (NEAR || !PAIR));
 
     uint32_t off[MINE];  // this lane's bytes from the stage's start, by piece
@@ -69,6 +69,14 @@ struct stager {
     {
         const int row = piece * 8 + lane / 8;
         return lane % 8 ^ (row / 2 & 7);
+    }
+
+    static __device__ bool exists(int piece, int lane, int left)  // whether this lane's k does
+    {
+        if constexpr (NEAR)
+            return chunk_of(piece, lane) * 8 < left;
+        else
+            return k_of(piece, lane) < left;
     }
 
     // r0: the tile's first row, rows: those that exist (the last one stands in for the others: what it gives there is
@@ -89,19 +97,18 @@ struct stager {
         }
     }
 
-    // base(piece): the address of the stage's start (uniform).  left: k that exist from there on.
-    template <class B>
-    __device__ void copy(int wave, int lane, B base, int64_t left, lds_byte *to) const
+    // base(piece): the address of the stage's start (uniform).  FULL: all its k exist; else `left` of them do.
+    template <bool FULL, class B>
+    __device__ void copy(int wave, int lane, B base, int left, lds_byte *to) const
     {
 #pragma unroll
         for (int i = 0; i < MINE; ++i) {
             const int piece = wave * MINE + i;
-            const char *from = base(piece) + off[i];
-            if (left < DEPTH) {
-                const bool in = NEAR ? chunk_of(piece, lane) * 8 < left : k_of(piece, lane) < left;
-                from = in ? from : (const char *)&zero_chunk;
-            }
-            copy_piece(from, to + piece * (NEAR ? PIECE : PIECE_APART));
+            uint32_t o = off[i];
+            asm volatile("" : "+v"(o));  // stays 32 bits wide: the copy adds it to a scalar address
+            const char *from = base(piece) + o;
+            if (!FULL && !exists(piece, lane, left)) from = (const char *)&zero_chunk;
+            copy_piece(from, to + piece * APART);
         }
     }
 
@@ -135,14 +142,13 @@ struct stager {
     }
 };
 
-// One launch: `problems` products of the same sizes, each a sum over `parts` operand pairs (one of the
-// two is 1), or two products with one A side by side (an epilogue of two sums).  The operands of one kind
-// share their stride.
+// One launch: `problems` products a[i] b[0] of the same sizes, or the sum a[0] b[0] + a[1] b[1] (PARTS = 2), or a[0] b[0] and
+// a[0] b[1] side by side (an epilogue of two sums).  The operands of one kind share their stride.
 struct product {
     const char *a[2], *b[2];
-    int64_t sa, sb;
+    int64_t sa, sb, sb2;  // sb2: of b[1], where it differs (few rows only)
     int64_t M, N, K;
-    int parts, problems;
+    int problems;
     int tiles_m, tiles_n;
     int splits, split_stages;  // stages (of all parts) that one workgroup takes
 };
@@ -170,7 +176,7 @@ __device__ inline tile_at find_tile(const product &pr)
     return t;
 }
 
-template <class T, class EPI, int TM, int TN, int WM, int WN, bool ANEAR, bool BNEAR>
+template <class T, class EPI, int TM, int TN, int WM, int WN, bool ANEAR, bool BNEAR, int PARTS>
 __global__ __launch_bounds__(WM *WN *WAVE) void k_product(product pr, EPI epi)
 {
     constexpr int WAVES = WM * WN, SUMS = EPI::SUMS;
@@ -185,7 +191,7 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(product pr, EPI epi)
     const tile_at t = find_tile(pr);
     const int64_t m0 = (int64_t)t.m * TM, n0 = (int64_t)t.n * (TN / SUMS);
     const int stages_k = (int)((pr.K + DEPTH - 1) / DEPTH);
-    const int first = t.split * pr.split_stages, last = min(stages_k * pr.parts, first + pr.split_stages);
+    const int first = t.split * pr.split_stages, last = min(stages_k * PARTS, first + pr.split_stages);
 
     SA sa;
     SB sb;
@@ -194,15 +200,19 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(product pr, EPI epi)
     const int64_t a_row0 = (ANEAR ? m0 * pr.sa : m0) * 2, b_row0 = (BNEAR ? n0 * pr.sb : n0) * 2;
     const int64_t a_step = ANEAR ? 2 : pr.sa * 2, b_step = BNEAR ? 2 : pr.sb * 2;
 
-    auto copy = [&](int s, lds_byte *a, lds_byte *b) {
-        const int part = s >= stages_k, which = part | t.problem;
-        const int64_t k0 = (int64_t)(s - part * stages_k) * DEPTH;
-        const char *pa = pr.a[which] + a_row0 + k0 * a_step;
-        sa.copy(wave, lane, [&](int) { return pa; }, pr.K - k0, a);
-        sb.copy(wave, lane, [&](int piece) {
-            return pr.b[SUMS == 2 ? piece / 4 & 1 : part] + b_row0 + k0 * b_step;
-        }, pr.K - k0, b);
+    // the operands of this workgroup's tile: of the first or only part, and of the second
+    const char *pa0 = pr.a[t.problem] + a_row0, *pa1 = pr.a[1] + a_row0;
+    const char *pb0 = pr.b[0] + b_row0, *pb1 = pr.b[1] + b_row0;
+    auto copy = [&](auto full, int s, lds_byte *a, lds_byte *b) {
+        const bool second = PARTS == 2 && s >= stages_k;
+        const int k0 = (s - (second ? stages_k : 0)) * DEPTH, left = (int)pr.K - k0;
+        const char *pa = (second ? pa1 : pa0) + k0 * a_step, *pb = (second ? pb1 : pb0) + k0 * b_step;
+        const char *pu = pb1 + k0 * b_step;
+        sa.template copy<full()>(wave, lane, [&](int) { return pa; }, left, a);
+        sb.template copy<full()>(wave, lane, [&](int piece) { return SUMS == 2 && piece / 4 % 2 ? pu : pb; }, left, b);
     };
+    constexpr std::true_type full{};
+    constexpr std::false_type any{};
     const int a_at[2] = {SA::place(wm * FM * 16, lane, 0), SA::place(wm * FM * 16, lane, 1)};
     const int b_at[2] = {SB::place(wn * FN * 16, lane, 0), SB::place(wn * FN * 16, lane, 1)};
 
@@ -220,30 +230,68 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(product pr, EPI epi)
 #pragma unroll
             for (int j = 0; j < FN; ++j) acc[i][j] = mma(fb[half][j], fa[half][i], acc[i][j]);
     };
+    // The reads of the next fragments, and `copies` of a later stage, are spread over the products of the
+    // present fragments: first B's, of which all are needed at once, then A's, each when about as
+    // many of the present ones have been used up, so that few registers hold both.
+    auto mix = [&](auto copies) {
+        constexpr int RA = ANEAR ? 1 : 2, RB = BNEAR ? 1 : 2, EACH = (FM * FN - 2 * FN) / FM;
+#pragma unroll
+        for (int i = 0; i < FN; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);   // matrix instructions
+            __builtin_amdgcn_sched_group_barrier(0x100, RB, 0);  // LDS reads
+            if (i < copies()) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < FM; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, RA, 0);
+            if (FN + i < copies()) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, FM * FN - FN - FM * EACH, 0);
+    };
     // Stage s from one buffer while the next lies in, or is on its way to, the other.  All waves have read the
     // present buffer when they pass the barrier, and all copies of the next stage have landed; so the
     // stage after it may be copied over the present one while its second half is multiplied.
-    auto stage = [&](int s, lds_byte *a, lds_byte *b, lds_byte *a_next, lds_byte *b_next) {
+    // AHEAD: that stage exists and is full.
+    auto stage = [&](auto ahead, int s, lds_byte *a, lds_byte *b, lds_byte *a_next, lds_byte *b_next) {
         fetch(1, a, b);
         multiply(0);
+        mix(std::integral_constant<int, 0>());
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_waitcnt(WAIT_ALL);
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
-        if (s + 2 < last) copy(s + 2, a, b);
-        if (s + 1 < last) fetch(0, a_next, b_next);
-        multiply(1);
+        if constexpr (ahead()) {
+            copy(full, s + 2, a, b);
+            fetch(0, a_next, b_next);
+            multiply(1);
+            mix(std::integral_constant<int, SA::MINE + SB::MINE>());
+            __builtin_amdgcn_sched_barrier(0);
+        } else {
+            if (s + 2 < last) copy(any, s + 2, a, b);
+            fetch(0, a_next, b_next);  // past the last stage: whatever lies there, not used
+            multiply(1);
+            mix(std::integral_constant<int, 0>());
+        }
     };
     lds_byte *la0 = (lds_byte *)a0, *la1 = (lds_byte *)a1, *lb0 = (lds_byte *)b0, *lb1 = (lds_byte *)b1;
     if (first < last) {
-        copy(first, la0, lb0);
-        if (first + 1 < last) copy(first + 1, la1, lb1);
+        if (first + 1 < last) copy(any, first + 1, la1, lb1);
+        copy(any, first, la0, lb0);
         __builtin_amdgcn_s_waitcnt(WAIT_ALL);
         __builtin_amdgcn_s_barrier();
         fetch(0, la0, lb0);
-        for (int s = first; s < last; s += 2) {
-            stage(s, la0, lb0, la1, lb1);
-            if (s + 1 < last) stage(s + 1, la1, lb1, la0, lb0);
+        const bool ragged = pr.K % DEPTH != 0;
+        for (int s = first; s < last;) {
+            // the next stage that is not full, or the end
+            const int stop = !ragged ? last : min(last, (PARTS == 2 && s + 2 >= stages_k ? 2 * stages_k : stages_k) - 1);
+            for (; s + 3 < stop; s += 2) {
+                stage(full, s, la0, lb0, la1, lb1);
+                stage(full, s + 1, la1, lb1, la0, lb0);
+            }
+            stage(any, s, la0, lb0, la1, lb1);
+            if (s + 1 < last) stage(any, s + 1, la1, lb1, la0, lb0);
+            s += 2;
         }
     }
 
