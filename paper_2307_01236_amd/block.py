@@ -16,6 +16,7 @@ as for torch's own operators.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import torch
@@ -131,10 +132,10 @@ def _matrix(t, where: str, dtype=None, device=None, rows=None, cols=None):
     return t.data_ptr(), n_rows, n_cols, stride if n_rows > 1 else n_cols
 
 
-def _vector(t, n: int, where: str, device, dtypes):
+def _vector(t, n: int, where: str, device, dtype):
     if t is None:
         return None
-    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype not in dtypes:
+    if not isinstance(t, torch.Tensor) or t.device != device or t.dtype != dtype:
         _refuse(where, "types or devices differ")
     if t.numel() != n or not t.is_contiguous():
         _refuse(where, "sizes do not match")
@@ -163,29 +164,44 @@ def _dtype(t, where: str, allowed=_DTYPE):
 _HALF = (torch.float16, torch.bfloat16)
 
 
-class _on:
-    """The tensors' device as the current one, and its current stream."""
-
-    __slots__ = ("index", "before")
-
-    def __init__(self, device):
-        self.index = device.index
-
-    def __enter__(self):
-        self.before = torch.cuda.current_device()
-        if self.before != self.index:
-            torch.cuda.set_device(self.index)
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.before != self.index:
-            torch.cuda.set_device(self.before)
+# The current device and a device's current stream, without the objects that torch.cuda wraps
+# them in (2 us a call, on calls that take 4).
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else lambda: -1
 
 
-def _workspace(query, device, where: str, *args):
+def _stream(device) -> int:
+    return torch._C._cuda_getCurrentRawStream(device.index)
+
+
+def _on_its_device(call):
+    """Runs a call with its first tensor's device as the current one."""
+
+    @functools.wraps(call)
+    def on_device(first, *args, **kw):
+        device = getattr(first, "device", None)
+        if device is None or device.type != "cuda" or device.index == _current_device():
+            return call(first, *args, **kw)
+        with torch.cuda.device(device):
+            return call(first, *args, **kw)
+
+    return on_device
+
+
+@functools.lru_cache(maxsize=4096)
+def _workspace_bytes(name: str, *sizes) -> int:
+    """What rkb_<name>_workspace reports, by its arguments."""
     n = C.c_size_t(0)
-    _check(query(*args, C.byref(n)), where)
-    return torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None
+    _check(getattr(load(), name + "_workspace")(*sizes, C.byref(n)), name)
+    return n.value
+
+
+def _workspace(device, name: str, *sizes):
+    """(workspace, pointer, bytes)"""
+    n = _workspace_bytes(name, *sizes)
+    if not n:
+        return None, None, 0
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    return ws, ws.data_ptr(), n
 
 
 def _aligned(p: int, stride: int) -> bool:
@@ -198,54 +214,56 @@ def _plain(mats) -> bool:
     return _aligned(xp, xs) and _aligned(wgp, wgs) and _aligned(wup, wus) and wgs == wus
 
 
-def _space(ws):
-    return (ws.data_ptr(), ws.numel()) if ws is not None else (None, 0)
-
-
 def _weight_type(w, b, x, where: str):
-    """The type of a layer norm's weight and bias: x's, or 32-bit."""
-    have = [t.dtype for t in (w, b) if t is not None]
-    if any(t != have[0] for t in have) or (have and have[0] not in (x.dtype, torch.float32)):
+    """The type of a layer norm's weight and bias: x's, or 32-bit (the one's is checked against the other's later)."""
+    t = w if w is not None else b
+    if t is None:
+        return x.dtype
+    if t.dtype != x.dtype and t.dtype != torch.float32:
         _refuse(where, "types or devices differ")
-    return have[0] if have else x.dtype
+    return t.dtype
 
 
+@_on_its_device
 def rkb_layer_norm_fwd(x, weight=None, bias=None, eps: float = 1e-5):
     """(y, mean, rstd): layer norm over the last dimension, and each row's mean and 1 / sqrt(variance + eps)."""
     where = "rkb_layer_norm_fwd"
-    lib, dt = load(), _dtype(x, where)
+    dt = _dtype(x, where)
     p, rows, cols, stride = _matrix(x, where)
+    device = x.device
     wt = _weight_type(weight, bias, x, where)
-    w, b = (_vector(t, cols, where, x.device, (wt,)) for t in (weight, bias))
-    with _on(x.device) as stream:
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
-        rstd = torch.empty_like(mean)
-        _check(lib.rkb_layer_norm_fwd(dt, _DTYPE[wt], rows, cols, p, stride, w, b, eps, y.data_ptr(), cols,
-                                      mean.data_ptr(), rstd.data_ptr(), stream), where)
+    w, b = _vector(weight, cols, where, device, wt), _vector(bias, cols, where, device, wt)
+    y = torch.empty_like(x, memory_format=torch.contiguous_format)
+    mean = x.new_empty(x.shape[:-1], dtype=torch.float32)
+    rstd = torch.empty_like(mean)
+    _check(load().rkb_layer_norm_fwd(dt, _DTYPE[wt], rows, cols, p, stride, w, b, eps, y.data_ptr(), cols, mean.data_ptr(),
+                                     rstd.data_ptr(), _stream(device)), where)
     return y, mean, rstd
 
 
+@_on_its_device
 def rkb_layer_norm_bwd(dy, x, mean, rstd, weight=None, bias: bool = False):
     """(dx, dweight, dbias) from dy and what the forward kept: x itself or its Ckpt8, and mean and rstd.
     dweight is None without a weight, dbias unless bias is asked for (it has weight's type, or dy's)."""
     where = "rkb_layer_norm_bwd"
-    lib, dt = load(), _dtype(dy, where)
+    dt = _dtype(dy, where)
     p, rows, cols, stride = _matrix(dy, where)
+    device = dy.device
     wt = _weight_type(weight, None, dy, where)
-    w = _vector(weight, cols, where, dy.device, (wt,))
-    m, r = (_vector(t, rows, where, dy.device, (torch.float32,)) for t in (mean, rstd))
-    xp, xs, codes, exps = _kept(x, where, dy.dtype, dy.device, rows, cols)
-    with _on(dy.device) as stream:
-        dx = torch.empty(dy.shape, dtype=dy.dtype, device=dy.device)
-        dw = torch.empty(cols, dtype=wt, device=dy.device) if weight is not None else None
-        db = torch.empty(cols, dtype=wt, device=dy.device) if bias else None
-        ws = None
-        if dw is not None or db is not None:
-            ws = _workspace(lib.rkb_layer_norm_bwd_workspace, dy.device, where, dt, rows, cols)
-        _check(lib.rkb_layer_norm_bwd(dt, _DTYPE[wt], rows, cols, p, stride, xp, xs, codes, exps, m, r, w, dx.data_ptr(),
-                                      cols, dw.data_ptr() if dw is not None else None,
-                                      db.data_ptr() if db is not None else None, *_space(ws), stream), where)
+    w = _vector(weight, cols, where, device, wt)
+    m, r = _vector(mean, rows, where, device, torch.float32), _vector(rstd, rows, where, device, torch.float32)
+    if m is None or r is None:
+        _refuse(where, "no mean or rstd")
+    xp, xs, codes, exps = _kept(x, where, dy.dtype, device, rows, cols)
+    dx = torch.empty_like(dy, memory_format=torch.contiguous_format)
+    dw = torch.empty_like(weight) if weight is not None else None
+    db = dy.new_empty(cols, dtype=wt) if bias else None
+    ws, ws_p, ws_n = None, None, 0
+    if dw is not None or db is not None:
+        ws, ws_p, ws_n = _workspace(device, where, dt, rows, cols)
+    _check(load().rkb_layer_norm_bwd(dt, _DTYPE[wt], rows, cols, p, stride, xp, xs, codes, exps, m, r, w, dx.data_ptr(), cols,
+                                     dw.data_ptr() if dw is not None else None, db.data_ptr() if bias else None, ws_p, ws_n,
+                                     _stream(device)), where)
     return dx, dw, db
 
 
@@ -257,53 +275,52 @@ def _kept(x, where: str, dtype, device, rows: int, cols: int):
     return p, stride, None, None
 
 
+def _new_ckpt(like, rows: int, cols: int):
+    groups = -(-cols // RKB_GROUP)
+    return like.new_empty((rows, groups * RKB_GROUP), dtype=torch.int8), like.new_empty((rows, groups), dtype=torch.uint8)
+
+
+@_on_its_device
 def rkb_ckpt8_save(x) -> Ckpt8:
     """The 8-bit checkpoint of x, in groups of 32 neighbours of the last dimension."""
     where = "rkb_ckpt8_save"
-    lib, dt = load(), _dtype(x, where)
+    dt = _dtype(x, where)
     p, rows, cols, stride = _matrix(x, where)
-    with _on(x.device) as stream:
-        codes, exps = _new_ckpt(rows, cols, x.device)
-        _check(lib.rkb_ckpt8_save(dt, rows, cols, p, stride, codes.data_ptr(), exps.data_ptr(), stream), where)
+    codes, exps = _new_ckpt(x, rows, cols)
+    _check(load().rkb_ckpt8_save(dt, rows, cols, p, stride, codes.data_ptr(), exps.data_ptr(), _stream(x.device)), where)
     return Ckpt8(codes, exps, x.shape, x.dtype)
 
 
-def _new_ckpt(rows: int, cols: int, device):
-    groups = -(-cols // RKB_GROUP)
-    return (torch.empty(rows, groups * RKB_GROUP, dtype=torch.int8, device=device),
-            torch.empty(rows, groups, dtype=torch.uint8, device=device))
-
-
+@_on_its_device
 def rkb_ckpt8_load(c: Ckpt8) -> torch.Tensor:
     """The tensor that a checkpoint stands for, of the shape and type it was made from."""
     where = "rkb_ckpt8_load"
     if not isinstance(c, Ckpt8) or not c.codes.is_cuda or c.dtype not in _DTYPE or not c.shape:
         _refuse(where, "not a checkpoint on the GPU")
-    lib, cols = load(), c.shape[-1]
+    device, cols = c.codes.device, c.shape[-1]
     rows = c.shape.numel() // cols if cols else 0
-    codes, exps = _ckpt(c, where, c.dtype, c.codes.device, rows, cols)
-    with _on(c.codes.device) as stream:
-        x = torch.empty(c.shape, dtype=c.dtype, device=c.codes.device)
-        _check(lib.rkb_ckpt8_load(_DTYPE[c.dtype], rows, cols, codes, exps, x.data_ptr(), cols, stream), where)
+    codes, exps = _ckpt(c, where, c.dtype, device, rows, cols)
+    x = c.codes.new_empty(c.shape, dtype=c.dtype)
+    _check(load().rkb_ckpt8_load(_DTYPE[c.dtype], rows, cols, codes, exps, x.data_ptr(), cols, _stream(device)), where)
     return x
 
 
+@_on_its_device
 def rkb_weight_grad(dy, x) -> torch.Tensor:
     """dy^T x [n, k], the weight gradient of a linear layer y = x W^T, from dy [..., n] and its input x
     [..., k], kept as it was or as a Ckpt8."""
     where = "rkb_weight_grad"
-    lib, dt = load(), _dtype(dy, where, _HALF)
+    dt = _dtype(dy, where, _HALF)
     p, rows, n, stride = _matrix(dy, where)
     if not isinstance(x, (Ckpt8, torch.Tensor)) or not len(x.shape):
         _refuse(where, "not a tensor of the GPU")
-    k = x.shape[-1]
-    xp, xs, codes, exps = _kept(x, where, dy.dtype, dy.device, rows, k)
-    with _on(dy.device) as stream:
-        dw = torch.empty(n, k, dtype=dy.dtype, device=dy.device)
-        aligned = _aligned(p, stride) and (codes is not None or _aligned(xp, xs))
-        ws = _workspace(lib.rkb_weight_grad_workspace, dy.device, where, dt, rows, n, k, codes is not None, aligned)
-        _check(lib.rkb_weight_grad(dt, rows, n, k, p, stride, xp, xs, codes, exps, dw.data_ptr(), k, *_space(ws), stream),
-               where)
+    device, k = dy.device, x.shape[-1]
+    xp, xs, codes, exps = _kept(x, where, dy.dtype, device, rows, k)
+    dw = dy.new_empty((n, k))
+    aligned = _aligned(p, stride) and (codes is not None or _aligned(xp, xs))
+    ws, ws_p, ws_n = _workspace(device, where, dt, rows, n, k, codes is not None, aligned)
+    _check(load().rkb_weight_grad(dt, rows, n, k, p, stride, xp, xs, codes, exps, dw.data_ptr(), k, ws_p, ws_n,
+                                  _stream(device)), where)
     return dw
 
 
@@ -317,40 +334,41 @@ def _gated_args(x, wg, wu, act, where: str):
     return dt, rows, d, f, (xp, xs, wgp, wgs, wup, wus)
 
 
+@_on_its_device
 def rkb_gated_fwd(x, wg, wu, act: str = "silu", keep: str = "none"):
     """(h, kept): h = act(x wg^T) * (x wu^T) for x [..., d] and wg, wu [f, d]; act is silu or gelu.
-    kept is what rkb_gated_bwd takes: None for keep="none", (g, u) as 32-bit tensors for "full", of x's type for "16bit", as Ckpt8
-    for "8bit"."""
+    kept is what rkb_gated_bwd takes: None for keep="none", (g, u) as 32-bit tensors for "full", of x's
+    type for "16bit", as Ckpt8 for "8bit"."""
     where = "rkb_gated_fwd"
     if keep not in _KEEP:
         _refuse(where, "keep")
-    lib = load()
     dt, rows, d, f, mats = _gated_args(x, wg, wu, act, where)
-    with _on(x.device) as stream:
-        shape = x.shape[:-1] + (f,)
-        h = torch.empty(shape, dtype=x.dtype, device=x.device)
-        kept, ptrs = None, (None,) * 4
-        if keep in ("full", "16bit"):
-            kept = tuple(torch.empty_like(h, dtype=torch.float32 if keep == "full" else x.dtype) for _ in range(2))
-            ptrs = (kept[0].data_ptr(), kept[1].data_ptr(), None, None)
-        elif keep == "8bit":
-            kept = tuple(Ckpt8(*_new_ckpt(rows, f, x.device), shape, torch.float32) for _ in range(2))
-            ptrs = tuple(c.codes.data_ptr() for c in kept) + tuple(c.exps.data_ptr() for c in kept)
-        ws = _workspace(lib.rkb_gated_fwd_workspace, x.device, where, dt, rows, d, f, _plain(mats))
-        _check(lib.rkb_gated_fwd(dt, _ACT[act], _KEEP[keep], rows, d, f, *mats, h.data_ptr(), f, *ptrs, *_space(ws),
-                                 stream), where)
+    shape = x.shape[:-1] + (f,)
+    h = x.new_empty(shape)
+    kept, ptrs = None, (None,) * 4
+    if keep in ("full", "16bit"):
+        kept = tuple(torch.empty_like(h, dtype=torch.float32 if keep == "full" else x.dtype) for _ in range(2))
+        ptrs = (kept[0].data_ptr(), kept[1].data_ptr(), None, None)
+    elif keep == "8bit":
+        kept = tuple(Ckpt8(*_new_ckpt(x, rows, f), shape, torch.float32) for _ in range(2))
+        ptrs = tuple(c.codes.data_ptr() for c in kept) + tuple(c.exps.data_ptr() for c in kept)
+    ws, ws_p, ws_n = _workspace(x.device, where, dt, rows, d, f, _plain(mats))
+    _check(load().rkb_gated_fwd(dt, _ACT[act], _KEEP[keep], rows, d, f, *mats, h.data_ptr(), f, *ptrs, ws_p, ws_n,
+                                _stream(x.device)), where)
     return h, kept
 
 
+@_on_its_device
 def rkb_gated_bwd(dh, x, wg, wu, act: str = "silu", kept=None, want_h: bool = False):
     """(dx, dwg, dwu, h) from dh and what rkb_gated_fwd kept; h (None unless want_h) is act(g) * u again, for the
     weight gradient of the layer that follows."""
     where = "rkb_gated_bwd"
-    lib = load()
     dt, rows, d, f, mats = _gated_args(x, wg, wu, act, where)
     dhp, _, _, dhs = _matrix(dh, where, x.dtype, x.device, rows, f)
     keep, ptrs = RKB_KEEP_NONE, (None,) * 4
     if kept is not None:
+        if not isinstance(kept, tuple) or len(kept) != 2:
+            _refuse(where, "kept")
         g, u = kept
         if isinstance(g, Ckpt8) and isinstance(u, Ckpt8):
             keep = RKB_KEEP_8BIT
@@ -363,12 +381,10 @@ def rkb_gated_bwd(dh, x, wg, wu, act: str = "silu", kept=None, want_h: bool = Fa
             if any(m[3] != f for m in mats_gu):
                 _refuse(where, "g and u are not contiguous")
             ptrs = (mats_gu[0][0], mats_gu[1][0], None, None)
-    with _on(x.device) as stream:
-        dx = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        dwg = torch.empty(f, d, dtype=x.dtype, device=x.device)
-        dwu = torch.empty_like(dwg)
-        h = torch.empty(dh.shape, dtype=x.dtype, device=x.device) if want_h else None
-        ws = _workspace(lib.rkb_gated_bwd_workspace, x.device, where, dt, keep, rows, d, f, _plain(mats))
-        _check(lib.rkb_gated_bwd(dt, _ACT[act], keep, rows, d, f, dhp, dhs, *mats, *ptrs, dx.data_ptr(), d, dwg.data_ptr(),
-                                 dwu.data_ptr(), d, h.data_ptr() if want_h else None, f, *_space(ws), stream), where)
+    dx = x.new_empty(x.shape)
+    dwg, dwu = x.new_empty((f, d)), x.new_empty((f, d))
+    h = x.new_empty(dh.shape) if want_h else None
+    ws, ws_p, ws_n = _workspace(x.device, where, dt, keep, rows, d, f, _plain(mats))
+    _check(load().rkb_gated_bwd(dt, _ACT[act], keep, rows, d, f, dhp, dhs, *mats, *ptrs, dx.data_ptr(), d, dwg.data_ptr(),
+                                dwu.data_ptr(), d, h.data_ptr() if want_h else None, f, ws_p, ws_n, _stream(x.device)), where)
     return dx, dwg, dwu, h

@@ -34,18 +34,25 @@ inline constexpr int CODE_TOP_EXP<f16> = 9;  // 64 * 2^10 = 65536
 // Chunk of a row, `left` of whose elements exist (any number; the others read as 0).  The
 // pointer has the alignment of T only: global loads take any address on gfx950.
 template <class T>
-__device__ inline void load_chunk(const T *p, int64_t left, float (&v)[CHUNK<T>])
+__device__ inline vec<T, CHUNK<T>> load_raw(const T *p, int64_t left)
 {
     constexpr int N = CHUNK<T>;
+    vec<T, N> t;
     if (left >= N) {
-        vec<T, N> t;
         __builtin_memcpy(&t, p, 16);
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = (float)t[i];
     } else {
 #pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = i < left ? (float)p[i] : 0.0f;
+        for (int i = 0; i < N; ++i) t[i] = i < left ? p[i] : (T)0.0f;
     }
+    return t;
+}
+
+template <class T>
+__device__ inline void load_chunk(const T *p, int64_t left, float (&v)[CHUNK<T>])
+{
+    const auto t = load_raw<T>(p, left);
+#pragma unroll
+    for (int i = 0; i < CHUNK<T>; ++i) v[i] = (float)t[i];
 }
 
 // A 32-bit result before it is rounded to T.  The compiler may fold a product into its rounding to

@@ -15,25 +15,35 @@ namespace {
 
 constexpr int NORM_BLOCK = 256;
 
-// Sum over the lanes of one row, in every one of them.  Rows of more than a wave join their waves
-// through LDS (`part`: one float per wave, and a barrier before each reuse).
-template <int LANES>
-__device__ inline float row_sum(float v, float *part)
-{
-    if constexpr (LANES <= WAVE) {
-        return lane_sum<LANES>(v);
-    } else {
-        constexpr int WAVES = LANES / WAVE;
-        v = lane_sum<WAVE>(v);
-        __syncthreads();
-        if (threadIdx.x % WAVE == 0) part[threadIdx.x / WAVE] = v;
-        __syncthreads();
-        v = 0.0f;
+// Sums over the lanes of one row, in every one of them.  Rows of more than a wave join their waves
+// through LDS: successive calls use two places in turn, so that one barrier each is enough.
+template <int LANES, int BLOCK, int COUNT>
+struct row_sums {
+    static constexpr int WAVES = LANES > WAVE ? LANES / WAVE : 1, ROWS = LANES > WAVE ? BLOCK / LANES : 1;
+    using place = float[2][ROWS][COUNT][WAVES];
+    place &part;
+    int turn = 0;
+    __device__ row_sums(place &p) : part(p) {}
+    __device__ void operator()(float (&v)[COUNT])
+    {
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) v += part[w];
-        return v;
+        for (int c = 0; c < COUNT; ++c) v[c] = lane_sum<LANES < WAVE ? LANES : WAVE>(v[c]);
+        if constexpr (LANES > WAVE) {
+            const int row = threadIdx.x / LANES, wave = threadIdx.x % LANES / WAVE;
+            if (threadIdx.x % WAVE == 0)
+#pragma unroll
+                for (int c = 0; c < COUNT; ++c) part[turn][row][c][wave] = v[c];
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < COUNT; ++c) {
+                v[c] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < WAVES; ++w) v[c] += part[turn][row][c][w];
+            }
+            turn ^= 1;
+        }
     }
-}
+};
 
 template <class T, class W>
 __device__ inline void load_weight(const W *w, int64_t at, int64_t cols, float none, float (&v)[CHUNK<T>])
@@ -65,33 +75,36 @@ __global__ __launch_bounds__(BLOCK) void k_norm_fwd(int64_t rows, int cols, cons
                                                     float *__restrict__ rstd)
 {
     constexpr int N = CHUNK<T>, ROWS = BLOCK / LANES;
-    __shared__ float part[LANES > WAVE ? LANES / WAVE : 1];
+    __shared__ typename row_sums<LANES, BLOCK, 1>::place part;
+    row_sums<LANES, BLOCK, 1> sum(part);
     const int lane = threadIdx.x % LANES;
     const float n = (float)cols;  // divided by, so that a row of one value has exactly that mean
     for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < rows; r0 += (int64_t)gridDim.x * ROWS) {
         const int64_t r = r0 + threadIdx.x / LANES;
         const bool live = r < rows;  // the same in all lanes of a row; sums are taken by all
         float v[NV][N];
-        float s = 0.0f;
+        float s[1] = {0.0f};
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int at = (k * LANES + lane) * N;
             load_chunk<T>(x + r * xs + at, live ? cols - at : 0, v[k]);
 #pragma unroll
-            for (int i = 0; i < N; ++i) s += v[k][i];
+            for (int i = 0; i < N; ++i) s[0] += v[k][i];
         }
-        const float m = row_sum<LANES>(s, part) / n;
-        s = 0.0f;
+        sum(s);
+        const float m = s[0] / n;
+        s[0] = 0.0f;
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int at = (k * LANES + lane) * N;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 v[k][i] -= m;
-                s += at + i < cols ? v[k][i] * v[k][i] : 0.0f;
+                s[0] += at + i < cols ? v[k][i] * v[k][i] : 0.0f;
             }
         }
-        const float inv = 1.0f / sqrtf(row_sum<LANES>(s, part) / n + eps);
+        sum(s);
+        const float inv = 1.0f / sqrtf(s[0] / n + eps);
         if (live) {
             if (lane == 0) {
                 if (mean) mean[r] = m;
@@ -121,28 +134,37 @@ struct kept_matrix {
     const uint8_t *exps;
 };
 
+// A chunk of it as it lies in memory.
 template <class T, bool CKPT>
-__device__ inline void load_kept(const kept_matrix<T> &x, int64_t r, int at, int64_t cols, bool live,
-                                 float (&v)[CHUNK<T>])
-{
-    constexpr int N = CHUNK<T>;
-    if constexpr (!CKPT) {
-        load_chunk<T>(x.x + r * x.stride + at, live ? cols - at : 0, v);
-    } else if (live && at < cols) {  // a code row is whole groups: no partial chunk
-        const int64_t ld = (cols + GROUP - 1) / GROUP * GROUP;
-        vec<int8_t, N> q;
-        __builtin_memcpy(&q, x.codes + r * ld + at, N);
-        const float step = step_of(x.exps[r * (ld / GROUP) + at / GROUP]);
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = (float)q[i] * step;
-    } else {
-#pragma unroll
-        for (int i = 0; i < N; ++i) v[i] = 0.0f;
+struct kept_chunk {
+    static constexpr int N = CHUNK<T>;
+    std::conditional_t<CKPT, vec<int8_t, N>, vec<T, N>> raw;
+    uint8_t exp;
+    __device__ void load(const kept_matrix<T> &x, int64_t r, int at, int cols, bool live)
+    {
+        if constexpr (!CKPT) {
+            raw = load_raw<T>(x.x + r * x.stride + at, live ? cols - at : 0);
+        } else {
+            raw = {};
+            exp = 0;
+            if (live && at < cols) {  // a code row is whole groups: no partial chunk
+                const int ld = (cols + GROUP - 1) / GROUP * GROUP;
+                __builtin_memcpy(&raw, x.codes + r * ld + at, N);
+                exp = x.exps[r * (ld / GROUP) + at / GROUP];
+            }
+        }
     }
-}
+    __device__ void values(float (&v)[N]) const
+    {
+        const float step = CKPT ? step_of(exp) : 1.0f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] = CKPT ? (float)raw[i] * step : (float)raw[i];
+    }
+};
 
-// dx of the rows that a block takes in turn; the columns' sums of dy xh and dy over those rows stay in registers
-// and leave as one partial row [2, cols] per block (`sums`; no sums where it is NULL).
+// dx of the rows that a block takes in turn, the next row's loads in flight while a row is summed; the columns' sums of
+// dy xh and dy over those rows stay in registers and leave as one partial row [2, cols] per block (`sums`; no
+// sums where it is NULL).
 template <class T, class W, int LANES, int NV, int BLOCK, bool CKPT>
 __global__ __launch_bounds__(BLOCK) void k_norm_bwd(int64_t rows, int cols, const T *__restrict__ dy, int64_t dys,
                                                     kept_matrix<T> x, const float *__restrict__ mean,
@@ -150,43 +172,58 @@ __global__ __launch_bounds__(BLOCK) void k_norm_bwd(int64_t rows, int cols, cons
                                                     T *__restrict__ dx, int64_t dxs, float *__restrict__ sums)
 {
     constexpr int N = CHUNK<T>, ROWS = BLOCK / LANES;
-    __shared__ float part[LANES > WAVE ? LANES / WAVE : 1];
+    __shared__ typename row_sums<LANES, BLOCK, 2>::place part;
     __shared__ float joined[ROWS > 1 ? LANES * NV * N : 1];
+    row_sums<LANES, BLOCK, 2> sum(part);
     const int lane = threadIdx.x % LANES;
     const float n = (float)cols;
-    float dw[NV][N] = {}, db[NV][N] = {};
-    for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < rows; r0 += (int64_t)gridDim.x * ROWS) {
+    float dw[NV][N] = {}, db[NV][N] = {}, ww[NV][N];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) load_weight<T>(w, (k * LANES + lane) * N, cols, 1.0f, ww[k]);
+    vec<T, N> next_dy[NV];
+    kept_chunk<T, CKPT> next_x[NV];
+    float next_m = 0.0f, next_inv = 0.0f;
+    auto load = [&](int64_t r) {
+        const bool live = r < rows;
+        next_m = live ? mean[r] : 0.0f;
+        next_inv = live ? rstd[r] : 0.0f;
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const int at = (k * LANES + lane) * N;
+            next_dy[k] = load_raw<T>(dy + r * dys + at, live ? cols - at : 0);
+            next_x[k].load(x, r, at, cols, live);
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * ROWS;
+    load((int64_t)blockIdx.x * ROWS + threadIdx.x / LANES);
+    for (int64_t r0 = (int64_t)blockIdx.x * ROWS; r0 < rows; r0 += step) {
         const int64_t r = r0 + threadIdx.x / LANES;
         const bool live = r < rows;
-        const float m = live ? mean[r] : 0.0f, inv = live ? rstd[r] : 0.0f;
-        float v[NV][N], xh[NV][N];
-        float s1 = 0.0f, s2 = 0.0f;
+        const float m = next_m, inv = next_inv;
+        float v[NV][N], xh[NV][N], s[2] = {};
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
-            const int at = (k * LANES + lane) * N;
-            load_chunk<T>(dy + r * dys + at, live ? cols - at : 0, v[k]);
-            load_kept<T, CKPT>(x, r, at, cols, live, xh[k]);
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[k][i] = (float)next_dy[k][i];
+            next_x[k].values(xh[k]);
         }
+        load(r + step);
 #pragma unroll
         for (int k = 0; k < NV; ++k) {
             const int at = (k * LANES + lane) * N;
-            float ww[N];
-            load_weight<T>(w, at, cols, 1.0f, ww);
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 // columns past the row's end take no part, whatever the row's statistics are
-                xh[k][i] = at + i < cols ? (xh[k][i] - m) * inv : 0.0f;
-                if (live) {
-                    dw[k][i] += v[k][i] * xh[k][i];
-                    db[k][i] += v[k][i];
-                }
-                v[k][i] *= ww[i];
-                s1 += v[k][i];
-                s2 += v[k][i] * xh[k][i];
+                xh[k][i] = live && at + i < cols ? (xh[k][i] - m) * inv : 0.0f;
+                dw[k][i] += v[k][i] * xh[k][i];
+                db[k][i] += v[k][i];
+                v[k][i] *= ww[k][i];
+                s[0] += v[k][i];
+                s[1] += v[k][i] * xh[k][i];
             }
         }
-        s1 = row_sum<LANES>(s1, part) / n;
-        s2 = row_sum<LANES>(s2, part) / n;
+        sum(s);
+        const float s1 = s[0] / n, s2 = s[1] / n;
         if (live) {
 #pragma unroll
             for (int k = 0; k < NV; ++k) {
@@ -200,15 +237,27 @@ __global__ __launch_bounds__(BLOCK) void k_norm_bwd(int64_t rows, int cols, cons
         }
     }
     if (!sums) return;
-    // join the block's rows, one after the other, and write the block's partial sums
+    // join the rows of a wave, then the block's waves one after the other, and write the block's partial sums
+    constexpr int SLOTS = BLOCK / (LANES < WAVE ? WAVE : LANES);
+    if constexpr (LANES < WAVE) {
+#pragma unroll
+        for (int d = LANES; d < WAVE; d *= 2)
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    dw[k][i] += __shfl_xor(dw[k][i], d);
+                    db[k][i] += __shfl_xor(db[k][i], d);
+                }
+    }
     float *out = sums + (int64_t)blockIdx.x * 2 * cols;
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
-        if constexpr (ROWS > 1) {
-            const int slot = threadIdx.x / LANES;
-            for (int t = 0; t < ROWS; ++t) {
+        if constexpr (SLOTS > 1) {
+            const bool first_row = LANES >= WAVE || threadIdx.x % WAVE < LANES;
+            for (int t = 0; t < SLOTS; ++t) {
                 __syncthreads();
-                if (slot == t) {
+                if ((int)threadIdx.x / (BLOCK / SLOTS) == t && first_row) {
 #pragma unroll
                     for (int k = 0; k < NV; ++k)
 #pragma unroll
@@ -236,36 +285,51 @@ __global__ __launch_bounds__(BLOCK) void k_norm_bwd(int64_t rows, int cols, cons
     }
 }
 
-// Columns' sums from the blocks' partial rows, in the blocks' order within each of 8 shares.
+// Columns' sums from the blocks' partial rows: 16 shares of the rows, each in the blocks' order, for 64 columns of
+// dw and db in a block.
 template <class W>
 __global__ __launch_bounds__(256) void k_norm_cols(int blocks, int cols, const float *__restrict__ sums,
                                                    W *__restrict__ dw, W *__restrict__ db)
 {
-    __shared__ float share[8][32];
-    const int c = blockIdx.x * 32 + threadIdx.x % 32, part = threadIdx.x / 32;
+    constexpr int SHARES = 16;
+    __shared__ float share[SHARES][64];
+    const int quad = threadIdx.x % 16, part = threadIdx.x / 16, c0 = blockIdx.x * 64 + quad * 4;
     W *out = blockIdx.y ? db : dw;
-    float s = 0.0f;
-    if (c < cols)
-        for (int b = part; b < blocks; b += 8) s += sums[((int64_t)b * 2 + blockIdx.y) * cols + c];
-    share[part][threadIdx.x % 32] = s;
-    __syncthreads();
-    if (part == 0 && c < cols && out) {
+    if (!out) return;
+    float s[4] = {};
+    const float *from = sums + (int64_t)blockIdx.y * cols + c0;
+#pragma unroll 8
+    for (int b = part; b < blocks; b += SHARES) {
+        float v[4];
+        load_chunk<float>(from + (int64_t)b * 2 * cols, cols - c0, v);
 #pragma unroll
-        for (int p = 1; p < 8; ++p) s += share[p][threadIdx.x];
-        out[c] = (W)s;
+        for (int i = 0; i < 4; ++i) s[i] += v[i];
     }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) share[part][quad * 4 + i] = s[i];
+    __syncthreads();
+    const int c = threadIdx.x;
+    if (c >= 64 || blockIdx.x * 64 + c >= cols) return;
+    float all = 0.0f;
+#pragma unroll
+    for (int p = 0; p < SHARES; ++p) all += share[p][c];
+    out[blockIdx.x * 64 + c] = (W)all;
 }
 
-// Most blocks of a backward pass: each leaves a partial row of sums.
-int64_t bwd_blocks(int64_t rows, int rows_per_block)
+// Blocks of a backward pass.  Each leaves a partial row of sums where columns' sums are wanted, so few are better
+// that still keep 8 waves on every compute unit, and each should have 2 rows in turn or more.
+int64_t bwd_blocks(int64_t rows, int rows_per_block, int block, bool want)
 {
-    const int64_t need = (rows + rows_per_block - 1) / rows_per_block;
-    return need < 1 ? 1 : need < 512 ? need : 512;
+    const int64_t need = (rows + rows_per_block - 1) / rows_per_block, most = block == 256 ? 512 : 256;
+    if (!want) return std::max<int64_t>(1, std::min<int64_t>(need, 4 * most));
+    return std::max<int64_t>(1, std::min(most, std::max(std::min<int64_t>(need, 128), need / 2)));
 }
 
 // The rows' layout: LANES lanes of a block of BLOCK, NV chunks each, as few lanes as keep a
-// row in 4 chunks a lane.  N: elements of a chunk.
-template <int N, class F>
+// row in 4 chunks a lane.  N: elements of a chunk.  The backward pass (BWD) holds four values for each of the forward's one, and
+// takes more lanes for the widest rows: 4096 x 8192 (bf16) goes in 49 us with 1024 lanes and in 75 with
+// 256, its forward in 47 and 31.
+template <bool BWD, int N, class F>
 int with_layout(int64_t cols, F go)
 {
     const int64_t chunks = (cols + N - 1) / N;
@@ -276,7 +340,12 @@ int with_layout(int64_t cols, F go)
     if (chunks <= 128) RKB_LAYOUT(64, 2, NORM_BLOCK);
     if (chunks <= 256) RKB_LAYOUT(64, 4, NORM_BLOCK);
     if (chunks <= 512) RKB_LAYOUT(256, 2, NORM_BLOCK);
-    if (chunks <= 1024) RKB_LAYOUT(256, 4, NORM_BLOCK);
+    if (chunks <= 1024) {
+        if constexpr (BWD)
+            RKB_LAYOUT(1024, 1, 1024);
+        else
+            RKB_LAYOUT(256, 4, NORM_BLOCK);
+    }
     if constexpr (N * 2048 < RKB_MAX_NORM_COLS)
         if (chunks > 2048) RKB_LAYOUT(1024, 4, 1024);
     RKB_LAYOUT(1024, 2, 1024);
@@ -291,10 +360,10 @@ int with_types(int dtype, int wdtype, F go)
     return wdtype == RKB_F32 ? go((bf16 *)nullptr, (float *)nullptr) : go((bf16 *)nullptr, (bf16 *)nullptr);
 }
 
-int rows_per_block(int dtype, int64_t cols)
+int64_t bwd_blocks_of(int dtype, int64_t rows, int64_t cols)
 {
-    auto rows = [](auto lanes, auto, auto block) { return block() / lanes(); };
-    return dtype == RKB_F32 ? with_layout<4>(cols, rows) : with_layout<8>(cols, rows);
+    auto blocks = [&](auto lanes, auto, auto block) { return (int)bwd_blocks(rows, block() / lanes(), block(), true); };
+    return dtype == RKB_F32 ? with_layout<true, 4>(cols, blocks) : with_layout<true, 8>(cols, blocks);
 }
 
 bool good_norm(int dtype, int wdtype, int64_t rows, int64_t cols)
@@ -322,7 +391,7 @@ extern "C" int rkb_layer_norm_fwd(int dtype, int wdtype, int64_t rows, int64_t c
     return with_types(dtype, wdtype, [&](auto *t, auto *wt) {
         using T = std::remove_pointer_t<decltype(t)>;
         using W = std::remove_pointer_t<decltype(wt)>;
-        return with_layout<CHUNK<T>>(cols, [&](auto lanes, auto nv, auto block) {
+        return with_layout<false, CHUNK<T>>(cols, [&](auto lanes, auto nv, auto block) {
             constexpr int ROWS = block() / lanes();
             const int64_t blocks = std::min<int64_t>((rows + ROWS - 1) / ROWS, (int64_t)1 << 22);
             hipLaunchKernelGGL((k_norm_fwd<T, W, lanes(), nv(), block()>), dim3((uint32_t)blocks), dim3(block()), 0,
@@ -336,7 +405,7 @@ extern "C" int rkb_layer_norm_fwd(int dtype, int wdtype, int64_t rows, int64_t c
 extern "C" int rkb_layer_norm_bwd_workspace(int dtype, int64_t rows, int64_t cols, size_t *bytes)
 {
     if (!bytes || !good_norm(dtype, dtype, rows, cols)) return RKB_E_INVAL;
-    *bytes = (size_t)bwd_blocks(rows, rows_per_block(dtype, cols)) * 2 * cols * sizeof(float);
+    *bytes = (size_t)bwd_blocks_of(dtype, rows, cols) * 2 * cols * sizeof(float);
     return RKB_OK;
 }
 
@@ -372,8 +441,8 @@ extern "C" int rkb_layer_norm_bwd(int dtype, int wdtype, int64_t rows, int64_t c
         const kept_matrix<T> kept{(const T *)x, x_stride, codes, exps};
         const hipStream_t st = (hipStream_t)stream;
         int64_t blocks = 0;
-        int rc = with_layout<CHUNK<T>>(cols, [&](auto lanes, auto nv, auto block) {
-            blocks = bwd_blocks(rows, block() / lanes());
+        int rc = with_layout<true, CHUNK<T>>(cols, [&](auto lanes, auto nv, auto block) {
+            blocks = bwd_blocks(rows, block() / lanes(), block(), want);
             auto go = [&](auto kernel) {
                 hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(block()), 0, st, rows, (int)cols, (const T *)dy,
                                    dy_stride, kept, mean, rstd, (const W *)w, (T *)dx, dx_stride, sums);
@@ -385,7 +454,7 @@ extern "C" int rkb_layer_norm_bwd(int dtype, int wdtype, int64_t rows, int64_t c
             return launched();
         });
         if (rc != RKB_OK || !want) return rc;
-        hipLaunchKernelGGL((k_norm_cols<W>), dim3((uint32_t)((cols + 31) / 32), 2), dim3(256), 0, st, (int)blocks,
+        hipLaunchKernelGGL((k_norm_cols<W>), dim3((uint32_t)((cols + 63) / 64), 2), dim3(256), 0, st, (int)blocks,
                            (int)cols, sums, (W *)dw, (W *)db);
         return launched();
     });
