@@ -13,8 +13,8 @@
  *   - the weight gradient of a linear layer whose input was kept in 8 bits.
  *
  * Matrices are row-major with neighbouring columns adjacent; `..._stride` is the distance
- * between rows in elements, at least the number of columns (it is not read for matrices of at
- * most one row).  All pointers but *bytes are device memory of the device that is current.
+ * between rows in elements (not read for matrices of at most one row): at least the number of columns
+ * for an output, any number from 0 (one row for all) to 2^40 for an input.  All pointers but *bytes are device memory of the device that is current.
  * Outputs must not overlap inputs, other outputs or the workspace.  Sums, statistics and
  * products accumulate in 32 bits whatever the type; outputs are rounded once, to nearest even.
  *

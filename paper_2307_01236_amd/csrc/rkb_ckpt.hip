@@ -113,7 +113,7 @@ using namespace rkb;
 extern "C" int rkb_ckpt8_save(int dtype, int64_t rows, int64_t cols, const void *x, int64_t x_stride, int8_t *codes,
                               uint8_t *exps, void *stream)
 {
-    if (!good_dtype(dtype) || !good_size(rows, cols) || !good_matrix(x, rows, cols, x_stride, dtype_size(dtype)))
+    if (!good_dtype(dtype) || !good_size(rows, cols) || !good_input(x, rows, x_stride, dtype_size(dtype)))
         return RKB_E_INVAL;
     if (rows == 0) return RKB_OK;
     if (!codes || !exps || (uintptr_t)codes % 16) return RKB_E_INVAL;
@@ -130,7 +130,7 @@ extern "C" int rkb_ckpt8_save(int dtype, int64_t rows, int64_t cols, const void 
 extern "C" int rkb_ckpt8_load(int dtype, int64_t rows, int64_t cols, const int8_t *codes, const uint8_t *exps, void *x,
                               int64_t x_stride, void *stream)
 {
-    if (!good_dtype(dtype) || !good_size(rows, cols) || !good_matrix(x, rows, cols, x_stride, dtype_size(dtype)))
+    if (!good_dtype(dtype) || !good_size(rows, cols) || !good_output(x, rows, cols, x_stride, dtype_size(dtype)))
         return RKB_E_INVAL;
     if (rows == 0) return RKB_OK;
     if (!codes || !exps || (uintptr_t)codes % 16) return RKB_E_INVAL;

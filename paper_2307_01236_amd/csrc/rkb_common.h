@@ -163,11 +163,15 @@ inline bool good_size(int64_t rows, int64_t cols)
     return rows >= 0 && rows <= RKB_MAX_ROWS && cols >= 1 && cols <= RKB_MAX_COLS;
 }
 
-// A matrix argument: present, aligned to its type, with rows that do not overlap (a stride is not read for one row).
-inline bool good_matrix(const void *p, int64_t rows, int64_t cols, int64_t stride, int size)
+// A matrix argument: present, aligned to its type, and for an output with rows that do not overlap (a stride is not read for
+// one row).
+inline bool good_input(const void *p, int64_t rows, int64_t stride, int size)
 {
-    if (rows == 0) return true;
-    return p && (uintptr_t)p % size == 0 && (rows == 1 || (stride >= cols && stride <= ((int64_t)1 << 40)));
+    return rows == 0 || (p && (uintptr_t)p % size == 0 && (rows == 1 || (stride >= 0 && stride <= ((int64_t)1 << 40))));
+}
+inline bool good_output(const void *p, int64_t rows, int64_t cols, int64_t stride, int size)
+{
+    return good_input(p, rows, stride, size) && (rows <= 1 || stride >= cols);
 }
 
 inline int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }

@@ -165,8 +165,8 @@ struct cut {
 // The tiles, with the microseconds of one stage in a workgroup that runs nearly alone and on a full chip
 // (where the clock is lower and L2 shared), and of a tile's start and end, fitted to measured products
 // of 64 to 8192 rows (bf16).  Small tiles pay more per product and fill the chip sooner: at 8192 x 4096 x 11264 the
-// gated forward takes 1140 us by 256 x 256, 1237 by 192 x 256, 1533 by 128 x 256 and 1368 by 128 x 128; at 1024 x 1280 x 5120
-// it takes 36.7, 30.7, 43.7 and 37.5; at 512 x 1024 x 4096, 27.3, 22.0, 16.7 and 12.4.
+// gated forward takes 1140 us by 256 x 256, 1237 by 192 x 256 and 1368 by 128 x 128; at 1024 x 1280 x 5120 it takes
+// 36.7, 30.7 and 37.5; at 512 x 1024 x 4096, 27.3, 22.0 and 12.4.
 struct tile_kind {
     int tm, tn, slots;  // slots: workgroups that 256 compute units hold at once
     double alone, busy, ends;
@@ -174,7 +174,6 @@ struct tile_kind {
 constexpr tile_kind TILES[] = {
     {256, 256, 256, 1.05, 1.68, 5.0},
     {192, 256, 256, 0.82, 1.29, 4.5},
-    {128, 256, 256, 0.66, 1.07, 4.0},
     {128, 128, 512, 0.50, 0.97, 3.0},
 };
 constexpr double JOIN_FIXED = 4.0, JOIN_BYTES = 4.5e6;  // microseconds, bytes a microsecond
@@ -225,8 +224,7 @@ int launch_product(product pr, const cut &c, const EPI &epi, hipStream_t st)
 template <class T, bool ANEAR, bool BNEAR, int PARTS, class EPI>
 int run_product(const product &pr, const cut &c, const EPI &epi, hipStream_t st)
 {
-    if (c.tn == 128) return launch_product<T, ANEAR, BNEAR, PARTS, 128, 128, 2, 2>(pr, c, epi, st);
-    if (c.tm == 128) return launch_product<T, ANEAR, BNEAR, PARTS, 128, 256, 2, 4>(pr, c, epi, st);
+    if (c.tm == 128) return launch_product<T, ANEAR, BNEAR, PARTS, 128, 128, 2, 2>(pr, c, epi, st);
     if constexpr (ANEAR)
         if (c.tm == 192) return launch_product<T, ANEAR, BNEAR, PARTS, 192, 256, 2, 4>(pr, c, epi, st);
     return launch_product<T, ANEAR, BNEAR, PARTS, 256, 256, 2, 4>(pr, c, epi, st);
@@ -544,10 +542,10 @@ extern "C" int rkb_weight_grad(int dtype, int64_t rows, int64_t n, int64_t k, co
                                int64_t dw_stride, void *workspace, size_t ws_bytes, void *stream)
 {
     const bool ckpt = codes != nullptr;
-    if (!good_dtype16(dtype) || !good_size(rows, n) || !good_size(rows, k) || !good_matrix(dy, rows, n, dy_stride, 2) ||
-        !good_matrix(dw, n, k, dw_stride, 2))
+    if (!good_dtype16(dtype) || !good_size(rows, n) || !good_size(rows, k) || !good_input(dy, rows, dy_stride, 2) ||
+        !good_output(dw, n, k, dw_stride, 2))
         return RKB_E_INVAL;
-    if (rows > 0 && (ckpt ? (x || !exps || (uintptr_t)codes % 16) : (exps || !good_matrix(x, rows, k, x_stride, 2))))
+    if (rows > 0 && (ckpt ? (x || !exps || (uintptr_t)codes % 16) : (exps || !good_input(x, rows, x_stride, 2))))
         return RKB_E_INVAL;
     const hipStream_t st = (hipStream_t)stream;
     workspace_taker ws(workspace, ws_bytes);
@@ -627,8 +625,8 @@ extern "C" int rkb_gated_fwd(int dtype, int act, int keep, int64_t rows, int64_t
                              int64_t h_stride, void *g, void *u, uint8_t *ge, uint8_t *ue, void *workspace, size_t ws_bytes,
                              void *stream)
 {
-    if (!good_gated(dtype, act, keep, rows, d, f) || !good_matrix(x, rows, d, x_stride, 2) ||
-        !good_matrix(wg, f, d, wg_stride, 2) || !good_matrix(wu, f, d, wu_stride, 2) || !good_matrix(h, rows, f, h_stride, 2) ||
+    if (!good_gated(dtype, act, keep, rows, d, f) || !good_input(x, rows, x_stride, 2) ||
+        !good_input(wg, f, wg_stride, 2) || !good_input(wu, f, wu_stride, 2) || !good_output(h, rows, f, h_stride, 2) ||
         !good_kept(keep, rows, g, u, ge, ue))
         return RKB_E_INVAL;
     if (rows == 0) return RKB_OK;
@@ -669,11 +667,11 @@ extern "C" int rkb_gated_bwd(int dtype, int act, int keep, int64_t rows, int64_t
                              const uint8_t *ue, void *dx, int64_t dx_stride, void *dwg, void *dwu, int64_t dw_stride, void *h,
                              int64_t h_stride, void *workspace, size_t ws_bytes, void *stream)
 {
-    if (!good_gated(dtype, act, keep, rows, d, f) || !good_matrix(dh, rows, f, dh_stride, 2) ||
-        !good_matrix(x, rows, d, x_stride, 2) || !good_matrix(wg, f, d, wg_stride, 2) || !good_matrix(wu, f, d, wu_stride, 2) ||
-        !good_kept(keep, rows, g, u, ge, ue) || (dx && !good_matrix(dx, rows, d, dx_stride, 2)) || (!dwg != !dwu) ||
-        (dwg && (!good_matrix(dwg, f, d, dw_stride, 2) || !good_matrix(dwu, f, d, dw_stride, 2))) ||
-        (h && !good_matrix(h, rows, f, h_stride, 2)))
+    if (!good_gated(dtype, act, keep, rows, d, f) || !good_input(dh, rows, dh_stride, 2) ||
+        !good_input(x, rows, x_stride, 2) || !good_input(wg, f, wg_stride, 2) || !good_input(wu, f, wu_stride, 2) ||
+        !good_kept(keep, rows, g, u, ge, ue) || (dx && !good_output(dx, rows, d, dx_stride, 2)) || (!dwg != !dwu) ||
+        (dwg && (!good_output(dwg, f, d, dw_stride, 2) || !good_output(dwu, f, d, dw_stride, 2))) ||
+        (h && !good_output(h, rows, f, h_stride, 2)))
         return RKB_E_INVAL;
     const hipStream_t st = (hipStream_t)stream;
     workspace_taker ws(workspace, ws_bytes);

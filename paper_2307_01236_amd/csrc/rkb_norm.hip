@@ -384,7 +384,7 @@ extern "C" int rkb_layer_norm_fwd(int dtype, int wdtype, int64_t rows, int64_t c
 {
     if (!good_norm(dtype, wdtype, rows, cols) || !(eps >= 0.0f) || !(eps < INFINITY)) return RKB_E_INVAL;
     const int size = dtype_size(dtype), wsize = dtype_size(wdtype);
-    if (!good_matrix(x, rows, cols, x_stride, size) || !good_matrix(y, rows, cols, y_stride, size) ||
+    if (!good_input(x, rows, x_stride, size) || !good_output(y, rows, cols, y_stride, size) ||
         !aligned_or_null(w, wsize) || !aligned_or_null(b, wsize) || !aligned_or_null(mean, 4) || !aligned_or_null(rstd, 4))
         return RKB_E_INVAL;
     if (rows == 0) return RKB_OK;
@@ -417,12 +417,12 @@ extern "C" int rkb_layer_norm_bwd(int dtype, int wdtype, int64_t rows, int64_t c
     if (!good_norm(dtype, wdtype, rows, cols)) return RKB_E_INVAL;
     const int size = dtype_size(dtype), wsize = dtype_size(wdtype);
     const bool ckpt = codes != nullptr;
-    if (!good_matrix(dy, rows, cols, dy_stride, size) || !good_matrix(dx, rows, cols, dx_stride, size) ||
+    if (!good_input(dy, rows, dy_stride, size) || !good_output(dx, rows, cols, dx_stride, size) ||
         !aligned_or_null(w, wsize) || !aligned_or_null(dw, wsize) || !aligned_or_null(db, wsize))
         return RKB_E_INVAL;
     if (rows > 0) {
         if (!mean || !rstd || !aligned_or_null(mean, 4) || !aligned_or_null(rstd, 4)) return RKB_E_INVAL;
-        if (ckpt ? (x || !exps || (uintptr_t)codes % 16) : (exps || !good_matrix(x, rows, cols, x_stride, size)))
+        if (ckpt ? (x || !exps || (uintptr_t)codes % 16) : (exps || !good_input(x, rows, x_stride, size)))
             return RKB_E_INVAL;
     }
     const bool want = dw || db;

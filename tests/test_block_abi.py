@@ -55,24 +55,24 @@ CALLS = dict(rkb_layer_norm_fwd=NORM_FWD, rkb_layer_norm_bwd=NORM_BWD, rkb_ckpt8
              rkb_weight_grad=WGRAD, rkb_gated_fwd=FWD, rkb_gated_bwd=BWD)
 COMMON = [dict(dtype=3), dict(dtype=-1), dict(rows=-1), dict(rows=(1 << 30) + 1)]
 REFUSED = dict(
-    rkb_layer_norm_fwd=COMMON + [dict(cols=0), dict(cols=16385), dict(x=None), dict(y=None), dict(x=P + 1), dict(xs=63),
+    rkb_layer_norm_fwd=COMMON + [dict(cols=0), dict(cols=16385), dict(x=None), dict(y=None), dict(x=P + 1), dict(xs=-1), dict(xs=(1 << 40) + 1),
                                  dict(ys=63), dict(eps=-1.0), dict(eps=float("nan")), dict(eps=float("inf")),
                                  dict(wdtype=bk.RKB_F16), dict(w=P + 1), dict(mean=P + 2)],
-    rkb_layer_norm_bwd=COMMON + [dict(cols=0), dict(cols=16385), dict(dy=None), dict(x=None), dict(dx=None), dict(dys=63),
+    rkb_layer_norm_bwd=COMMON + [dict(cols=0), dict(cols=16385), dict(dy=None), dict(x=None), dict(dx=None), dict(dys=-1), dict(dxs=63),
                                  dict(codes=P), dict(exps=P), dict(x=None, codes=P), dict(x=None, codes=P + 8, exps=P),
                                  dict(mean=None), dict(rstd=None), dict(ws=None), dict(ws=P + 16), dict(wdtype=bk.RKB_F16)],
-    rkb_ckpt8_save=COMMON + [dict(cols=0), dict(cols=(1 << 24) + 1), dict(x=None), dict(xs=63), dict(codes=None),
+    rkb_ckpt8_save=COMMON + [dict(cols=0), dict(cols=(1 << 24) + 1), dict(x=None), dict(xs=-1), dict(codes=None),
                              dict(exps=None), dict(codes=P + 8), dict(x=P + 1)],
     rkb_ckpt8_load=COMMON + [dict(cols=0), dict(x=None), dict(xs=63), dict(codes=None), dict(exps=None), dict(codes=P + 8)],
-    rkb_weight_grad=COMMON + [dict(dtype=bk.RKB_F32), dict(n=0), dict(k=0), dict(dy=None), dict(dys=31), dict(dw=None),
+    rkb_weight_grad=COMMON + [dict(dtype=bk.RKB_F32), dict(n=0), dict(k=0), dict(dy=None), dict(dys=-1), dict(dw=None),
                               dict(dws=63), dict(x=P), dict(codes=None), dict(exps=None), dict(codes=None, exps=None),
                               dict(codes=P + 4), dict(ws=None), dict(ws=P + 8)],
     rkb_gated_fwd=COMMON + [dict(dtype=bk.RKB_F32), dict(act=2), dict(act=-1), dict(keep=4), dict(keep=3), dict(keep=-1), dict(d=0),
-                            dict(f=0), dict(x=None), dict(wg=None), dict(wu=None), dict(h=None), dict(xs=63), dict(wgs=63),
-                            dict(wus=63), dict(hs=31), dict(g=None), dict(ge=None), dict(u=P + 8), dict(keep=1),
+                            dict(f=0), dict(x=None), dict(wg=None), dict(wu=None), dict(h=None), dict(xs=-1), dict(wgs=-1),
+                            dict(wus=-2), dict(hs=31), dict(g=None), dict(ge=None), dict(u=P + 8), dict(keep=1),
                             dict(keep=0)],
     rkb_gated_bwd=COMMON + [dict(dtype=bk.RKB_F32), dict(act=2), dict(keep=4), dict(keep=3), dict(d=0), dict(f=0), dict(dh=None),
-                            dict(x=None), dict(wg=None), dict(wu=None), dict(dhs=31), dict(xs=63), dict(g=None),
+                            dict(x=None), dict(wg=None), dict(wu=None), dict(dhs=-1), dict(xs=-3), dict(g=None),
                             dict(ue=None), dict(keep=1), dict(keep=0), dict(dwg=None), dict(dwu=None), dict(dws=63),
                             dict(dxs=63), dict(hs=31), dict(ws=None), dict(ws=P + 64)],
 )

@@ -313,6 +313,76 @@ def test_gated_keeps_a_bad_token_to_itself():
     assert bool(got[1].isnan().all())  # every weight saw the token
 
 
+@pytest.mark.parametrize("act,dtype", [("silu", BF), ("gelu", HF)])
+@pytest.mark.parametrize("rows,width,hidden", [(1000, 520, 8200), (4100, 72, 3000), (3000, 264, 2056), (4096, 4096, 72),
+                                               (40, 2000, 6000), (90, 4096, 2000)])
+def test_gated_at_sizes_of_every_tile(rows, width, hidden, act, dtype):
+    """Large enough for the larger tiles, split sums and many workgroups; the 64-bit side runs on the GPU."""
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    x, wg, wu, dh = (torch.randn(*s, generator=gen, device="cuda").mul_(f).to(dtype) for s, f in (
+        ((rows, width), 1.0), ((hidden, width), width ** -0.5), ((hidden, width), width ** -0.5), ((rows, hidden), 0.1)))
+    X, G, U, DH = x.double(), wg.double(), wu.double(), dh.double()
+    mm = lambda a, b: torch.mm(a.contiguous(), b.contiguous())  # noqa: E731
+    g, u = mm(X, G.t()), mm(X, U.t())
+    a, s = bo.act(g, act)
+    h, kept = bk.rkb_gated_fwd(x, wg, wu, act, keep="full")
+    assert float(((h.double() - a * u).norm() / (a * u).norm())) <= bo.ROUND[dtype][0]
+    for t, ref in zip(kept, (g, u)):
+        assert float((t.double() - ref).abs().max()) <= bo.U32 * width * float(mm(X.abs(), G.abs().t()).max())
+    dx, dwg, dwu, h2 = bk.rkb_gated_bwd(dh, x, wg, wu, act, kept, want_h=True)
+    again = bk.rkb_gated_bwd(dh, x, wg, wu, act, None, want_h=True)
+    assert torch.equal(h, h2) and all(torch.equal(p, q) for p, q in zip((dx, dwg, dwu, h2), again))
+    dg, du = DH * u * s, DH * a
+    # each operand dg or du and each output is rounded once: two roundings of u, rms below the bound of one
+    for got, ref in ((dx, mm(dg, G) + mm(du, U)), (dwg, mm(dg.t(), X)), (dwu, mm(du.t(), X))):
+        assert float((got.double() - ref).norm() / ref.norm()) <= bo.ROUND[dtype][0]
+
+
+def test_offsets_past_32_bits():
+    """Rows 2^22 elements apart, and matrices of more than 2^31 elements."""
+    far = 1 << 22
+    store = torch.zeros(1100 * far // 2, dtype=BF, device="cuda")  # 2.3e9 elements
+    x = torch.as_strided(store, (540, 64), (far, 1))
+    x.copy_(rand(540, 64, seed=1, dtype=BF))
+    near = x.clone()
+    wg, wu, dh = rand(96, 64, seed=2, dtype=BF), rand(96, 64, seed=3, dtype=BF), rand(540, 96, seed=4, dtype=BF)
+    a, b = bk.rkb_gated_fwd(x, wg, wu, keep="8bit"), bk.rkb_gated_fwd(near, wg, wu, keep="8bit")
+    assert torch.equal(a[0], b[0])
+    assert all(torch.equal(p, q) for p, q in zip(bk.rkb_gated_bwd(dh, x, wg, wu, kept=a[1])[:3],
+                                                 bk.rkb_gated_bwd(dh, near, wg, wu, kept=b[1])[:3]))
+    assert torch.equal(bk.rkb_weight_grad(dh, x), bk.rkb_weight_grad(dh, near))
+    assert all(torch.equal(p, q) for p, q in zip(bk.rkb_layer_norm_fwd(x), bk.rkb_layer_norm_fwd(near)))
+    assert torch.equal(bk.rkb_ckpt8_save(x).codes, bk.rkb_ckpt8_save(near).codes)
+    del store, x
+    rows, cols = (1 << 18) + 3, 8200
+    big = torch.empty(rows, cols, dtype=BF, device="cuda").normal_()
+    y, mean, rstd = bk.rkb_layer_norm_fwd(big)
+    c = bk.rkb_ckpt8_save(big)
+    dx = bk.rkb_layer_norm_bwd(big, c, mean, rstd)[0]
+    values = bk.rkb_ckpt8_load(c)
+    last = big[-5:].clone()
+    y2, mean2, rstd2 = bk.rkb_layer_norm_fwd(last)
+    c2 = bk.rkb_ckpt8_save(last)
+    assert torch.equal(y[-5:], y2) and torch.equal(mean[-5:], mean2) and torch.equal(rstd[-5:], rstd2)
+    assert torch.equal(c.codes[-5:], c2.codes) and torch.equal(values[-5:], bk.rkb_ckpt8_load(c2))
+    assert torch.equal(dx[-5:], bk.rkb_layer_norm_bwd(last, c2, mean2, rstd2)[0])
+
+
+def test_broadcast_rows():
+    """One row that stands for all of an input (a stride of 0), as an expanded gradient has."""
+    x, wg, wu, _ = gated_inputs(70, 136, 200, BF)
+    dy, dh = rand(1, 136, seed=8, dtype=BF), rand(1, 200, seed=9, dtype=BF)
+    _, mean, rstd = bk.rkb_layer_norm_fwd(x)
+    wide, full = dy.expand(70, 136), dy.expand(70, 136).contiguous()
+    for p, q in zip(bk.rkb_layer_norm_bwd(wide, x, mean, rstd, bias=True), bk.rkb_layer_norm_bwd(full, x, mean, rstd, bias=True)):
+        assert (p is None and q is None) or torch.equal(p, q)
+    assert torch.equal(bk.rkb_weight_grad(wide, x), bk.rkb_weight_grad(full, x))
+    for kept in (None, bk.rkb_gated_fwd(x, wg, wu, keep="8bit")[1]):
+        assert all(torch.equal(p, q) for p, q in zip(bk.rkb_gated_bwd(dh.expand(70, 200), x, wg, wu, kept=kept)[:3],
+                                                     bk.rkb_gated_bwd(dh.expand(70, 200).contiguous(), x, wg, wu, kept=kept)[:3]))
+    assert torch.equal(bk.rkb_ckpt8_save(wide).codes, bk.rkb_ckpt8_save(full).codes)
+
+
 # ------------------------------------------------------------------ calls
 
 def all_calls(x, w, b, dy, wg, wu, dh):
