@@ -156,9 +156,9 @@ constexpr int64_t MAX_TILES = (int64_t)1 << 22;  // workgroups of a launch: 512 
 
 // ------------------------------------------------------------------ products
 
-// How a product is cut: the tile, and how many workgroups share the stages of one tile (splits).
+// How a product is cut: the tile, its buffers, and how many workgroups share the stages of one tile (splits).
 struct cut {
-    int tm, tn, splits;
+    int tm, tn, bufs, splits;
     double us;  // what the choice expects it to take
 };
 
@@ -166,15 +166,18 @@ struct cut {
 // (where the clock is lower and L2 shared), and of a tile's start and end, fitted to measured products
 // of 64 to 8192 rows (bf16).  Small tiles pay more per product and fill the chip sooner: at 8192 x 4096 x 11264 the
 // gated forward takes 1140 us by 256 x 256, 1237 by 192 x 256 and 1368 by 128 x 128; at 1024 x 1280 x 5120 it takes
-// 36.7, 30.7 and 37.5; at 512 x 1024 x 4096, 27.3, 22.0 and 12.4.
+// 36.7, 30.7 and 36.4; at 512 x 1024 x 4096, 27.3, 22.0 and 12.2.  Four buffers hide the latency of copies where a compute
+// unit has one workgroup: 128 x 4096 x 4096 takes 26.8 us with them and 40.0 with two, 1024 x 1280 x 5120
+// 36.7 and 36.4.
 struct tile_kind {
-    int tm, tn, slots;  // slots: workgroups that 256 compute units hold at once
+    int tm, tn, bufs, slots;  // slots: workgroups that 256 compute units hold at once
     double alone, busy, ends;
 };
 constexpr tile_kind TILES[] = {
-    {256, 256, 256, 1.05, 1.68, 5.0},
-    {192, 256, 256, 0.82, 1.29, 4.5},
-    {128, 128, 512, 0.50, 0.97, 3.0},
+    {256, 256, 2, 256, 1.05, 1.68, 5.0},
+    {192, 256, 2, 256, 0.82, 1.29, 4.5},
+    {128, 128, 2, 512, 0.49, 0.95, 2.5},
+    {128, 128, 4, 256, 0.36, 0.48, 3.5},
 };
 constexpr double JOIN_FIXED = 4.0, JOIN_BYTES = 4.5e6;  // microseconds, bytes a microsecond
 
@@ -184,7 +187,7 @@ constexpr double JOIN_FIXED = 4.0, JOIN_BYTES = 4.5e6;  // microseconds, bytes a
 cut choose_cut(int64_t M, int64_t N, int64_t K, int parts, int problems, int sums, bool near)
 {
     const int64_t stages = std::max<int64_t>(1, (K + DEPTH - 1) / DEPTH * parts);
-    cut best{256, 256, 1, 1e30};
+    cut best{256, 256, 2, 1, 1e30};
     for (const tile_kind &t : TILES) {
         if (t.tm == 192 && !near) continue;
         const int64_t tiles = (M + t.tm - 1) / t.tm * ((N + t.tn / sums - 1) / (t.tn / sums)) * problems;
@@ -195,7 +198,7 @@ cut choose_cut(int64_t M, int64_t N, int64_t K, int parts, int problems, int sum
             double us = rounds * (each * t.busy + t.ends);
             if (rest) us += each * (t.alone + (t.busy - t.alone) * rest / t.slots) + t.ends;
             if (splits > 1) us += JOIN_FIXED + 2.0 * 4.0 * splits * problems * (double)M * N / JOIN_BYTES;
-            if (us < best.us) best = cut{t.tm, t.tn, splits, us};
+            if (us < best.us) best = cut{t.tm, t.tn, t.bufs, splits, us};
         }
     }
     return best;
@@ -206,7 +209,7 @@ size_t split_bytes(const cut &c, int64_t M, int64_t N, int problems)
     return c.splits == 1 ? 0 : (size_t)round_up((int64_t)c.splits * problems * M * round_up(N, 8) * 4, WS_ALIGN);
 }
 
-template <class T, bool ANEAR, bool BNEAR, int PARTS, int TM, int TN, int WM, int WN, class EPI>
+template <class T, bool ANEAR, bool BNEAR, int PARTS, int TM, int TN, int WM, int WN, int BUFS, class EPI>
 int launch_product(product pr, const cut &c, const EPI &epi, hipStream_t st)
 {
     pr.tiles_m = (int)((pr.M + TM - 1) / TM);
@@ -216,7 +219,7 @@ int launch_product(product pr, const cut &c, const EPI &epi, hipStream_t st)
     pr.split_stages = (stages + c.splits - 1) / c.splits;
     const int64_t total = (int64_t)pr.tiles_m * pr.tiles_n * pr.problems * pr.splits;
     if (total > MAX_TILES) return RKB_E_INVAL;
-    hipLaunchKernelGGL((k_product<T, EPI, TM, TN, WM, WN, ANEAR, BNEAR, PARTS>), dim3((uint32_t)total), dim3(WM * WN * WAVE), 0, st,
+    hipLaunchKernelGGL((k_product<T, EPI, TM, TN, WM, WN, BUFS, ANEAR, BNEAR, PARTS>), dim3((uint32_t)total), dim3(WM * WN * WAVE), 0, st,
                        pr, epi);
     return launched();
 }
@@ -224,10 +227,12 @@ int launch_product(product pr, const cut &c, const EPI &epi, hipStream_t st)
 template <class T, bool ANEAR, bool BNEAR, int PARTS, class EPI>
 int run_product(const product &pr, const cut &c, const EPI &epi, hipStream_t st)
 {
-    if (c.tm == 128) return launch_product<T, ANEAR, BNEAR, PARTS, 128, 128, 2, 2>(pr, c, epi, st);
+    if (c.tm == 128)
+        return c.bufs == 2 ? launch_product<T, ANEAR, BNEAR, PARTS, 128, 128, 4, 2, 2>(pr, c, epi, st)
+                           : launch_product<T, ANEAR, BNEAR, PARTS, 128, 128, 4, 2, 4>(pr, c, epi, st);
     if constexpr (ANEAR)
-        if (c.tm == 192) return launch_product<T, ANEAR, BNEAR, PARTS, 192, 256, 2, 4>(pr, c, epi, st);
-    return launch_product<T, ANEAR, BNEAR, PARTS, 256, 256, 2, 4>(pr, c, epi, st);
+        if (c.tm == 192) return launch_product<T, ANEAR, BNEAR, PARTS, 192, 256, 2, 4, 2>(pr, c, epi, st);
+    return launch_product<T, ANEAR, BNEAR, PARTS, 256, 256, 2, 4, 2>(pr, c, epi, st);
 }
 
 // The splits' partial sums, in their order.

@@ -3,7 +3,7 @@
 // C[m, n] = sum over k of A(m, k) B(n, k) in tiles of TM x TN, depth 64.  A workgroup of WM x WN
 // waves keeps its tile of C in registers; the operands' next 64 columns are copied from memory
 // straight into LDS (16 bytes a lane, no registers in between) while the waves work on the present
-// ones, in two buffers.  An operand lies in memory either with k adjacent (a row per m or n)
+// ones, in two or four buffers.  An operand lies in memory either with k adjacent (a row per m or n)
 // or with m or n adjacent (a row per k); the matrix units want 8 neighbouring k of one row in a
 // lane, which LDS reads as they lie in the first form, and by its transposing read in the second.
 //
@@ -33,7 +33,8 @@ __device__ inline f32x4 mma(frag<f16> a, frag<f16> b, f32x4 c)
 }
 
 constexpr int DEPTH = 64;                // k of a stage
-constexpr int WAIT_ALL = 0x0070;         // s_waitcnt vmcnt(0) lgkmcnt(0)
+// s_waitcnt for all LDS reads and all but the last n copies
+constexpr int wait_copies(int n) { return (n & 15) | 0x70 | n >> 4 << 14; }
 constexpr int PIECE = 1024;              // bytes that one wave's copy instruction brings
 constexpr int PIECE_APART = PIECE + 32;  // distance of pieces of the row-per-k form
 
@@ -176,7 +177,8 @@ __device__ inline tile_at find_tile(const product &pr)
     return t;
 }
 
-template <class T, class EPI, int TM, int TN, int WM, int WN, bool ANEAR, bool BNEAR, int PARTS>
+// BUFS: stages that LDS holds.
+template <class T, class EPI, int TM, int TN, int WM, int WN, int BUFS, bool ANEAR, bool BNEAR, int PARTS>
 __global__ __launch_bounds__(WM *WN *WAVE) void k_product(product pr, EPI epi)
 {
     constexpr int WAVES = WM * WN, SUMS = EPI::SUMS;
@@ -184,7 +186,11 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(product pr, EPI epi)
     static_assert(FN == 4);
     using SA = stager<T, TM, WAVES, ANEAR, false>;
     using SB = stager<T, TN, WAVES, BNEAR, SUMS == 2>;
-    __shared__ __align__(16) char a0[SA::BYTES], a1[SA::BYTES], b0[SB::BYTES], b1[SB::BYTES];
+    // separate arrays: the compiler must see that reads of one do not wait for copies into another
+    __shared__ __align__(16) char s0[SA::BYTES + SB::BYTES], s1[SA::BYTES + SB::BYTES];
+    __shared__ __align__(16) char s2[BUFS > 2 ? SA::BYTES + SB::BYTES : 16], s3[BUFS > 2 ? SA::BYTES + SB::BYTES : 16];
+    static_assert(BUFS == 2 || BUFS == 4);
+    lds_byte *const lds[4] = {(lds_byte *)s0, (lds_byte *)s1, (lds_byte *)s2, (lds_byte *)s3};
 
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int wm = wave / WN, wn = wave % WN;
@@ -203,13 +209,13 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(product pr, EPI epi)
     // the operands of this workgroup's tile: of the first or only part, and of the second
     const char *pa0 = pr.a[t.problem] + a_row0, *pa1 = pr.a[1] + a_row0;
     const char *pb0 = pr.b[0] + b_row0, *pb1 = pr.b[1] + b_row0;
-    auto copy = [&](auto full, int s, lds_byte *a, lds_byte *b) {
+    auto copy = [&](auto full, int s, lds_byte *to) {
         const bool second = PARTS == 2 && s >= stages_k;
         const int k0 = (s - (second ? stages_k : 0)) * DEPTH, left = (int)pr.K - k0;
         const char *pa = (second ? pa1 : pa0) + k0 * a_step, *pb = (second ? pb1 : pb0) + k0 * b_step;
         const char *pu = pb1 + k0 * b_step;
-        sa.template copy<full()>(wave, lane, [&](int) { return pa; }, left, a);
-        sb.template copy<full()>(wave, lane, [&](int piece) { return SUMS == 2 && piece / 4 % 2 ? pu : pb; }, left, b);
+        sa.template copy<full()>(wave, lane, [&](int) { return pa; }, left, to);
+        sb.template copy<full()>(wave, lane, [&](int piece) { return SUMS == 2 && piece / 4 % 2 ? pu : pb; }, left, to + SA::BYTES);
     };
     constexpr std::true_type full{};
     constexpr std::false_type any{};
@@ -218,11 +224,11 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(product pr, EPI epi)
 
     f32x4 acc[FM][FN] = {};
     frag<T> fa[2][FM], fb[2][FN];
-    auto fetch = [&](int half, lds_byte *a, lds_byte *b) {
+    auto fetch = [&](int half, lds_byte *from) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j) fb[half][j] = SB::read(b + b_at[half], j);
+        for (int j = 0; j < FN; ++j) fb[half][j] = SB::read(from + SA::BYTES + b_at[half], j);
 #pragma unroll
-        for (int i = 0; i < FM; ++i) fa[half][i] = SA::read(a + a_at[half], i);
+        for (int i = 0; i < FM; ++i) fa[half][i] = SA::read(from + a_at[half], i);
     };
     auto multiply = [&](int half) {
 #pragma unroll
@@ -243,55 +249,70 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(product pr, EPI epi)
         }
 #pragma unroll
         for (int i = 0; i < FM; ++i) {
-            __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
+            if constexpr (EACH > 0) __builtin_amdgcn_sched_group_barrier(0x008, EACH, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, RA, 0);
             if (FN + i < copies()) __builtin_amdgcn_sched_group_barrier(0x010, 1, 0);
         }
         __builtin_amdgcn_sched_group_barrier(0x008, FM * FN - FN - FM * EACH, 0);
     };
-    // Stage s from one buffer while the next lies in, or is on its way to, the other.  All waves have read the
-    // present buffer when they pass the barrier, and all copies of the next stage have landed; so the
-    // stage after it may be copied over the present one while its second half is multiplied.
-    // AHEAD: that stage exists and is full.
-    auto stage = [&](auto ahead, int s, lds_byte *a, lds_byte *b, lds_byte *a_next, lds_byte *b_next) {
-        fetch(1, a, b);
+    // Stage s from buffer `at` while the next ones lie in, or are on their way to, the others.  All waves have read
+    // this buffer when they pass the barrier, and all copies of the next stage have landed (copies land in
+    // order: those of BUFS - 2 later stages may still be on their way); so stage s + BUFS may be copied over
+    // this one while its second half is multiplied.  AHEAD: that stage exists and is full.
+    constexpr int FLYING = (BUFS - 2) * (SA::MINE + SB::MINE);
+    auto stage = [&](auto ahead, int s, auto at) {
+        lds_byte *here = lds[at()], *next = lds[(at() + 1) % BUFS];
+        fetch(1, here);
         multiply(0);
         mix(std::integral_constant<int, 0>());
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(WAIT_ALL);
+        __builtin_amdgcn_s_waitcnt(ahead() ? wait_copies(FLYING) : wait_copies(0));
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         if constexpr (ahead()) {
-            copy(full, s + 2, a, b);
-            fetch(0, a_next, b_next);
+            copy(full, s + BUFS, here);
+            fetch(0, next);
             multiply(1);
             mix(std::integral_constant<int, SA::MINE + SB::MINE>());
             __builtin_amdgcn_sched_barrier(0);
         } else {
-            if (s + 2 < last) copy(any, s + 2, a, b);
-            fetch(0, a_next, b_next);  // past the last stage: whatever lies there, not used
+            if (s + BUFS < last) copy(any, s + BUFS, here);
+            fetch(0, next);  // past the last stage: whatever lies there, not used
             multiply(1);
             mix(std::integral_constant<int, 0>());
         }
     };
-    lds_byte *la0 = (lds_byte *)a0, *la1 = (lds_byte *)a1, *lb0 = (lds_byte *)b0, *lb1 = (lds_byte *)b1;
+    constexpr std::integral_constant<int, 0> at0{};
+    constexpr std::integral_constant<int, 1> at1{};
+    constexpr std::integral_constant<int, BUFS == 4 ? 2 : 0> at2{};
+    constexpr std::integral_constant<int, BUFS == 4 ? 3 : 1> at3{};
     if (first < last) {
-        if (first + 1 < last) copy(any, first + 1, la1, lb1);
-        copy(any, first, la0, lb0);
-        __builtin_amdgcn_s_waitcnt(WAIT_ALL);
+        if (BUFS == 4 && first + 3 < last) copy(any, first + 3, lds[3]);
+        if (BUFS == 4 && first + 2 < last) copy(any, first + 2, lds[2]);
+        if (first + 1 < last) copy(any, first + 1, lds[1]);
+        copy(any, first, lds[0]);
+        __builtin_amdgcn_s_waitcnt(wait_copies(0));
         __builtin_amdgcn_s_barrier();
-        fetch(0, la0, lb0);
+        fetch(0, lds[0]);
         const bool ragged = pr.K % DEPTH != 0;
         for (int s = first; s < last;) {
             // the next stage that is not full, or the end
-            const int stop = !ragged ? last : min(last, (PARTS == 2 && s + 2 >= stages_k ? 2 * stages_k : stages_k) - 1);
-            for (; s + 3 < stop; s += 2) {
-                stage(full, s, la0, lb0, la1, lb1);
-                stage(full, s + 1, la1, lb1, la0, lb0);
+            const int stop = !ragged ? last : min(last, (PARTS == 2 && s + BUFS >= stages_k ? 2 * stages_k : stages_k) - 1);
+            for (; s + 2 * BUFS - 1 < stop; s += BUFS) {
+                stage(full, s, at0);
+                stage(full, s + 1, at1);
+                if constexpr (BUFS == 4) {
+                    stage(full, s + 2, at2);
+                    stage(full, s + 3, at3);
+                }
             }
-            stage(any, s, la0, lb0, la1, lb1);
-            if (s + 1 < last) stage(any, s + 1, la1, lb1, la0, lb0);
-            s += 2;
+            stage(any, s, at0);
+            if (s + 1 < last) stage(any, s + 1, at1);
+            if constexpr (BUFS == 4) {
+                if (s + 2 < last) stage(any, s + 2, at2);
+                if (s + 3 < last) stage(any, s + 3, at3);
+            }
+            s += BUFS;
         }
     }
 
