@@ -160,11 +160,11 @@ struct tile_at {
     int m, n, problem, split;
 };
 
-__device__ inline tile_at find_tile(const product &pr)
+__device__ inline tile_at find_tile(const product &pr, int block)
 {
     const int tiles = pr.tiles_m * pr.tiles_n, total = tiles * pr.problems * pr.splits;
-    const int die = blockIdx.x % 8, share = total / 8, rest = total % 8;
-    int w = die * share + min(die, rest) + blockIdx.x / 8;
+    const int die = block % 8, share = total / 8, rest = total % 8;
+    int w = die * share + min(die, rest) + block / 8;
     tile_at t;
     t.problem = w / (tiles * pr.splits);
     w -= t.problem * tiles * pr.splits;
@@ -177,24 +177,22 @@ __device__ inline tile_at find_tile(const product &pr)
     return t;
 }
 
-// BUFS: stages that LDS holds.
+// Bytes of a stage of both operands in LDS.
+template <class T, int TM, int TN, int WAVES, bool ANEAR, bool BNEAR, bool PAIR>
+constexpr int STAGE_BYTES = stager<T, TM, WAVES, ANEAR, false>::BYTES + stager<T, TN, WAVES, BNEAR, PAIR>::BYTES;
+
+// The workgroup's tile of a launch's `block`th workgroup.  BUFS: stages that LDS holds, one in each of `lds`.
 template <class T, class EPI, int TM, int TN, int WM, int WN, int BUFS, bool ANEAR, bool BNEAR, int PARTS>
-__global__ __launch_bounds__(WM *WN *WAVE) void k_product(product pr, EPI epi)
+__device__ __forceinline__ void product_tile(const product &pr, const EPI &epi, int block, lds_byte *const (&lds)[4])
 {
     constexpr int WAVES = WM * WN, SUMS = EPI::SUMS;
     constexpr int FM = TM / WM / 16, FN = TN / WN / 16;  // fragments of a wave
-    static_assert(FN == 4);
+    static_assert(FN == 4 && (BUFS == 2 || BUFS == 4));
     using SA = stager<T, TM, WAVES, ANEAR, false>;
     using SB = stager<T, TN, WAVES, BNEAR, SUMS == 2>;
-    // separate arrays: the compiler must see that reads of one do not wait for copies into another
-    __shared__ __align__(16) char s0[SA::BYTES + SB::BYTES], s1[SA::BYTES + SB::BYTES];
-    __shared__ __align__(16) char s2[BUFS > 2 ? SA::BYTES + SB::BYTES : 16], s3[BUFS > 2 ? SA::BYTES + SB::BYTES : 16];
-    static_assert(BUFS == 2 || BUFS == 4);
-    lds_byte *const lds[4] = {(lds_byte *)s0, (lds_byte *)s1, (lds_byte *)s2, (lds_byte *)s3};
-
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int wm = wave / WN, wn = wave % WN;
-    const tile_at t = find_tile(pr);
+    const tile_at t = find_tile(pr, block);
     const int64_t m0 = (int64_t)t.m * TM, n0 = (int64_t)t.n * (TN / SUMS);
     const int stages_k = (int)((pr.K + DEPTH - 1) / DEPTH);
     const int first = t.split * pr.split_stages, last = min(stages_k * PARTS, first + pr.split_stages);
@@ -340,6 +338,19 @@ __global__ __launch_bounds__(WM *WN *WAVE) void k_product(product pr, EPI epi)
                 epi(t.problem * pr.splits + t.split, row, n0 + wn * 64 + unit * 32 + col8, v[unit]);
         }
     }
+}
+
+// The stages' buffers, as separate arrays: the compiler must see that reads of one do not wait for copies into another.
+#define RKB_STAGE_BUFFERS(BYTES, BUFS)                                                                                   \
+    __shared__ __align__(16) char s0[BYTES], s1[BYTES], s2[BUFS > 2 ? BYTES : 16], s3[BUFS > 2 ? BYTES : 16];            \
+    lds_byte *const lds[4] = {(lds_byte *)s0, (lds_byte *)s1, (lds_byte *)s2, (lds_byte *)s3}
+
+template <class T, class EPI, int TM, int TN, int WM, int WN, int BUFS, bool ANEAR, bool BNEAR, int PARTS>
+__global__ __launch_bounds__(WM *WN *WAVE) void k_product(product pr, EPI epi)
+{
+    constexpr int BYTES = STAGE_BYTES<T, TM, TN, WM * WN, ANEAR, BNEAR, EPI::SUMS == 2>;
+    RKB_STAGE_BUFFERS(BYTES, BUFS);
+    product_tile<T, EPI, TM, TN, WM, WN, BUFS, ANEAR, BNEAR, PARTS>(pr, epi, blockIdx.x, lds);
 }
 
 }  // namespace rkb
