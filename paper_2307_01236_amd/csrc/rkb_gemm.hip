@@ -35,6 +35,7 @@ template <class T>
 struct out_matrix {
     T *p;
     int64_t stride, rows, cols;
+    int64_t low = 0;  // distance to a second matrix that takes what rounding to T leaves over (0: none)
     // The same into rows whose columns go on to a multiple of 8: those past the end become 0.
     __device__ void put_padded(int64_t row, int64_t col, float (&v)[8]) const
     {
@@ -42,6 +43,11 @@ struct out_matrix {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = col + i < cols ? v[i] : 0.0f;
         store8<T>(p + row * stride + col, 8, v);
+        if (low) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] -= (float)(T)settled<T>(v[i]);
+            store8<T>(p + low + row * stride + col, 8, v);
+        }
     }
     __device__ void put(int64_t row, int64_t col, const float (&v)[8]) const
     {
@@ -118,7 +124,9 @@ struct epi_gated_fwd {
 };
 
 // dg = dh u act'(g) and du = dh act(g), rounded to T: they are operands of the next products, whose
-// matrix units take T; and h again where it is asked for.
+// matrix units take T, and over many of them the error comes to that of the results' own rounding.  Few of
+// them (FINE_ELEMENTS) need not average out: they go into the products with what the rounding left over.  And
+// h again where it is asked for.
 template <class T, int ACT>
 __device__ inline void gated_grads(const float (&g)[8], const float (&u)[8], const float (&d)[8], float (&dg)[8],
                                    float (&du)[8], float (&h)[8])
@@ -236,18 +244,18 @@ int run_product(const product &pr, const cut &c, const EPI &epi, hipStream_t st)
     return launch_product<T, ANEAR, BNEAR, PARTS, 256, 256, 2, 4, 2>(pr, c, epi, st);
 }
 
-// The two products of a backward pass in one launch: dx in the first `first` workgroups (they have the longer sums), the weight gradients
-// in the others.
-template <class T, class EPI, int BUFS>
+// The two products of a backward pass in one launch: dx in the first `first` workgroups (they have the longer sums), the weights'
+// gradients in the others.  FINE: dg and du come in two parts each.
+template <class T, class EPI, int BUFS, bool FINE>
 __global__ __launch_bounds__(512) void k_backward(product dx, EPI dx_epi, int first, product dw, epi_store<T> dw_epi)
 {
     constexpr int X = STAGE_BYTES<T, 128, 128, 8, true, false, false>, W = STAGE_BYTES<T, 128, 128, 8, false, false, false>;
     constexpr int BYTES = X > W ? X : W;
     RKB_STAGE_BUFFERS(BYTES, BUFS);
     if ((int)blockIdx.x < first)
-        product_tile<T, EPI, 128, 128, 4, 2, BUFS, true, false, 2>(dx, dx_epi, blockIdx.x, lds);
+        product_tile<T, EPI, 128, 128, 4, 2, BUFS, true, false, FINE ? 4 : 2>(dx, dx_epi, blockIdx.x, lds);
     else
-        product_tile<T, epi_store<T>, 128, 128, 4, 2, BUFS, false, false, 1>(dw, dw_epi, blockIdx.x - first, lds);
+        product_tile<T, epi_store<T>, 128, 128, 4, 2, BUFS, false, false, FINE ? 2 : 1>(dw, dw_epi, blockIdx.x - first, lds);
 }
 
 // The splits' partial sums, in their order.
@@ -322,7 +330,8 @@ pair_cut choose_pair(int64_t rows, int64_t d, int64_t f)
     return best;
 }
 
-template <class T>
+// Either product may be left out (no rows of output).
+template <class T, bool FINE>
 int run_pair(product dx, product dw, const pair_cut &c, void *scratch, const epi_store<T> &out_x, const epi_store<T> &out_w, hipStream_t st)
 {
     auto tiles = [](product &pr, int splits, int stages) {
@@ -332,7 +341,8 @@ int run_pair(product dx, product dw, const pair_cut &c, void *scratch, const epi
         pr.split_stages = (stages + splits - 1) / splits;
         return (int64_t)pr.tiles_m * pr.tiles_n * pr.problems * splits;
     };
-    const int64_t nx = tiles(dx, c.splits, (int)((dx.K + DEPTH - 1) / DEPTH) * 2), nw = tiles(dw, 1, (int)((dw.K + DEPTH - 1) / DEPTH));
+    const int64_t nx = tiles(dx, c.splits, (int)((dx.K + DEPTH - 1) / DEPTH) * (FINE ? 4 : 2)),
+                  nw = tiles(dw, 1, (int)((dw.K + DEPTH - 1) / DEPTH) * (FINE ? 2 : 1));
     if (nx + nw > MAX_TILES) return RKB_E_INVAL;
     auto go = [&](auto epi) {
         using EPI = decltype(epi);
@@ -340,9 +350,11 @@ int run_pair(product dx, product dw, const pair_cut &c, void *scratch, const epi
             hipLaunchKernelGGL(kernel, dim3((uint32_t)(nx + nw)), dim3(512), 0, st, dx, epi, (int)nx, dw, out_w);
             return launched();
         };
-        return c.bufs == 2 ? launch(k_backward<T, EPI, 2>) : launch(k_backward<T, EPI, 4>);
+        if constexpr (!FINE)
+            if (c.bufs == 4) return launch(k_backward<T, EPI, 4, false>);
+        return launch(k_backward<T, EPI, 2, FINE>);
     };
-    if (c.splits == 1) return go(out_x);
+    if (c.splits == 1 || nx == 0) return go(out_x);
     const int rc = go(epi_part{(float *)scratch, out_x.c[0].rows, out_x.c[0].cols, round_up(out_x.c[0].cols, 8)});
     return rc != RKB_OK ? rc : join<T>((const float *)scratch, c.splits, 1, out_x, st);
 }
@@ -649,7 +661,7 @@ extern "C" int rkb_weight_grad(int dtype, int64_t rows, int64_t n, int64_t k, co
     if (rc != RKB_OK) return rc;
     return with_type16(dtype, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        const product pr{{(const char *)a.p, nullptr}, {(const char *)b.p, nullptr}, a.stride, b.stride, b.stride, round_up(n, 8), round_up(k, 8), rows, 1};
+        const product pr{{(const char *)a.p}, {(const char *)b.p, nullptr}, a.stride, b.stride, b.stride, round_up(n, 8), round_up(k, 8), rows, 1};
         return store_product<T, false, false, 1>(pr, c, parts, epi_store<T>{{{(T *)dw, dw_stride, n, k}}}, st);
     });
 }
@@ -676,14 +688,19 @@ static cut sums_cut(int64_t rows, int64_t d, int64_t f) { return choose_cut(rows
 static cut dx_cut(int64_t rows, int64_t d, int64_t f) { return choose_cut(rows, d, f, 2, 1, 1, true); }
 static cut dw_cut(int64_t rows, int64_t d, int64_t f) { return choose_cut(f, d, rows, 1, 2, 1, false); }
 
+// Up to so many elements of dg go into the products in two parts: twice the products, of a size that is all latency.  At 1 x 64 x
+// 64 the gradients' errors are 1.0 of a rounding's instead of up to 1.8.
+constexpr int64_t FINE_ELEMENTS = 4096;
+
 // The backward's two products, one after the other or in one launch.
 struct backward_cut {
     cut x, w;
     pair_cut both;
-    bool together;
+    bool together, fine;
     backward_cut(int64_t rows, int64_t d, int64_t f) : x(dx_cut(rows, d, f)), w(dw_cut(rows, d, f)), both(choose_pair(rows, d, f))
     {
         together = both.us < x.us + w.us + LAUNCH;
+        fine = rows * f <= FINE_ELEMENTS;
     }
     size_t bytes(int64_t rows, int64_t d, int64_t f) const
     {
@@ -715,7 +732,7 @@ struct gated_operands {
     }
     product sums(int64_t rows, int64_t d, int64_t f) const  // g and u
     {
-        return product{{(const char *)x.p, nullptr}, {(const char *)wg.p, (const char *)wu.p}, x.stride, wg.stride, wu.stride, rows, f, d, 1};
+        return product{{(const char *)x.p}, {(const char *)wg.p, (const char *)wu.p}, x.stride, wg.stride, wu.stride, rows, f, d, 1};
     }
 };
 
@@ -755,7 +772,7 @@ extern "C" int rkb_gated_fwd(int dtype, int act, int keep, int64_t rows, int64_t
 extern "C" int rkb_gated_bwd_workspace(int dtype, int keep, int64_t rows, int64_t d, int64_t f, int aligned, size_t *bytes)
 {
     if (!bytes || !good_gated(dtype, RKB_SILU, keep, rows, d, f)) return RKB_E_INVAL;
-    *bytes = 2 * padded_bytes(rows, f) + (d % 8 || !aligned ? padded_bytes(rows, d) + 2 * padded_bytes(f, d) : 0) +
+    *bytes = (rows * f <= FINE_ELEMENTS ? 4 : 2) * padded_bytes(rows, f) + (d % 8 || !aligned ? padded_bytes(rows, d) + 2 * padded_bytes(f, d) : 0) +
              backward_cut(rows, d, f).bytes(rows, d, f);
     return RKB_OK;
 }
@@ -775,10 +792,12 @@ extern "C" int rkb_gated_bwd(int dtype, int act, int keep, int64_t rows, int64_t
     const hipStream_t st = (hipStream_t)stream;
     workspace_taker ws(workspace, ws_bytes);
     const int64_t ld = round_up(f, 8);
-    void *dg = ws.take(padded_bytes(rows, f)), *du = ws.take(padded_bytes(rows, f));
+    const backward_cut cuts(rows, d, f);
+    const size_t part = padded_bytes(rows, f);
+    char *dg = (char *)ws.take(part), *du = (char *)ws.take(part);  // and what their rounding left over, at the same distance
+    if (cuts.fine) ws.take(2 * part);
     gated_operands in{{x, x_stride, rows, d}, {wg, wg_stride, f, d}, {wu, wu_stride, f, d}};
     if (rows > 0) in.align(ws);
-    const backward_cut cuts(rows, d, f);
     void *parts = ws.take(cuts.bytes(rows, d, f));
     if (ws.at != workspace && !good_workspace(workspace)) return RKB_E_INVAL;
     if (!ws.fits()) return RKB_E_NOMEM;
@@ -786,7 +805,8 @@ extern "C" int rkb_gated_bwd(int dtype, int act, int keep, int64_t rows, int64_t
     if (rc != RKB_OK) return rc;
     return with_type16(dtype, [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        const out_matrix<T> og{(T *)dg, ld, rows, f}, ou{(T *)du, ld, rows, f}, oh{(T *)h, h_stride, rows, f};
+        const int64_t low = cuts.fine ? (int64_t)part : 0;  // 2 matrices of `part` bytes on, in elements of 2
+        const out_matrix<T> og{(T *)dg, ld, rows, f, low}, ou{(T *)du, ld, rows, f, low}, oh{(T *)h, h_stride, rows, f};
         if (rows > 0)
             rc = with_act(act, [&](auto a) {
                 if (keep == RKB_KEEP_NONE) {
@@ -803,11 +823,18 @@ extern "C" int rkb_gated_bwd(int dtype, int act, int keep, int64_t rows, int64_t
                 return with_kept(keep, go);
             });
         if (rc != RKB_OK) return rc;
-        const product px{{(const char *)dg, (const char *)du}, {(const char *)in.wg.p, (const char *)in.wu.p}, ld, in.wg.stride, in.wg.stride, rows, round_up(d, 8), f, 1};
-        const product pw{{(const char *)dg, (const char *)du}, {(const char *)in.x.p, nullptr}, ld, in.x.stride, in.x.stride, ld, round_up(d, 8), rows, 2};
-        const epi_store<T> ox{{{(T *)dx, dx_stride, rows, d}}}, ow{{{(T *)dwg, dw_stride, f, d}, {(T *)dwu, dw_stride, f, d}}};
         const bool want_x = dx && rows > 0;
-        if (want_x && dwg && cuts.together) return run_pair<T>(px, pw, cuts.both, parts, ox, ow, st);
+        const char *gl = dg + 2 * part, *ul = du + 2 * part;
+        product px{{dg, du, gl, ul}, {(const char *)in.wg.p, (const char *)in.wu.p}, ld, in.wg.stride, in.wg.stride, rows, round_up(d, 8), f, 1};
+        product pw{{dg, du}, {(const char *)in.x.p, nullptr}, ld, in.x.stride, in.x.stride, ld, round_up(d, 8), rows, 2};
+        const epi_store<T> ox{{{(T *)dx, dx_stride, rows, d}}}, ow{{{(T *)dwg, dw_stride, f, d}, {(T *)dwu, dw_stride, f, d}}};
+        if (cuts.fine) {
+            if (!want_x) px.M = 0;
+            if (!dwg) pw.M = 0;
+            pw.a[0] = dg, pw.a[1] = gl, pw.a[2] = du, pw.a[3] = ul;
+            return px.M || pw.M ? run_pair<T, true>(px, pw, cuts.both, parts, ox, ow, st) : RKB_OK;
+        }
+        if (want_x && dwg && cuts.together) return run_pair<T, false>(px, pw, cuts.both, parts, ox, ow, st);
         if (want_x) rc = store_product<T, true, false, 2>(px, cuts.x, parts, ox, st);
         if (rc == RKB_OK && dwg) rc = store_product<T, false, false, 1>(pw, cuts.w, parts, ow, st);
         return rc;

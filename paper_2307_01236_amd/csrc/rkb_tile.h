@@ -143,10 +143,13 @@ struct stager {
     }
 };
 
-// One launch: `problems` products a[i] b[0] of the same sizes, or the sum a[0] b[0] + a[1] b[1] (PARTS = 2), or a[0] b[0] and
-// a[0] b[1] side by side (an epilogue of two sums).  The operands of one kind share their stride.
+// One launch: `problems` products of the same sizes, each a sum over PARTS operand pairs.  Part p of problem i is
+//   a[PARTS i + p] b[0]   where weights' gradients are formed (B a row per k, as is A),
+//   a[p] b[p % 2]         where dx is (one problem),
+//   a[0] b[0] and a[0] b[1] side by side for an epilogue of two sums.
+// The operands of one kind share their stride.
 struct product {
-    const char *a[2], *b[2];
+    const char *a[4], *b[2];
     int64_t sa, sb, sb2;  // sb2: of b[1], where it differs (few rows only)
     int64_t M, N, K;
     int problems;
@@ -204,14 +207,16 @@ __device__ __forceinline__ void product_tile(const product &pr, const EPI &epi, 
     const int64_t a_row0 = (ANEAR ? m0 * pr.sa : m0) * 2, b_row0 = (BNEAR ? n0 * pr.sb : n0) * 2;
     const int64_t a_step = ANEAR ? 2 : pr.sa * 2, b_step = BNEAR ? 2 : pr.sb * 2;
 
-    // the operands of this workgroup's tile: of the first or only part, and of the second
-    const char *pa0 = pr.a[t.problem] + a_row0, *pa1 = pr.a[1] + a_row0;
-    const char *pb0 = pr.b[0] + b_row0, *pb1 = pr.b[1] + b_row0;
     auto copy = [&](auto full, int s, lds_byte *to) {
-        const bool second = PARTS == 2 && s >= stages_k;
-        const int k0 = (s - (second ? stages_k : 0)) * DEPTH, left = (int)pr.K - k0;
-        const char *pa = (second ? pa1 : pa0) + k0 * a_step, *pb = (second ? pb1 : pb0) + k0 * b_step;
-        const char *pu = pb1 + k0 * b_step;
+        const int part = PARTS == 1 ? 0 : PARTS == 2 ? s >= stages_k : s / stages_k;
+        const int k0 = (s - part * stages_k) * DEPTH, left = (int)pr.K - k0;
+        const char *pa = pr.a[0], *pb = pr.b[0], *pu = pr.b[1] + b_row0 + k0 * b_step;
+#pragma unroll
+        for (int i = 1; i < 4; ++i)  // by selection: a place in an array that is only known at run time would be loaded again
+            if (i < (ANEAR ? PARTS : 2 * PARTS) && i == (ANEAR ? part : PARTS * t.problem + part)) pa = pr.a[i];
+        if (ANEAR && !BNEAR && part % 2) pb = pr.b[1];
+        pa += a_row0 + k0 * a_step;
+        pb += b_row0 + k0 * b_step;
         sa.template copy<full()>(wave, lane, [&](int) { return pa; }, left, to);
         sb.template copy<full()>(wave, lane, [&](int piece) { return SUMS == 2 && piece / 4 % 2 ? pu : pb; }, left, to + SA::BYTES);
     };
@@ -295,7 +300,7 @@ __device__ __forceinline__ void product_tile(const product &pr, const EPI &epi, 
         const bool ragged = pr.K % DEPTH != 0;
         for (int s = first; s < last;) {
             // the next stage that is not full, or the end
-            const int stop = !ragged ? last : min(last, (PARTS == 2 && s + BUFS >= stages_k ? 2 * stages_k : stages_k) - 1);
+            const int stop = !ragged ? last : min(last, ((PARTS == 1 ? 0 : (s + BUFS) / stages_k) + 1) * stages_k - 1);
             for (; s + 2 * BUFS - 1 < stop; s += BUFS) {
                 stage(full, s, at0);
                 stage(full, s + 1, at1);

@@ -143,9 +143,10 @@ def gated_bounds(x, wg, wu, kind, dtype):
     return e + rounding(h, dtype), eg, eu
 
 
-def gated_grad_bounds(dh, x, wg, wu, kind, g, u, dtype, eg=0.0, eu=0.0):
-    """Bounds of dx, dwg, dwu and h for g and u that may be off by eg and eu (0: as given)."""
-    ud = ROUND[dtype][0]
+def gated_grad_bounds(dh, x, wg, wu, kind, g, u, dtype, eg=0.0, eu=0.0, fine=False):
+    """Bounds of dx, dwg, dwu and h for g and u that may be off by eg and eu (0: as given).  fine: dg and du
+    enter the products in two parts, and lose the square of a rounding only."""
+    ud = ROUND[dtype][0] ** (2 if fine else 1)
     dx, dwg, dwu, h = gated_grads(dh, x, wg, wu, kind, g, u)
     a, s = act(g, kind)
     ae = act_error(g, kind)

@@ -1,5 +1,6 @@
 """The block operators (paper_2307_01236_amd/block.py) on an MI355X against their 64-bit definitions,
 within the bounds that 32-bit sums and one rounding of each output allow (block_oracle)."""
+import ctypes
 import math
 
 import pytest
@@ -267,6 +268,43 @@ def test_gated(rows, width, hidden, act, dtype):
         for name, t, ref, e in zip(("dx", "dwg", "dwu", "h"), got, refs,
                                    bo.gated_grad_bounds(DH, X, G, U, act, g, u, dtype, *slack)):
             assert bo.worst(t, ref, e) <= 1.0, (keep, name)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("rows,width,hidden", [(1, 1, 1), (1, 64, 64), (3, 1000, 130), (40, 24, 96), (1, 96, 4096)])
+def test_gated_gradients_of_few_elements_round_once(rows, width, hidden, dtype):
+    """Up to 4096 elements of dg enter the products in two parts, so that only the results are rounded."""
+    x, wg, wu, dh = gated_inputs(rows, width, hidden, dtype)
+    args = (bo.d(dh), bo.d(x), bo.d(wg), bo.d(wu), "silu")
+    kept = bk.rkb_gated_fwd(x, wg, wu, keep="full")[1]
+    g, u = bo.d(kept[0]), bo.d(kept[1])
+    got = bk.rkb_gated_bwd(dh, x, wg, wu, kept=kept)
+    for t, ref, e in zip(got[:3], bo.gated_grads(*args, g, u), bo.gated_grad_bounds(*args, g, u, dtype, fine=True)):
+        assert bo.worst(t, ref, e) <= 1.0
+    assert all(torch.equal(p, q) for p, q in zip(got[:3], bk.rkb_gated_bwd(dh, x, wg, wu)[:3]))
+
+
+def test_gated_one_gradient_alone():
+    """dx or the weights' gradients left out at the C interface: the others are the same."""
+    lib = bk.load()
+    for rows, width, hidden in ((3, 64, 96), (300, 136, 264), (1500, 72, 520)):
+        x, wg, wu, dh = gated_inputs(rows, width, hidden, BF)
+        kept = bk.rkb_gated_fwd(x, wg, wu, keep="16bit")[1]
+        want = bk.rkb_gated_bwd(dh, x, wg, wu, kept=kept)
+        n = ctypes.c_size_t(0)
+        assert lib.rkb_gated_bwd_workspace(bk.RKB_BF16, bk.RKB_KEEP_16BIT, rows, width, hidden, 1, ctypes.byref(n)) == 0
+        ws = torch.empty(n.value, dtype=torch.uint8, device="cuda")
+        for only_dx in (True, False):
+            dx, dwg, dwu = (torch.zeros_like(t) for t in want[:3])
+            rc = lib.rkb_gated_bwd(bk.RKB_BF16, bk.RKB_SILU, bk.RKB_KEEP_16BIT, rows, width, hidden, dh.data_ptr(), hidden,
+                                   x.data_ptr(), width, wg.data_ptr(), width, wu.data_ptr(), width, kept[0].data_ptr(),
+                                   kept[1].data_ptr(), None, None, dx.data_ptr() if only_dx else None, width,
+                                   None if only_dx else dwg.data_ptr(), None if only_dx else dwu.data_ptr(), width, None, hidden,
+                                   ws.data_ptr(), n.value, torch.cuda.current_stream().cuda_stream)
+            assert rc == 0
+            close = lambda a, b: float((a.double() - b.double()).norm() / b.double().norm()) <= bo.ROUND[BF][0]  # noqa: E731
+            # by another cut of the sum the last bit may differ
+            assert close(dx, want[0]) if only_dx else close(dwg, want[1]) and close(dwu, want[2])
 
 
 def test_gated_far_ends_of_the_activation():
