@@ -10,18 +10,31 @@ namespace {
 
 // ------------------------------------------------------------------ activations
 
-// act(g) and act'(g).  1 / (1 + e^-g) is taken from e^-|g|, which cannot overflow.
+// act(g) and act'(g).  1 / (1 + e^-g) is taken from e^-|g|, which cannot overflow.  Phi(-y) for y >= 0 is e^(-y^2/2)
+// times a function that falls slowly from 1/2, here t P(t) with t = 1 / (1 + 0.3 y) and P of degree 7, fitted to the least largest
+// relative error over 0 <= y <= 14 (1.5e-7, and 4.3e-7 as evaluated in 32 bits).  It shares its exponential with the slope;
+// with the library's erfcf the forward of 5797 x 944 x 1040 took 41.8 us instead of 34.7.
 template <int ACT>
 __device__ inline void activate(float g, float &value, float &slope)
 {
     if constexpr (ACT == RKB_SILU) {
-        const float t = __expf(-fabsf(g)), s = (g >= 0.0f ? 1.0f : t) / (1.0f + t);
+        const float t = __expf(-fabsf(g)), s = (g >= 0.0f ? 1.0f : t) * __builtin_amdgcn_rcpf(1.0f + t);
         value = g * s;
         slope = s * (1.0f + g * (1.0f - s));
     } else {
-        const float below = 0.5f * erfcf(-0.70710678f * g);
+        const float e = __expf(-0.5f * g * g), t = __builtin_amdgcn_rcpf(1.0f + 0.3f * fabsf(g));
+        float p = 3.56748775e-02f;
+        p = p * t + -1.57203496e-01f;
+        p = p * t + 2.06354186e-01f;
+        p = p * t + -5.36842421e-02f;
+        p = p * t + 1.28561929e-01f;
+        p = p * t + 9.99134108e-02f;
+        p = p * t + 1.20753966e-01f;
+        p = p * t + 1.19629301e-01f;
+        p *= e * t;
+        const float below = g < 0.0f ? p : 1.0f - p;
         value = g * below;
-        slope = below + 0.39894228f * g * __expf(-0.5f * g * g);
+        slope = below + 0.39894228f * g * e;
     }
 }
 
@@ -274,7 +287,7 @@ __global__ __launch_bounds__(256) void k_join(const float *__restrict__ parts, i
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] += w[e];
         }
-        const int64_t row = i / chunks;
+        const int64_t row = all >> 32 ? i / chunks : (uint32_t)i / (uint32_t)chunks;  // 64-bit division is slow
         c.put(row, (i - row * chunks) * 8, v);
     }
 }
@@ -513,7 +526,7 @@ __global__ __launch_bounds__(256) void k_pad(pad_jobs jobs)
     const pad_job j = jobs.job[blockIdx.y];
     const int64_t all = j.rows * j.chunks;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / j.chunks;
+        const int64_t r = all >> 32 ? i / j.chunks : (uint32_t)i / (uint32_t)j.chunks;  // 64-bit division is slow
         const int c = (int)(i - r * j.chunks) * 8, left = j.cols - c;
         const uint16_t *from = j.from + r * j.stride + c;
         vec<uint16_t, 8> v;

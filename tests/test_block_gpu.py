@@ -96,6 +96,29 @@ def test_layer_norm_far_from_zero_and_flat_rows():
     assert bool((y[1:3] == 0).all()) and math.isclose(float(rstd[2]), 1e-5 ** -0.5, rel_tol=1e-6)
 
 
+def test_layer_norm_with_pointers_left_out():
+    """At the C interface: no statistics, a bias without a weight, one of dw and db alone."""
+    lib, st = bk.load(), torch.cuda.current_stream().cuda_stream
+    x, dy, b = rand(70, 130, dtype=HF), rand(70, 130, seed=1, dtype=HF), rand(130, seed=2, dtype=HF)
+    want, mean, rstd = bk.rkb_layer_norm_fwd(x, None, b)
+    y = torch.empty_like(x)
+    assert lib.rkb_layer_norm_fwd(bk.RKB_F16, bk.RKB_F16, 70, 130, x.data_ptr(), 130, None, b.data_ptr(), 1e-5, y.data_ptr(), 130,
+                                  None, None, st) == 0
+    assert torch.equal(y, want)
+    _, dw, db = bk.rkb_layer_norm_bwd(dy, x, mean, rstd, torch.ones_like(b), bias=True)
+    n = ctypes.c_size_t(0)
+    assert lib.rkb_layer_norm_bwd_workspace(bk.RKB_F16, 70, 130, ctypes.byref(n)) == 0
+    ws = torch.empty(n.value, dtype=torch.uint8, device="cuda")
+    for which in (0, 1):
+        out = [torch.zeros_like(b), torch.zeros_like(b)]
+        ptrs = [None, None]
+        ptrs[which] = out[which].data_ptr()
+        assert lib.rkb_layer_norm_bwd(bk.RKB_F16, bk.RKB_F16, 70, 130, dy.data_ptr(), 130, x.data_ptr(), 130, None, None,
+                                      mean.data_ptr(), rstd.data_ptr(), None, y.data_ptr(), 130, *ptrs, ws.data_ptr(), n.value,
+                                      st) == 0
+        assert torch.equal(out[which], (dw, db)[which]) and not out[1 - which].any()
+
+
 def test_layer_norm_keeps_a_bad_row_to_itself():
     x, dy, w = rand(9, 300, dtype=HF), rand(9, 300, seed=1, dtype=HF), rand(300, seed=2, dtype=HF)
     clean = bk.rkb_layer_norm_fwd(x, w)
