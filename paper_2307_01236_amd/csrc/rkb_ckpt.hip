@@ -57,13 +57,12 @@ __global__ __launch_bounds__(CKPT_BLOCK) void k_ckpt_save(span_map m, const T *_
         const float most = __uint_as_float(top);
         const bool ok = finite(most);
         const int e = ok ? step_exp(most) : 0;
-        const float inv = ok ? two_to(-e) : 0.0f, limit = e > CODE_TOP_EXP<T> ? 63.0f : 127.0f;
-        vec<int8_t, SPAN> q;
+        float flat[SPAN];
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int i = 0; i < N; ++i) q[k * N + i] = ok ? (int8_t)code_of(v[k][i], inv, limit) : (int8_t)0;
-        *(vec<int8_t, SPAN> *)(codes + row * m.ld + col) = q;
+            for (int i = 0; i < N; ++i) flat[k * N + i] = ok ? v[k][i] : 0.0f;
+        *(vec<uint32_t, SPAN / 4> *)(codes + row * m.ld + col) = codes_of<SPAN>(flat, two_to(-e), e > CODE_TOP_EXP<T>);
         if (col % GROUP == 0) exps[row * (m.ld / GROUP) + col / GROUP] = ok ? (uint8_t)(e + 127) : (uint8_t)255;
     }
 }

@@ -134,9 +134,26 @@ __device__ inline uint32_t max_bits(uint32_t a, float b)
     return max(a, __float_as_uint(b) & 0x7fffffffu);
 }
 
-__device__ inline int code_of(float x, float inv_step, float limit)
+// Codes of N values of one group: round-half-even(x * 2^-e).  Scaling by a power of two is exact, and adding 1.5 * 2^23
+// rounds to a whole number whose low byte is the code, so one instruction does both.  A value is at most 127 steps by
+// the choice of e; only where the type's range ends (`top`: 64 steps would pass it) is it limited to 63.
+template <int N>
+__device__ inline vec<uint32_t, N / 4> codes_of(const float (&x)[N], float inv_step, bool top)
 {
-    return (int)fminf(fmaxf(rintf(x * inv_step), -limit), limit);
+    vec<uint32_t, N / 4> q;
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        uint32_t b[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float v = x[i + j];
+            if (top) v = fminf(fmaxf(v, -63.0f / inv_step), 63.0f / inv_step);
+            b[j] = __float_as_uint(__builtin_fmaf(v, inv_step, 12582912.0f));
+        }
+        const uint32_t lo = __builtin_amdgcn_perm(b[1], b[0], 0x0c0c0400), hi = __builtin_amdgcn_perm(b[3], b[2], 0x0c0c0400);
+        q[i / 4] = __builtin_amdgcn_perm(hi, lo, 0x05040100);
+    }
+    return q;
 }
 
 // The value that stands for a group's stored exponent byte: its step, or NaN.

@@ -82,11 +82,10 @@ __device__ inline void put_codes(int64_t row, int64_t col, int64_t rows, int64_t
     const float most = __uint_as_float(top);
     const bool ok = finite(most);
     const int e = ok ? step_exp(most) : 0;
-    const float inv = ok ? two_to(-e) : 0.0f, limit = e > CODE_TOP_EXP<float> ? 63.0f : 127.0f;
-    vec<int8_t, 8> q;
+    float x[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = ok && col + i < cols ? (int8_t)code_of(v[i], inv, limit) : (int8_t)0;
-    *(vec<int8_t, 8> *)(codes + row * ld + col) = q;
+    for (int i = 0; i < 8; ++i) x[i] = ok && col + i < cols ? v[i] : 0.0f;
+    *(vec<uint32_t, 2> *)(codes + row * ld + col) = codes_of<8>(x, two_to(-e), e > CODE_TOP_EXP<float>);
     if (col % GROUP == 0) exps[row * (ld / GROUP) + col / GROUP] = ok ? (uint8_t)(e + 127) : (uint8_t)255;
 }
 

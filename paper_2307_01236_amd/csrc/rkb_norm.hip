@@ -173,7 +173,8 @@ __global__ __launch_bounds__(BLOCK) void k_norm_bwd(int64_t rows, int cols, cons
 {
     constexpr int N = CHUNK<T>, ROWS = BLOCK / LANES;
     __shared__ typename row_sums<LANES, BLOCK, 2>::place part;
-    __shared__ float joined[ROWS > 1 ? LANES * NV * N : 1];
+    constexpr int SLOTS = BLOCK / (LANES < WAVE ? WAVE : LANES);  // rows that are joined through LDS
+    __shared__ __align__(16) float joined[SLOTS > 1 ? SLOTS : 1][SLOTS > 1 ? LANES * NV * N : 4];
     row_sums<LANES, BLOCK, 2> sum(part);
     const int lane = threadIdx.x % LANES;
     const float n = (float)cols;
@@ -237,8 +238,7 @@ __global__ __launch_bounds__(BLOCK) void k_norm_bwd(int64_t rows, int cols, cons
         }
     }
     if (!sums) return;
-    // join the rows of a wave, then the block's waves one after the other, and write the block's partial sums
-    constexpr int SLOTS = BLOCK / (LANES < WAVE ? WAVE : LANES);
+    // join the rows of a wave, then the block's waves in their order, and write the block's partial sums
     if constexpr (LANES < WAVE) {
 #pragma unroll
         for (int d = LANES; d < WAVE; d *= 2)
@@ -254,24 +254,23 @@ __global__ __launch_bounds__(BLOCK) void k_norm_bwd(int64_t rows, int cols, cons
 #pragma unroll
     for (int which = 0; which < 2; ++which) {
         if constexpr (SLOTS > 1) {
-            const bool first_row = LANES >= WAVE || threadIdx.x % WAVE < LANES;
-            for (int t = 0; t < SLOTS; ++t) {
-                __syncthreads();
-                if ((int)threadIdx.x / (BLOCK / SLOTS) == t && first_row) {
+            if (which) __syncthreads();
+            if (LANES >= WAVE || threadIdx.x % WAVE < LANES) {
+                float *mine = joined[threadIdx.x / (BLOCK / SLOTS)];
 #pragma unroll
-                    for (int k = 0; k < NV; ++k)
+                for (int k = 0; k < NV; ++k)
 #pragma unroll
-                        for (int i = 0; i < N; ++i) {
-                            float *j = &joined[(k * N + i) * LANES + lane];
-                            const float mine = which ? db[k][i] : dw[k][i];
-                            *j = t ? *j + mine : mine;
-                        }
-                }
+                    for (int i = 0; i < N; i += 4)
+                        *(f32x4 *)&mine[(k * LANES + lane) * N + i] =
+                            which ? f32x4{db[k][i], db[k][i + 1], db[k][i + 2], db[k][i + 3]}
+                                  : f32x4{dw[k][i], dw[k][i + 1], dw[k][i + 2], dw[k][i + 3]};
             }
             __syncthreads();
             for (int c = threadIdx.x; c < cols; c += BLOCK) {
-                const int k = c / (LANES * N), l = c / N % LANES, i = c % N;
-                out[which * cols + c] = joined[(k * N + i) * LANES + l];
+                float all = joined[0][c];
+#pragma unroll
+                for (int t = 1; t < SLOTS; ++t) all += joined[t][c];
+                out[which * cols + c] = all;
             }
         } else {
 #pragma unroll
