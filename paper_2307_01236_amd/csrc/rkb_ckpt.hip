@@ -52,7 +52,7 @@ __global__ __launch_bounds__(CKPT_BLOCK) void k_ckpt_save(span_map m, const T *_
             for (int i = 0; i < N; ++i) top = max_bits(top, v[k][i]);
         }
         // spans come in pairs (a code row is whole groups), and a pair in neighbouring lanes
-        top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+        top = max(top, dpp<DPP_XOR1>(top));
         if (!live) continue;
         const float most = __uint_as_float(top);
         const bool ok = finite(most);

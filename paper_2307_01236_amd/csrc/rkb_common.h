@@ -162,13 +162,42 @@ __device__ inline float step_of(uint8_t exp_byte)
     return exp_byte == 255 ? __uint_as_float(0x7fc00000u) : two_to((int)exp_byte - 127);
 }
 
-// Sum over groups of LANES neighbouring lanes (LANES a power of two up to 64), in every lane.
+// Exchanges between lanes in vector instructions (an exchange through LDS takes some hundred cycles).  Each leaves both partners
+// with the same pair.
+template <int CTRL>
+__device__ inline uint32_t dpp(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+}
+constexpr int DPP_XOR1 = 0xb1, DPP_XOR2 = 0x4e;      // quad permutations
+constexpr int DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140;  // of 8 and of 16 lanes
+
+// Sum over groups of LANES (16 or 64) neighbouring lanes, in every lane and the same bits in each.
 template <int LANES>
 __device__ inline float lane_sum(float v)
 {
-#pragma unroll
-    for (int d = 1; d < LANES; d *= 2) v += __shfl_xor(v, d);
+    static_assert(LANES == 16 || LANES == 64);
+    auto f = [](uint32_t u) { return __uint_as_float(u); };
+    v += f(dpp<DPP_XOR1>(__float_as_uint(v)));
+    v += f(dpp<DPP_XOR2>(__float_as_uint(v)));
+    v += f(dpp<DPP_HALF_MIRROR>(__float_as_uint(v)));
+    v += f(dpp<DPP_MIRROR>(__float_as_uint(v)));
+    if constexpr (LANES == 64) {
+        const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(a[0]) + f(a[1]);
+        const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(b[0]) + f(b[1]);
+    }
     return v;
+}
+
+// Maximum over the lanes l, l + 16, l + 32 and l + 48, in each.
+__device__ inline uint32_t max_of_rows(uint32_t v)
+{
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = max((uint32_t)a[0], (uint32_t)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return max((uint32_t)b[0], (uint32_t)b[1]);
 }
 
 inline bool good_dtype(int dtype) { return dtype == RKB_F32 || dtype == RKB_F16 || dtype == RKB_BF16; }

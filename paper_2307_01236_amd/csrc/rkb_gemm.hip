@@ -75,8 +75,7 @@ __device__ inline void put_codes(int64_t row, int64_t col, int64_t rows, int64_t
     uint32_t top = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) top = max_bits(top, col + i < cols ? v[i] : 0.0f);
-    top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+    top = max_of_rows(top);
     const int64_t ld = (cols + GROUP - 1) / GROUP * GROUP;
     if (row >= rows || col >= ld) return;
     const float most = __uint_as_float(top);
