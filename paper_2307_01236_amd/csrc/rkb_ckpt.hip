@@ -61,8 +61,8 @@ __global__ __launch_bounds__(CKPT_BLOCK) void k_ckpt_save(span_map m, const T *_
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
-            for (int i = 0; i < N; ++i) flat[k * N + i] = ok ? v[k][i] : 0.0f;
-        *(vec<uint32_t, SPAN / 4> *)(codes + row * m.ld + col) = codes_of<SPAN>(flat, two_to(-e), e > CODE_TOP_EXP<T>);
+            for (int i = 0; i < N; ++i) flat[k * N + i] = v[k][i];
+        *(vec<uint32_t, SPAN / 4> *)(codes + row * m.ld + col) = codes_of<SPAN>(flat, ok ? two_to(-e) : 0.0f, e > CODE_TOP_EXP<T>);
         if (col % GROUP == 0) exps[row * (m.ld / GROUP) + col / GROUP] = ok ? (uint8_t)(e + 127) : (uint8_t)255;
     }
 }

@@ -53,8 +53,9 @@ struct out_matrix {
     __device__ void put_padded(int64_t row, int64_t col, float (&v)[8]) const
     {
         if (row >= rows || col >= cols) return;
+        const int left = (int)min(cols - col, (int64_t)8);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = col + i < cols ? v[i] : 0.0f;
+        for (int i = 0; i < 8; ++i) v[i] = i < left ? v[i] : 0.0f;
         store8<T>(p + row * stride + col, 8, v);
         if (low) {
 #pragma unroll
@@ -72,19 +73,21 @@ struct out_matrix {
 __device__ inline void put_codes(int64_t row, int64_t col, int64_t rows, int64_t cols, int8_t *codes, uint8_t *exps,
                                  const float (&v)[8])
 {
+    const int left = (int)min(cols - col, (int64_t)8);
+    float x[8];
     uint32_t top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max_bits(top, col + i < cols ? v[i] : 0.0f);
+    for (int i = 0; i < 8; ++i) {
+        x[i] = i < left ? v[i] : 0.0f;
+        top = max_bits(top, x[i]);
+    }
     top = max_of_rows(top);
     const int64_t ld = (cols + GROUP - 1) / GROUP * GROUP;
     if (row >= rows || col >= ld) return;
     const float most = __uint_as_float(top);
     const bool ok = finite(most);
     const int e = ok ? step_exp(most) : 0;
-    float x[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = ok && col + i < cols ? v[i] : 0.0f;
-    *(vec<uint32_t, 2> *)(codes + row * ld + col) = codes_of<8>(x, two_to(-e), e > CODE_TOP_EXP<float>);
+    *(vec<uint32_t, 2> *)(codes + row * ld + col) = codes_of<8>(x, ok ? two_to(-e) : 0.0f, e > CODE_TOP_EXP<float>);
     if (col % GROUP == 0) exps[row * (ld / GROUP) + col / GROUP] = ok ? (uint8_t)(e + 127) : (uint8_t)255;
 }
 
