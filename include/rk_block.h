@@ -85,8 +85,8 @@ int rkb_layer_norm_bwd(int dtype, int wdtype, int64_t rows, int64_t cols, const 
  * power of two with max|x| <= 127 * 2^e (e >= -126); a value is kept as the whole number
  * q = round-half-even(x 2^-e), |q| <= 127 (63 where 64 * 2^e would pass dtype's largest
  * finite value), and stands for q * 2^e, which every dtype holds exactly where x's type held x.
- * So |x - q 2^e| <= 2^(e-1) < max|x| / 127 for e > -126 (below 2^e where 63 limits).  A group with an infinity or NaN stands for NaN as a whole, so that such a
- * value still reaches the gradients.
+ * So |x - q 2^e| <= 2^(e-1) < max|x| / 127 for e > -126 (below 2^e where 63 limits).  A group with an infinity or NaN stands for NaN as a whole, whatever
+ * its codes, so that such a value still reaches the gradients.
  *   codes [rows, ld] with ld = cols rounded up to RKB_GROUP (the rest zero), 16-byte aligned
  *   exps  [rows, ld / RKB_GROUP]: e + 127, or 255 for NaN
  */

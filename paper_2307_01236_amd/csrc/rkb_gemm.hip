@@ -401,7 +401,7 @@ __global__ __launch_bounds__(FEW_WAVES *WAVE) void k_few(product pr, EPI epi)
 {
     constexpr int F = 2 * NB;  // fragments of weights
     __shared__ f32x4 part[FEW_WAVES][MT][F][WAVE];
-    const int lane = threadIdx.x % WAVE, wave = threadIdx.x / WAVE, r = lane % 16, q = lane / 16;
+    const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE), r = lane % 16, q = lane / 16;
     const int64_t n0 = (int64_t)blockIdx.x * (16 * NB);
     const int K = (int)pr.K, steps = (K + 31) / 32, each = (steps + FEW_WAVES - 1) / FEW_WAVES;
     const int first = wave * each, last = min(steps, first + each);
@@ -416,11 +416,25 @@ __global__ __launch_bounds__(FEW_WAVES *WAVE) void k_few(product pr, EPI epi)
     auto load = [&](int at, int s) {  // steps from s on, past the share's end as zeros
 #pragma unroll
         for (int i = 0; i < FEW_STEPS; ++i) {
-            const int k = (s + i) * 32, left = s + i < last ? K - k - q * 8 : 0;
+            if (s + i >= last) {
 #pragma unroll
-            for (int f = 0; f < F; ++f) fw[at][i][f] = load_frag(w[f] + k, left);
+                for (int f = 0; f < F; ++f) fw[at][i][f] = frag<T>{};
 #pragma unroll
-            for (int m = 0; m < MT; ++m) fx[at][i][m] = load_frag(x[m] + k, left);
+                for (int m = 0; m < MT; ++m) fx[at][i][m] = frag<T>{};
+                continue;
+            }
+            const int k = (s + i) * 32, left = K - k - q * 8;
+            if (K - k >= 32) {
+#pragma unroll
+                for (int f = 0; f < F; ++f) __builtin_memcpy(&fw[at][i][f], w[f] + k, 16);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) __builtin_memcpy(&fx[at][i][m], x[m] + k, 16);
+            } else {
+#pragma unroll
+                for (int f = 0; f < F; ++f) fw[at][i][f] = load_frag(w[f] + k, left);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) fx[at][i][m] = load_frag(x[m] + k, left);
+            }
         }
     };
     auto multiply = [&](int at) {
@@ -462,14 +476,14 @@ __global__ __launch_bounds__(FEW_WAVES *WAVE) void k_few(product pr, EPI epi)
 constexpr int FEW_ROWS = 64;
 
 // Whether the few-rows form is expected to beat tiles that take `tiles_us`.  Weights come at the rate of a large read, and
-// with the rows that every workgroup reads again (from L2) at 7.3 TB/s in all, after 3 us of start and end.  At 1024 x 4096, 1
-// and 64 rows take 6.2 and 10.5 us (tiles: 9.7, 10.9); at 4096 x 11264, 33 and 75 (tiles: 41, 43).  What is kept
-// has no say: h, and g and u made again, are the same bits in every form.
+// with the rows that every workgroup reads again (from L2) at 7.3 TB/s in all, after 2.2 us of start and end.  At 1024 x 4096 one
+// row takes 5.2 us and 64 take 9.1 (tiles: 9.4), at 4096 x 4096 14.5 and 26 (26), at 4096 x 11264 33 and 75 (30).  What is
+// kept has no say: h, and g and u made again, are the same bits in every form.
 bool few_rows_win(int64_t M, int64_t N, int64_t K, double tiles_us)
 {
     if (M > FEW_ROWS) return false;
     const double weights = 4.0 * N * K, again = (double)((N + 15) / 16) * M * K * 2.0;
-    return 3.0 + std::max(weights / 5.5e6, (weights + again) / 7.3e6) < tiles_us;
+    return 2.2 + std::max(weights / 5.5e6, (weights + again) / 7.3e6) < tiles_us;
 }
 
 template <class T, int NB, class EPI>
