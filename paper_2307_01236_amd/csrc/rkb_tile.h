@@ -13,6 +13,10 @@
 //   a row per k: rows that a transposing read takes together (k, k+1, k+2, k+3 and the
 //     same 8 further on) lie in different pieces, each 32 bytes longer than it is full, which puts them
 //     into different banks and leaves every fragment's place a constant offset.
+//
+// Bound by the matrix units, whose clock falls with the operands' bits: 256 x 256 tiles reach 1.45 PFLOP/s at
+// 8192 x 4096 x 8192 (bf16, random operands; 1.83 on zeros), 1.36 at 4096 x 4096 x 4096, and 1.26 and 1.35 at 8192 x 11264 x
+// 4096 and 11264 x 4096 x 8192, whose tiles fill 5.5 rounds of workgroups.  A tile's start and end cost about 5 us.
 #pragma once
 #include <type_traits>
 
