@@ -42,7 +42,8 @@ extern "C" {
 
 enum {
     RKB_OK = 0,
-    RKB_E_INVAL = -1,   /* bad argument (NULL, negative, out of range, misaligned)      */
+    RKB_E_INVAL = -1,   /* bad argument (NULL, negative, out of range, misaligned), or a
+                           product of more than 2^22 tiles (128 x 128 at least)         */
     RKB_E_NOMEM = -3,   /* workspace too small                                          */
     RKB_E_DEVICE = -4   /* a HIP call failed (no device, launch error, ...)             */
 };

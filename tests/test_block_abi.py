@@ -98,6 +98,14 @@ def test_short_workspaces_are_refused():
     assert lib.rkb_gated_bwd_workspace(bk.RKB_F16, 5, 4, 64, 32, 1, C.byref(n)) == bk.RKB_E_INVAL
 
 
+def test_too_many_tiles_are_refused():
+    big = {**FWD, "rows": 1 << 30, "f": 1 << 20, "hs": 1 << 20, "keep": 0, "g": None, "u": None, "ge": None, "ue": None}
+    assert bk.load().rkb_gated_fwd(*big.values()) == bk.RKB_E_INVAL
+    big = {**WGRAD, "n": 1 << 24, "k": 1 << 24, "dys": 1 << 21, "xs": 1 << 21, "dws": 1 << 24, "x": P, "codes": None, "exps": None,
+           "wsb": 1 << 62}
+    assert bk.load().rkb_weight_grad(*big.values()) == bk.RKB_E_INVAL
+
+
 def test_no_rows_need_no_pointers():
     """Nothing to compute and nothing to clear: no device call is made."""
     none = dict(x=None, y=None, h=None, codes=None, exps=None, mean=None, rstd=None, w=None, b=None, rows=0)
