@@ -236,6 +236,19 @@ def test_weight_grad(rows, n, k, form, dtype):
     assert bo.worst(got, ref, bound) <= 1.0
 
 
+@pytest.mark.parametrize("rows,n,k", [(1024, 22528, 4096), (1024, 22533, 4096)])
+def test_weight_grad_of_many_tiles(rows, n, k):
+    """Several rounds of large tiles, the last one part empty; element by element."""
+    gen = torch.Generator(device="cuda").manual_seed(6)
+    dy, x = (torch.randn(rows, c, generator=gen, device="cuda").to(BF) for c in (n, k))
+    got = bk.rkb_weight_grad(dy, x)
+    for at in range(0, n, 4096):  # rows of dw, a few at a time in 64 bits
+        ref = torch.mm(dy[:, at:at + 4096].t().double().contiguous(), x.double())
+        bound = (rows + 8) * bo.U32 * torch.mm(dy[:, at:at + 4096].t().abs().double().contiguous(), x.abs().double()) \
+            + ref.abs() * bo.ROUND[BF][0]
+        assert float(((got[at:at + 4096].double() - ref).abs() / bound).max()) <= 1.0
+
+
 def test_weight_grad_of_rows_apart():
     dy, x = rand(300, 72, dtype=BF), rand(300, 136, seed=1, dtype=BF)
     want = bk.rkb_weight_grad(dy, x)
