@@ -3,6 +3,7 @@
 #include <algorithm>
 #include <type_traits>
 
+#include "rkb_cut.h"
 #include "rkb_tile.h"
 
 namespace rkb {
@@ -174,59 +175,10 @@ struct epi_gated_bwd {
 };
 
 constexpr size_t WS_ALIGN = 256;
-constexpr int64_t MAX_TILES = (int64_t)1 << 22;  // workgroups of a launch: 512 threads of each in 32 bits
 
 // ------------------------------------------------------------------ products
 
-// How a product is cut: the tile, its buffers, and how many workgroups share the stages of one tile (splits).
-struct cut {
-    int tm, tn, bufs, splits;
-    double us;  // what the choice expects it to take
-};
-
-// The tiles, with the microseconds of one stage in a workgroup that runs nearly alone and on a full chip
-// (where the clock is lower and L2 shared), and of a tile's start and end, fitted to measured products
-// of 64 to 8192 rows (bf16).  Small tiles pay more per product and fill the chip sooner: at 8192 x 4096 x 11264 the
-// gated forward takes 1140 us by 256 x 256, 1237 by 192 x 256 and 1368 by 128 x 128; at 1024 x 1280 x 5120 it takes
-// 36.7, 30.7 and 36.4; at 512 x 1024 x 4096, 27.3, 22.0 and 12.2.  Four buffers hide the latency of copies where a compute
-// unit has one workgroup: 128 x 4096 x 4096 takes 26.8 us with them and 40.0 with two, 1024 x 1280 x 5120
-// 36.7 and 36.4.
-struct tile_kind {
-    int tm, tn, bufs, slots;  // slots: workgroups that 256 compute units hold at once
-    double alone, busy, ends;
-};
-constexpr tile_kind TILES[] = {
-    {256, 256, 2, 256, 1.05, 1.68, 5.0},
-    {192, 256, 2, 256, 0.82, 1.29, 4.5},
-    {128, 128, 2, 512, 0.49, 0.95, 2.5},
-    {128, 128, 4, 256, 0.36, 0.48, 3.5},
-};
-constexpr double JOIN_FIXED = 4.0, JOIN_BYTES = 4.5e6;  // microseconds, bytes a microsecond
-constexpr double LAUNCH = 6.0;                          // a launch more, from the end of the work before it
-
-// The cut that these figures expect to be fastest.  Splits share a long K among workgroups where the tiles alone do
-// not fill the chip, at the price of 32-bit partial sums written and read once: dw of 512 x 512 over 16384
-// rows takes 174 us whole and 25 in 16 splits, of 2048 x 2048 over 2048 rows 28 whole and 34 in 2.
-cut choose_cut(int64_t M, int64_t N, int64_t K, int parts, int problems, int sums, bool near)
-{
-    const int64_t stages = std::max<int64_t>(1, (K + DEPTH - 1) / DEPTH * parts);
-    cut best{256, 256, 2, 1, 1e30};
-    for (const tile_kind &t : TILES) {
-        if (t.tm == 192 && !near) continue;
-        const int64_t tiles = (M + t.tm - 1) / t.tm * ((N + t.tn / sums - 1) / (t.tn / sums)) * problems;
-        for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-            if (splits > 1 && (sums == 2 || splits * 4 > stages || splits * tiles > 2 * t.slots)) break;
-            const int64_t groups = tiles * splits, rounds = groups / t.slots, rest = groups % t.slots;
-            const double each = (double)((stages + splits - 1) / splits);
-            double us = rounds * (each * t.busy + t.ends);
-            if (rest) us += each * (t.alone + (t.busy - t.alone) * rest / t.slots) + t.ends;
-            if (splits > 1) us += JOIN_FIXED + 2.0 * 4.0 * splits * problems * (double)M * N / JOIN_BYTES;
-            if (us < best.us) best = cut{t.tm, t.tn, t.bufs, splits, us};
-        }
-    }
-    return best;
-}
-
+// Bytes of a cut's partial sums.
 size_t split_bytes(const cut &c, int64_t M, int64_t N, int problems)
 {
     return c.splits == 1 ? 0 : (size_t)round_up((int64_t)c.splits * problems * M * round_up(N, 8) * 4, WS_ALIGN);
@@ -310,38 +262,6 @@ int store_product(const product &pr, const cut &c, void *scratch, const epi_stor
     const int64_t rows = out.c[0].rows, cols = out.c[0].cols, ld = round_up(cols, 8);
     const int rc = run_product<T, ANEAR, BNEAR, PARTS>(pr, c, epi_part{(float *)scratch, rows, cols, ld}, st);
     return rc != RKB_OK ? rc : join<T>((const float *)scratch, c.splits, pr.problems, out, st);
-}
-
-// How dx (in `splits`) and the weight gradients go in one launch of 128 x 128 tiles, and what it is expected to take.  Together they
-// fill the chip where each alone does not, and a launch is saved: the backward from 8-bit checkpoints takes 14 us
-// instead of 20 at 128 x 512 x 856, 36 instead of 43 at 512 x 1024 x 4096, 165 instead of 180 at 3000 x 1500 x 3000;
-// at 2048 x 2048 x 2048 87 instead of 85.
-struct pair_cut {
-    int bufs, splits;
-    double us;
-};
-
-pair_cut choose_pair(int64_t rows, int64_t d, int64_t f)
-{
-    const int64_t tiles_x = (rows + 127) / 128 * ((d + 127) / 128), tiles_w = 2 * ((f + 127) / 128) * ((d + 127) / 128);
-    const int64_t stages_x = (f + DEPTH - 1) / DEPTH * 2, each_w = (rows + DEPTH - 1) / DEPTH;
-    pair_cut best{2, 1, 1e30};
-    for (const tile_kind &t : TILES) {
-        if (t.tm != 128) continue;
-        for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-            if (splits > 1 && splits * 4 > stages_x) break;
-            const int64_t each_x = (stages_x + splits - 1) / splits, groups = tiles_x * splits + tiles_w;
-            const double longest = (double)std::max(each_x, each_w);
-            double us;
-            if (groups <= t.slots)
-                us = longest * (t.alone + (t.busy - t.alone) * groups / t.slots) + t.ends;
-            else
-                us = ((double)(tiles_x * splits * each_x + tiles_w * each_w) * t.busy + groups * t.ends) / t.slots + 0.2 * longest * t.busy;
-            if (splits > 1) us += JOIN_FIXED + 2.0 * 4.0 * splits * (double)rows * d / JOIN_BYTES;
-            if (us < best.us) best = pair_cut{t.bufs, splits, us};
-        }
-    }
-    return best;
 }
 
 // Either product may be left out (no rows of output).
@@ -471,19 +391,6 @@ __global__ __launch_bounds__(FEW_WAVES *WAVE) void k_few(product pr, EPI epi)
             for (int e = 0; e < 4; ++e) v[which][h * 4 + e] = sum[e];
         }
     epi(0, wave * 16 + r, n0 + q * 8, v[0], v[1]);
-}
-
-constexpr int FEW_ROWS = 64;
-
-// Whether the few-rows form is expected to beat tiles that take `tiles_us`.  Weights come at the rate of a large read, and
-// with the rows that every workgroup reads again (from L2) at 7.3 TB/s in all, after 2.2 us of start and end.  At 1024 x 4096 one
-// row takes 5.2 us and 64 take 9.1 (tiles: 9.4), at 4096 x 4096 14.5 and 26 (26), at 4096 x 11264 33 and 75 (30).  What is
-// kept has no say: h, and g and u made again, are the same bits in every form.
-bool few_rows_win(int64_t M, int64_t N, int64_t K, double tiles_us)
-{
-    if (M > FEW_ROWS) return false;
-    const double weights = 4.0 * N * K, again = (double)((N + 15) / 16) * M * K * 2.0;
-    return 2.2 + std::max(weights / 5.5e6, (weights + again) / 7.3e6) < tiles_us;
 }
 
 template <class T, int NB, class EPI>
@@ -712,31 +619,11 @@ static bool good_kept(int keep, int64_t rows, const void *g, const void *u, cons
     return ge && ue && (uintptr_t)g % 16 == 0 && (uintptr_t)u % 16 == 0;
 }
 
-// The three products of a gated block: g and u, dx, and dwg and dwu.
-static cut sums_cut(int64_t rows, int64_t d, int64_t f) { return choose_cut(rows, f, d, 1, 1, 2, true); }
-static cut dx_cut(int64_t rows, int64_t d, int64_t f) { return choose_cut(rows, d, f, 2, 1, 1, true); }
-static cut dw_cut(int64_t rows, int64_t d, int64_t f) { return choose_cut(f, d, rows, 1, 2, 1, false); }
-
-// Up to so many elements of dg go into the products in two parts: twice the products, of a size that is all latency.  At 1 x 64 x
-// 64 the gradients' errors are 1.0 of a rounding's instead of up to 1.8.
-constexpr int64_t FINE_ELEMENTS = 4096;
-
-// The backward's two products, one after the other or in one launch.
-struct backward_cut {
-    cut x, w;
-    pair_cut both;
-    bool together, fine;
-    backward_cut(int64_t rows, int64_t d, int64_t f) : x(dx_cut(rows, d, f)), w(dw_cut(rows, d, f)), both(choose_pair(rows, d, f))
-    {
-        together = both.us < x.us + w.us + LAUNCH;
-        fine = rows * f <= FINE_ELEMENTS;
-    }
-    size_t bytes(int64_t rows, int64_t d, int64_t f) const
-    {
-        // of any way: a caller may want one of the two only
-        return std::max({split_bytes(x, rows, d, 1), split_bytes(w, f, d, 2), split_bytes(cut{128, 128, 2, both.splits, 0.0}, rows, d, 1)});
-    }
-};
+// Of a backward pass, any way: a caller may want one of the two only.
+static size_t backward_bytes(const backward_cut &c, int64_t rows, int64_t d, int64_t f)
+{
+    return std::max({split_bytes(c.x, rows, d, 1), split_bytes(c.w, f, d, 2), split_bytes(cut{128, 128, 2, c.both.splits, 0.0}, rows, d, 1)});
+}
 
 extern "C" int rkb_gated_fwd_workspace(int dtype, int64_t rows, int64_t d, int64_t f, int aligned, size_t *bytes)
 {
@@ -802,7 +689,7 @@ extern "C" int rkb_gated_bwd_workspace(int dtype, int keep, int64_t rows, int64_
 {
     if (!bytes || !good_gated(dtype, RKB_SILU, keep, rows, d, f)) return RKB_E_INVAL;
     *bytes = (rows * f <= FINE_ELEMENTS ? 4 : 2) * padded_bytes(rows, f) + (d % 8 || !aligned ? padded_bytes(rows, d) + 2 * padded_bytes(f, d) : 0) +
-             backward_cut(rows, d, f).bytes(rows, d, f);
+             backward_bytes(backward_cut(rows, d, f), rows, d, f);
     return RKB_OK;
 }
 
@@ -827,7 +714,7 @@ extern "C" int rkb_gated_bwd(int dtype, int act, int keep, int64_t rows, int64_t
     if (cuts.fine) ws.take(2 * part);
     gated_operands in{{x, x_stride, rows, d}, {wg, wg_stride, f, d}, {wu, wu_stride, f, d}};
     if (rows > 0) in.align(ws);
-    void *parts = ws.take(cuts.bytes(rows, d, f));
+    void *parts = ws.take(backward_bytes(cuts, rows, d, f));
     if (ws.at != workspace && !good_workspace(workspace)) return RKB_E_INVAL;
     if (!ws.fits()) return RKB_E_NOMEM;
     int rc = ws.run(st);

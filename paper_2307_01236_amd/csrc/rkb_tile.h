@@ -21,6 +21,7 @@
 #include <type_traits>
 
 #include "rkb_common.h"
+#include "rkb_cut.h"
 
 namespace rkb {
 
@@ -36,7 +37,6 @@ __device__ inline f32x4 mma(frag<f16> a, frag<f16> b, f32x4 c)
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
 }
 
-constexpr int DEPTH = 64;                // k of a stage
 // s_waitcnt for all LDS reads and all but the last n copies
 constexpr int wait_copies(int n) { return (n & 15) | 0x70 | n >> 4 << 14; }
 constexpr int PIECE = 1024;              // bytes that one wave's copy instruction brings
