@@ -4,10 +4,19 @@
 #include <algorithm>
 #include <cstdint>
 
+#include "rk_block.h"
+
 namespace rkb {
 
 constexpr int DEPTH = 64;                        // k of a tile's stage
 constexpr int64_t MAX_TILES = (int64_t)1 << 22;  // workgroups of a launch: 512 threads of each in 32 bits
+
+// Whether a lane's place in a stage of `tile_rows` rows that run along k, `stride` elements apart, is a 32-bit number of
+// bytes from the tile's first row.  Callers' strides are at most STRIDE_LIMIT (others' rows are copied into the
+// workspace); copies, and dg and du, have rows as long as their columns rounded up to 8, up to RKB_MAX_COLS.
+constexpr int64_t STRIDE_LIMIT = (int64_t)1 << 22;
+constexpr bool rows_in_reach(int tile_rows, int64_t stride) { return (tile_rows - 1) * stride * 2 + (DEPTH - 8) * 2 <= UINT32_MAX; }
+static_assert(rows_in_reach(256, STRIDE_LIMIT) && rows_in_reach(128, RKB_MAX_COLS));
 
 // How a product is cut: the tile, its buffers, and how many workgroups share the stages of one tile (splits).
 struct cut {
@@ -37,13 +46,14 @@ constexpr double LAUNCH = 6.0;                          // a launch more, from t
 
 // The cut that these figures expect to be fastest.  Splits share a long K among workgroups where the tiles alone do
 // not fill the chip, at the price of 32-bit partial sums written and read once: dw of 512 x 512 over 16384
-// rows takes 174 us whole and 25 in 16 splits, of 2048 x 2048 over 2048 rows 28 whole and 34 in 2.
+// rows takes 174 us whole and 25 in 16 splits, of 2048 x 2048 over 2048 rows 28 whole and 34 in 2.  near: A's rows run along k (and
+// B's in g and u, by 128); tiles that would pass their offsets' range are left out, above 8.4 million columns.
 inline cut choose_cut(int64_t M, int64_t N, int64_t K, int parts, int problems, int sums, bool near)
 {
     const int64_t stages = std::max<int64_t>(1, (K + DEPTH - 1) / DEPTH * parts);
     cut best{256, 256, 2, 1, 1e30};
     for (const tile_kind &t : TILES) {
-        if (t.tm == 192 && !near) continue;
+        if (near ? !rows_in_reach(t.tm, (K + 7) / 8 * 8) : t.tm == 192) continue;
         const int64_t tiles = (M + t.tm - 1) / t.tm * ((N + t.tn / sums - 1) / (t.tn / sums)) * problems;
         for (int splits : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
             if (splits > 1 && (sums == 2 || splits * 4 > stages || splits * tiles > 2 * t.slots)) break;

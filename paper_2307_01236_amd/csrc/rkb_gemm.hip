@@ -420,8 +420,6 @@ int run_sums(const product &pr, bool few, const cut &c, const EPI &epi, hipStrea
 // out otherwise is copied into the workspace once, its rows ending in zeros: one more pass
 // over that matrix (26803 x 1740: 31 us, 6 TB/s), against the many that its product makes.
 
-constexpr int64_t STRIDE_LIMIT = (int64_t)1 << 22;  // 256 rows' offsets stay in 32 bits
-
 struct matrix {
     const void *p;
     int64_t stride, rows, cols;

@@ -8,6 +8,7 @@ from collections import namedtuple
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(os.path.dirname(HERE), "paper_2307_01236_amd", "csrc")
+INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 
 Cut = namedtuple("Cut", "rows bufs splits")  # rows: of a tile
 Gated = namedtuple("Gated", "few together fine pair sums dx dw")  # pair: (buffers, splits)
@@ -20,7 +21,7 @@ def _load():
     if _lib is None:
         with tempfile.TemporaryDirectory() as tmp:
             out = os.path.join(tmp, "cut_query.so")
-            subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Werror", "-shared", "-fPIC", "-I", CSRC,
+            subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Werror", "-shared", "-fPIC", "-I", CSRC, "-I", INCLUDE,
                             os.path.join(HERE, "cut_query.cpp"), "-o", out], check=True)
             _lib = C.CDLL(out)
         _lib.gated_cuts.argtypes = [C.c_int64] * 3 + [C.POINTER(C.c_int)]

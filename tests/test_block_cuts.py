@@ -26,3 +26,21 @@ def test_the_sizes_leave_no_tile_out():
 @pytest.mark.parametrize("size,want", cuts.WEIGHT_GRAD_SIZES)
 def test_weight_gradient_sizes_take_the_tiles_they_are_there_for(size, want):
     assert cuts.weight_grad(*size) == want
+
+
+def test_rows_of_a_tile_stay_within_32_bit_offsets():
+    """A lane's place in a stage of an operand whose rows run along k is a 32-bit number of bytes from the tile's first
+    row: the last row's last chunk must not pass it, over all widths that the calls take.  The longest rows are
+    copies in the workspace and dg and du, whose columns are rounded up to 8."""
+    rng, longest = random.Random(3), bk.RKB_MAX_COLS
+
+    def reaches(tile_rows, columns):
+        return (tile_rows - 1) * (-(-columns // 8) * 8) * 2 + 7 * 16 < 1 << 32
+
+    sizes = [(256, 1024, 8421512), (512, 512, longest), (200, longest, 64), (8192, longest, 8192), (8192, 8192, longest)]
+    sizes += [tuple(round(2 ** rng.uniform(0, top)) for top in (14, 24, 24)) for _ in range(20000)]
+    assert any(not reaches(256, f) for _, _, f in sizes)  # a case for the choice
+    for rows, width, hidden in sizes:
+        c = cuts.gated(rows, width, hidden)
+        assert reaches(c.sums.rows, width) and reaches(c.dx.rows, hidden), (rows, width, hidden)
+        assert reaches(128, width) and reaches(128, hidden)  # wg and wu beside x, and dg and du in a launch with the weights' gradients

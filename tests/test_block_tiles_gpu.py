@@ -81,3 +81,26 @@ def test_weight_gradient_by_every_tile(size, what):
         want = torch.mm(dy.double().t().contiguous(), ref)
         bound = bo.sum_bound(torch.mm(dy.double().abs().t().contiguous(), ref.abs()), rows) + bo.rounding(want, BF)
         assert worst(bk.rkb_weight_grad(dy, kept), want, bound) <= 1.0
+
+
+def test_offsets_past_31_bits_within_a_tile():
+    """128 rows of the widest matrices, which lie 2^24 elements apart in the workspace: x in the forward, dg and du in the
+    backward.  One element of each row is not zero, so that every result is one known number."""
+    rows, wide = 128, bk.RKB_MAX_COLS - 1
+    at = torch.arange(rows, device="cuda") * (wide // (rows - 1))  # from the first column to near the last
+    at[-1] = wide - 1
+    row = torch.arange(rows, device="cuda")
+    assert cuts.gated(rows, wide, 8).sums.rows == cuts.gated(rows, 8, wide).dx.rows == 128
+    x, w = torch.zeros(rows, wide, dtype=BF, device="cuda"), torch.ones(8, wide, dtype=BF, device="cuda")
+    x[row, at] = (row + 1).to(BF)
+    _, (g, u) = bk.rkb_gated_fwd(x, w, w, keep="full")
+    assert torch.equal(g, (row + 1.0)[:, None].expand(rows, 8)) and torch.equal(u, g)
+    del x, w
+    dh = torch.zeros(rows, wide, dtype=BF, device="cuda")
+    dh[row, at] = 1.0
+    g, u = torch.zeros_like(dh), torch.full_like(dh, 2.0)  # silu(0) = 0 with a slope of 1/2: dg = dh, du = 0
+    w = normal(torch.Generator(device="cuda").manual_seed(14), wide, 8, dtype=BF)
+    x = torch.ones(rows, 8, dtype=BF, device="cuda")
+    dx, dwg, dwu, _ = bk.rkb_gated_bwd(dh, x, w, w, kept=(g, u))
+    assert torch.equal(dx, w[at])
+    assert bool((dwg[at] == 1).all()) and int(dwg.count_nonzero()) == rows * 8 and not dwu.any()
