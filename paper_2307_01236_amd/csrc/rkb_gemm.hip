@@ -60,7 +60,10 @@ struct out_matrix {
         store8<T>(p + row * stride + col, 8, v);
         if (low) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] -= (float)(T)settled<T>(v[i]);
+            for (int i = 0; i < 8; ++i) {
+                const float high = (float)(T)settled<T>(v[i]);
+                v[i] = finite(fabsf(high)) ? v[i] - high : 0.0f;  // an infinity leaves nothing over (its difference would be NaN)
+            }
             store8<T>(p + low + row * stride + col, 8, v);
         }
     }

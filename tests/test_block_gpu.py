@@ -570,3 +570,36 @@ def test_the_binding_refuses_what_does_not_fit():
         with pytest.raises(bk.RKBError) as e:
             call()
         assert e.value.code == bk.RKB_E_INVAL, i
+
+
+@pytest.mark.parametrize("rows,hidden", [(3, 40), (70, 72)])
+def test_gated_gradients_past_the_range(rows, hidden):
+    """dg or du beyond the largest value of 16 bits: the infinity that it rounds to reaches the gradients it belongs to, and no
+    other, with its sign, for few elements (two parts) as for many."""
+    width, at = 24, (1, 5)
+    x, wg, wu = (torch.full(s, 0.5, dtype=HF, device="cuda") for s in ((rows, width), (hidden, width), (hidden, width)))
+    for which in ("g", "u"):
+        for sign in (1.0, -1.0):
+            g, u = (torch.ones(rows, hidden, device="cuda") for _ in range(2))
+            (u if which == "g" else g)[at] = 1000.0  # dg = dh u act'(g), du = dh act(g)
+            dh = torch.full((rows, hidden), 0.01, dtype=HF, device="cuda")
+            dh[at] = 200.0 * sign
+            dx, dwg, dwu, _ = bk.rkb_gated_bwd(dh, x, wg, wu, kept=(g, u))
+            bad, good = (dwg, dwu) if which == "g" else (dwu, dwg)
+            assert bool((dx[at[0]] == sign * math.inf).all()) and bool((bad[at[1]] == sign * math.inf).all())
+            assert bool(good.isfinite().all())
+            others = torch.arange(rows, device="cuda") != at[0], torch.arange(hidden, device="cuda") != at[1]
+            assert bool(dx[others[0]].isfinite().all()) and bool(bad[others[1]].isfinite().all())
+
+
+@pytest.mark.parametrize("rows,hidden", [(3, 40), (70, 72)])
+def test_gated_gradients_of_a_bad_element(rows, hidden):
+    """NaN and infinities in dh stay NaN and infinities where they belong."""
+    x, wg, wu = (torch.full(s, 0.5, dtype=BF, device="cuda") for s in ((rows, 24), (hidden, 24), (hidden, 24)))
+    one = torch.ones(rows, hidden, device="cuda")
+    for value, check in ((math.nan, torch.isnan), (math.inf, torch.isposinf), (-math.inf, torch.isneginf)):
+        dh = torch.full((rows, hidden), 0.01, dtype=BF, device="cuda")
+        dh[2, 7] = value
+        dx, dwg, dwu, _ = bk.rkb_gated_bwd(dh, x, wg, wu, kept=(one, one))
+        for t, line in ((dx, 2), (dwg, 7), (dwu, 7)):
+            assert bool(check(t[line]).all()) and int(t.isfinite().all(1).sum()) == t.shape[0] - 1
