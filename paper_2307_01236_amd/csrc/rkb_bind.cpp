@@ -72,18 +72,19 @@ matrix as_matrix(const at::Tensor &t, const char *where)
     const int64_t dims = t.dim();
     if (dims == 0) fail(RKB_E_INVAL, where, "no columns");
     matrix m{t.data_ptr(), 1, t.size(dims - 1), t.size(dims - 1)};
+    for (int64_t i = dims - 2; i >= 0; --i) m.rows *= t.size(i);
+    if (m.rows == 0) return m;  // no row, so none that is out of place
     int64_t next = -1;  // what the next outer dimension's stride has to be
     for (int64_t i = dims - 2; i >= 0; --i) {
         const int64_t n = t.size(i);
-        m.rows *= n;
         if (n == 1) continue;
         if (next < 0)
             m.stride = t.stride(i);
-        else if (t.stride(i) != next && n != 0)
+        else if (t.stride(i) != next)
             fail(RKB_E_INVAL, where, "rows that are not evenly spaced");
         next = t.stride(i) * n;
     }
-    if (m.cols > 1 && m.rows > 0 && t.stride(dims - 1) != 1) fail(RKB_E_INVAL, where, "columns that are not adjacent");
+    if (m.cols > 1 && t.stride(dims - 1) != 1) fail(RKB_E_INVAL, where, "columns that are not adjacent");
     return m;
 }
 

@@ -603,3 +603,22 @@ def test_gated_gradients_of_a_bad_element(rows, hidden):
         dx, dwg, dwu, _ = bk.rkb_gated_bwd(dh, x, wg, wu, kept=(one, one))
         for t, line in ((dx, 2), (dwg, 7), (dwu, 7)):
             assert bool(check(t[line]).all()) and int(t.isfinite().all(1).sum()) == t.shape[0] - 1
+
+
+@pytest.mark.parametrize("lead", [(3, 0), (0, 3), (0, 3, 5), (2, 0, 5), (0,)])
+def test_no_rows_of_any_leading_dimensions(lead):
+    x, dh, w = torch.zeros(*lead, 64, dtype=BF, device="cuda"), torch.zeros(*lead, 40, dtype=BF, device="cuda"), rand(40, 64, dtype=BF)
+    y, mean, rstd = bk.rkb_layer_norm_fwd(x)
+    assert y.shape == x.shape and mean.shape == lead
+    dx, _, db = bk.rkb_layer_norm_bwd(x, x, mean, rstd, bias=True)
+    assert dx.shape == x.shape and not db.any()
+    c = bk.rkb_ckpt8_save(x)
+    assert bk.rkb_ckpt8_load(c).shape == x.shape
+    assert not bk.rkb_weight_grad(dh, c).any() and not bk.rkb_weight_grad(dh, x).any()
+    for keep in ("none", "full", "16bit", "8bit"):
+        h, kept = bk.rkb_gated_fwd(x, w, w, keep=keep)
+        assert h.shape == dh.shape
+        dx, dwg, dwu, again = bk.rkb_gated_bwd(dh, x, w, w, kept=kept, want_h=True)
+        assert dx.shape == x.shape and again.shape == dh.shape and not dwg.any() and not dwu.any()
+    wide = torch.zeros(*lead, 80, dtype=BF, device="cuda")[..., 3:67]  # no elements, whatever the strides
+    assert bk.rkb_layer_norm_fwd(wide)[0].shape == x.shape and bk.rkb_ckpt8_save(wide).shape == x.shape
