@@ -118,9 +118,7 @@ extern "C" int rkb_ckpt8_save(int dtype, int64_t rows, int64_t cols, const void 
     const span_map m = make_map(rows, cols, SAVE_SPAN);
     auto go = [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        hipLaunchKernelGGL(k_ckpt_save<T>, map_grid(m), dim3(CKPT_BLOCK), 0, (hipStream_t)stream, m, (const T *)x, x_stride,
-                           codes, exps);
-        return launched();
+        return launch(k_ckpt_save<T>, map_grid(m), dim3(CKPT_BLOCK), (hipStream_t)stream, m, (const T *)x, x_stride, codes, exps);
     };
     return dtype == RKB_F32 ? go((float *)nullptr) : dtype == RKB_F16 ? go((f16 *)nullptr) : go((bf16 *)nullptr);
 }
@@ -135,9 +133,7 @@ extern "C" int rkb_ckpt8_load(int dtype, int64_t rows, int64_t cols, const int8_
     const span_map m = make_map(rows, cols, dtype == RKB_F32 ? CHUNK<float> : CHUNK<f16>);
     auto go = [&](auto *t) {
         using T = std::remove_pointer_t<decltype(t)>;
-        hipLaunchKernelGGL(k_ckpt_load<T>, map_grid(m), dim3(CKPT_BLOCK), 0, (hipStream_t)stream, m, codes, exps, (T *)x,
-                           x_stride);
-        return launched();
+        return launch(k_ckpt_load<T>, map_grid(m), dim3(CKPT_BLOCK), (hipStream_t)stream, m, codes, exps, (T *)x, x_stride);
     };
     return dtype == RKB_F32 ? go((float *)nullptr) : dtype == RKB_F16 ? go((f16 *)nullptr) : go((bf16 *)nullptr);
 }

@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <tuple>
 #include <type_traits>
 
 #include "rk_block.h"
@@ -223,6 +224,22 @@ inline bool good_output(const void *p, int64_t rows, int64_t cols, int64_t strid
 inline int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 inline int64_t code_ld(int64_t cols) { return round_up(cols, GROUP); }
 
-inline int launched() { return hipGetLastError() == hipSuccess ? RKB_OK : RKB_E_DEVICE; }
+// Queues a kernel.  The launch's own result is looked at, not the thread's last error, which an earlier call of someone
+// else's may have left: that is neither reported here nor taken from whoever asks for it.
+template <class... P, class... A>
+int launch(void (*kernel)(P...), dim3 grid, dim3 block, hipStream_t st, const A &...a)
+{
+    static_assert(sizeof...(P) == sizeof...(A));
+    std::tuple<P...> values(a...);
+    const hipError_t e = std::apply(
+        [&](auto &...v) {
+            void *at[] = {(void *)&v...};
+            return hipLaunchKernel((const void *)kernel, grid, block, at, 0, st);
+        },
+        values);
+    if (e == hipSuccess) return RKB_OK;
+    (void)hipGetLastError();
+    return RKB_E_DEVICE;
+}
 
 }  // namespace rkb

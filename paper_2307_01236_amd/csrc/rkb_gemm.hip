@@ -197,9 +197,7 @@ int launch_product(product pr, const cut &c, const EPI &epi, hipStream_t st)
     pr.split_stages = (stages + c.splits - 1) / c.splits;
     const int64_t total = (int64_t)pr.tiles_m * pr.tiles_n * pr.problems * pr.splits;
     if (total > MAX_TILES) return RKB_E_INVAL;
-    hipLaunchKernelGGL((k_product<T, EPI, TM, TN, WM, WN, BUFS, ANEAR, BNEAR, PARTS>), dim3((uint32_t)total), dim3(WM * WN * WAVE), 0, st,
-                       pr, epi);
-    return launched();
+    return launch(k_product<T, EPI, TM, TN, WM, WN, BUFS, ANEAR, BNEAR, PARTS>, dim3((uint32_t)total), dim3(WM * WN * WAVE), st, pr, epi);
 }
 
 template <class T, bool ANEAR, bool BNEAR, int PARTS, class EPI>
@@ -252,9 +250,7 @@ template <class T>
 int join(const float *parts, int splits, int problems, const epi_store<T> &out, hipStream_t st)
 {
     const int64_t ld = round_up(out.c[0].cols, 8), blocks = (out.c[0].rows * ld / 8 + 255) / 256;
-    hipLaunchKernelGGL((k_join<T>), dim3((uint32_t)std::min<int64_t>(blocks, 1 << 16), problems), dim3(256), 0, st, parts, splits, ld,
-                       out);
-    return launched();
+    return launch(k_join<T>, dim3((uint32_t)std::min<int64_t>(blocks, 1 << 16), problems), dim3(256), st, parts, splits, ld, out);
 }
 
 // A product stored as it is; `scratch` has split_bytes.
@@ -283,13 +279,10 @@ int run_pair(product dx, product dw, const pair_cut &c, void *scratch, const epi
     if (nx + nw > MAX_TILES) return RKB_E_INVAL;
     auto go = [&](auto epi) {
         using EPI = decltype(epi);
-        auto launch = [&](auto kernel) {
-            hipLaunchKernelGGL(kernel, dim3((uint32_t)(nx + nw)), dim3(512), 0, st, dx, epi, (int)nx, dw, out_w);
-            return launched();
-        };
+        auto by = [&](auto kernel) { return launch(kernel, dim3((uint32_t)(nx + nw)), dim3(512), st, dx, epi, (int)nx, dw, out_w); };
         if constexpr (!FINE)
-            if (c.bufs == 4) return launch(k_backward<T, EPI, 4, false>);
-        return launch(k_backward<T, EPI, 2, FINE>);
+            if (c.bufs == 4) return by(k_backward<T, EPI, 4, false>);
+        return by(k_backward<T, EPI, 2, FINE>);
     };
     if (c.splits == 1 || nx == 0) return go(out_x);
     const int rc = go(epi_part{(float *)scratch, out_x.c[0].rows, out_x.c[0].cols, round_up(out_x.c[0].cols, 8)});
@@ -400,13 +393,9 @@ template <class T, int NB, class EPI>
 int launch_few(const product &pr, const EPI &epi, hipStream_t st)
 {
     const dim3 grid((uint32_t)((pr.N + 16 * NB - 1) / (16 * NB))), block(FEW_WAVES * WAVE);
-    if (pr.M <= 16)
-        hipLaunchKernelGGL((k_few<T, EPI, 1, NB>), grid, block, 0, st, pr, epi);
-    else if (pr.M <= 32)
-        hipLaunchKernelGGL((k_few<T, EPI, 2, NB>), grid, block, 0, st, pr, epi);
-    else
-        hipLaunchKernelGGL((k_few<T, EPI, 4, NB>), grid, block, 0, st, pr, epi);
-    return launched();
+    if (pr.M <= 16) return launch(k_few<T, EPI, 1, NB>, grid, block, st, pr, epi);
+    if (pr.M <= 32) return launch(k_few<T, EPI, 2, NB>, grid, block, st, pr, epi);
+    return launch(k_few<T, EPI, 4, NB>, grid, block, st, pr, epi);
 }
 
 // g and u of a block, by tiles or by the few-rows form (which takes operands of any alignment).  WHOLE: the epilogue needs units
@@ -492,8 +481,7 @@ struct workspace_taker {
         if (!n_jobs) return RKB_OK;
         int64_t most = 0;
         for (int i = 0; i < n_jobs; ++i) most = std::max(most, jobs.job[i].rows * jobs.job[i].chunks);
-        hipLaunchKernelGGL(k_pad, dim3((uint32_t)std::min<int64_t>((most + 255) / 256, 4096), n_jobs), dim3(256), 0, st, jobs);
-        return launched();
+        return launch(k_pad, dim3((uint32_t)std::min<int64_t>((most + 255) / 256, 4096), n_jobs), dim3(256), st, jobs);
     }
 };
 
@@ -733,9 +721,7 @@ extern "C" int rkb_gated_bwd(int dtype, int act, int keep, int64_t rows, int64_t
                 }
                 const dim3 grid((uint32_t)((f + 2047) / 2048), (uint32_t)std::min<int64_t>(rows, 32768));
                 auto go = [&](auto kind) {
-                    hipLaunchKernelGGL((k_gated_grads<T, a(), kind()>), grid, dim3(256), 0, st, (const T *)dh, dh_stride, g, u,
-                                       ge, ue, og, ou, oh);
-                    return launched();
+                    return launch(k_gated_grads<T, a(), kind()>, grid, dim3(256), st, (const T *)dh, dh_stride, g, u, ge, ue, og, ou, oh);
                 };
                 return with_kept(keep, go);
             });

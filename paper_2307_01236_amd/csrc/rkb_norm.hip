@@ -399,10 +399,8 @@ extern "C" int rkb_layer_norm_fwd(int dtype, int wdtype, int64_t rows, int64_t c
         return with_layout<false, CHUNK<T>>(cols, [&](auto lanes, auto nv, auto block) {
             constexpr int ROWS = block() / lanes();
             const int64_t blocks = std::min<int64_t>((rows + ROWS - 1) / ROWS, (int64_t)1 << 22);
-            hipLaunchKernelGGL((k_norm_fwd<T, W, lanes(), nv(), block()>), dim3((uint32_t)blocks), dim3(block()), 0,
-                               (hipStream_t)stream, rows, (int)cols, (const T *)x, x_stride, (const W *)w, (const W *)b,
-                               eps, (T *)y, y_stride, mean, rstd);
-            return launched();
+            return launch(k_norm_fwd<T, W, lanes(), nv(), block()>, dim3((uint32_t)blocks), dim3(block()), (hipStream_t)stream, rows,
+                          (int)cols, (const T *)x, x_stride, (const W *)w, (const W *)b, eps, (T *)y, y_stride, mean, rstd);
         });
     });
 }
@@ -449,18 +447,13 @@ extern "C" int rkb_layer_norm_bwd(int dtype, int wdtype, int64_t rows, int64_t c
         int rc = with_layout<true, CHUNK<T>>(cols, [&](auto lanes, auto nv, auto block) {
             blocks = bwd_blocks(rows, block() / lanes(), block(), want);
             auto go = [&](auto kernel) {
-                hipLaunchKernelGGL(kernel, dim3((uint32_t)blocks), dim3(block()), 0, st, rows, (int)cols, (const T *)dy,
-                                   dy_stride, kept, mean, rstd, (const W *)w, (T *)dx, dx_stride, sums);
+                return launch(kernel, dim3((uint32_t)blocks), dim3(block()), st, rows, (int)cols, (const T *)dy, dy_stride, kept, mean,
+                              rstd, (const W *)w, (T *)dx, dx_stride, sums);
             };
-            if (ckpt)
-                go(k_norm_bwd<T, W, lanes(), nv(), block(), true>);
-            else
-                go(k_norm_bwd<T, W, lanes(), nv(), block(), false>);
-            return launched();
+            return ckpt ? go(k_norm_bwd<T, W, lanes(), nv(), block(), true>) : go(k_norm_bwd<T, W, lanes(), nv(), block(), false>);
         });
         if (rc != RKB_OK || !want) return rc;
-        hipLaunchKernelGGL((k_norm_cols<W>), dim3((uint32_t)((cols + 63) / 64), 2), dim3(256), 0, st, (int)blocks,
-                           (int)cols, sums, (W *)dw, (W *)db);
-        return launched();
+        return launch(k_norm_cols<W>, dim3((uint32_t)((cols + 63) / 64), 2), dim3(256), st, (int)blocks, (int)cols, sums, (W *)dw,
+                      (W *)db);
     });
 }

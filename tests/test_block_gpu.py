@@ -622,3 +622,37 @@ def test_no_rows_of_any_leading_dimensions(lead):
         assert dx.shape == x.shape and again.shape == dh.shape and not dwg.any() and not dwu.any()
     wide = torch.zeros(*lead, 80, dtype=BF, device="cuda")[..., 3:67]  # no elements, whatever the strides
     assert bk.rkb_layer_norm_fwd(wide)[0].shape == x.shape and bk.rkb_ckpt8_save(wide).shape == x.shape
+
+
+def test_an_earlier_error_is_neither_reported_nor_cleared():
+    """An error that some call before left with the HIP runtime is not these calls', and stays for whoever asks for it.  At
+    the C interface: torch's allocator asks by itself."""
+    rows, d, f = 100, 64, 96
+    lib, st = bk.load(), torch.cuda.current_stream().cuda_stream
+    x, wg, wu, dh = gated_inputs(rows, d, f, BF)
+    y, dx, h, dw, dwg, dwu = (torch.zeros(s, dtype=BF, device="cuda") for s in ((rows, d), (rows, d), (rows, f), (f, d), (f, d), (f, d)))
+    mean, rstd = (torch.zeros(rows, device="cuda") for _ in range(2))
+    codes, exps = torch.zeros(rows, d, dtype=torch.int8, device="cuda"), torch.zeros(rows, d // 32, dtype=torch.uint8, device="cuda")
+    db = torch.zeros(d, dtype=BF, device="cuda")
+    ws = torch.zeros(1 << 24, dtype=torch.uint8, device="cuda")
+    p, B = (lambda t: t.data_ptr()), bk.RKB_BF16
+    calls = [
+        lambda: lib.rkb_layer_norm_fwd(B, B, rows, d, p(x), d, None, None, 1e-5, p(y), d, p(mean), p(rstd), st),
+        lambda: lib.rkb_ckpt8_save(B, rows, d, p(x), d, p(codes), p(exps), st),
+        lambda: lib.rkb_ckpt8_load(B, rows, d, p(codes), p(exps), p(y), d, st),
+        lambda: lib.rkb_weight_grad(B, rows, f, d, p(dh), f, None, d, p(codes), p(exps), p(dw), d, p(ws), 1 << 24, st),
+        lambda: lib.rkb_layer_norm_bwd(B, B, rows, d, p(x), d, p(x), d, None, None, p(mean), p(rstd), None, p(dx), d, None, p(db), p(ws),
+                                       1 << 24, st),
+        lambda: lib.rkb_gated_fwd(B, 0, 0, rows, d, f, p(x), d, p(wg), d, p(wu), d, p(h), f, None, None, None, None, p(ws), 1 << 24, st),
+        lambda: lib.rkb_gated_bwd(B, 0, 0, rows, d, f, p(dh), f, p(x), d, p(wg), d, p(wu), d, None, None, None, None, p(dx), d, p(dwg),
+                                  p(dwu), d, None, f, p(ws), 1 << 24, st),
+    ]
+    torch.cuda.synchronize()
+    lib.hipGetLastError()
+    left = lib.hipSetDevice(1 << 20)  # no such device; refused by the runtime on the host
+    codes_returned = [c() for c in calls]
+    stays = lib.hipGetLastError()
+    assert left != 0 and stays == left
+    assert codes_returned == [bk.RKB_OK] * len(calls)
+    torch.cuda.synchronize()
+    assert torch.equal(h, bk.rkb_gated_fwd(x, wg, wu)[0]) and torch.equal(dx, bk.rkb_gated_bwd(dh, x, wg, wu)[0])
