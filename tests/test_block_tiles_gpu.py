@@ -1,6 +1,6 @@
-"""The block operators at sizes that take every tile, split and launch (cuts.GATED_SIZES), element by
-element against the 64-bit definitions within the bounds that 32-bit sums and one rounding of each output (and of dg
-and du) allow; the 64-bit side runs on the GPU."""
+"""The block operators at sizes that take every tile, split and launch (cuts.GATED_SIZES), and layer norm's
+column sums over many rows in turn, element by element against the 64-bit definitions within the bounds that
+32-bit sums and one rounding of each output (and of dg and du) allow; the 64-bit side runs on the GPU."""
 import math
 
 import pytest
@@ -104,3 +104,18 @@ def test_offsets_past_31_bits_within_a_tile():
     dx, dwg, dwu, _ = bk.rkb_gated_bwd(dh, x, w, w, kept=(g, u))
     assert torch.equal(dx, w[at])
     assert bool((dwg[at] == 1).all()) and int(dwg.count_nonzero()) == rows * 8 and not dwu.any()
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, FP])
+@pytest.mark.parametrize("cols", [100, 250, 500, 1000, 2000, 4000, 8000, 16384])
+def test_layer_norm_columns_over_many_rows(cols, dtype):
+    """dw and db over blocks that each take several rows in turn, the last turn not full, by every layout of a row."""
+    rows, gen = 1403, torch.Generator(device="cuda").manual_seed(13)
+    x, dy, w = normal(gen, rows, cols, dtype=dtype) + 0.5, normal(gen, rows, cols, dtype=dtype, scale=0.1), normal(gen, cols, dtype=dtype)
+    _, mean, rstd = bk.rkb_layer_norm_fwd(x, w)
+    c = bk.rkb_ckpt8_save(x)
+    for kept, ref in ((x, x.double()), (c, bk.rkb_ckpt8_load(c).double())):
+        args = (dy.double(), ref, mean.double(), rstd.double(), w.double())
+        got = bk.rkb_layer_norm_bwd(dy, kept, mean, rstd, w, bias=True)
+        for t, want, e in zip(got, bo.layer_norm_grads(*args), bo.layer_norm_grad_bounds(*args, dtype, dtype)):
+            assert worst(t, want, e) <= 1.0
