@@ -398,7 +398,8 @@ extern "C" int rkb_layer_norm_fwd(int dtype, int wdtype, int64_t rows, int64_t c
         using W = std::remove_pointer_t<decltype(wt)>;
         return with_layout<false, CHUNK<T>>(cols, [&](auto lanes, auto nv, auto block) {
             constexpr int ROWS = block() / lanes();
-            const int64_t blocks = std::min<int64_t>((rows + ROWS - 1) / ROWS, (int64_t)1 << 22);
+            // a launch's lanes are counted in 32 bits: more rows go in turn
+            const int64_t blocks = std::min<int64_t>((rows + ROWS - 1) / ROWS, ((int64_t)1 << 30) / block());
             return launch(k_norm_fwd<T, W, lanes(), nv(), block()>, dim3((uint32_t)blocks), dim3(block()), (hipStream_t)stream, rows,
                           (int)cols, (const T *)x, x_stride, (const W *)w, (const W *)b, eps, (T *)y, y_stride, mean, rstd);
         });

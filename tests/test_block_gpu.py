@@ -656,3 +656,14 @@ def test_an_earlier_error_is_neither_reported_nor_cleared():
     assert codes_returned == [bk.RKB_OK] * len(calls)
     torch.cuda.synchronize()
     assert torch.equal(h, bk.rkb_gated_fwd(x, wg, wu)[0]) and torch.equal(dx, bk.rkb_gated_bwd(dh, x, wg, wu)[0])
+
+
+def test_layer_norm_of_more_rows_than_a_launch_has_blocks():
+    """Wide rows take a block of 1024 lanes each, and 2^22 such blocks pass 32 bits of lanes; one row stands for all."""
+    rows, cols = (1 << 22) + 3, 8200
+    x, w = rand(1, cols, seed=1, dtype=BF), rand(cols, seed=2, dtype=BF)
+    want = bk.rkb_layer_norm_fwd(x, w)
+    got = bk.rkb_layer_norm_fwd(x.expand(rows, cols), w)
+    for at in (0, (1 << 20) - 1, 1 << 20, (1 << 21) + 1, (1 << 22) - 1, 1 << 22, rows - 1):
+        assert all(torch.equal(p[at], q[0]) for p, q in zip(got, want)), at
+    assert bool((got[1] == want[1]).all()) and bool((got[2] == want[2]).all())
