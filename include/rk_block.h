@@ -98,7 +98,8 @@ int rkb_ckpt8_load(int dtype, int64_t rows, int64_t cols, const int8_t *codes, c
 
 /*
  * Weight gradient of y = x W^T: dw [n, k] = dy^T x, summed over rows; dy [rows, n], x [rows, k], given as it
- * was or as its checkpoint, as above.  dtype: RKB_F16 or RKB_BF16.  rows == 0 gives zeros.
+ * was or as its checkpoint, as above.  A checkpoint is loaded whole into the workspace first, as the 16-bit matrix that it
+ * stands for.  dtype: RKB_F16 or RKB_BF16.  rows == 0 gives zeros.
  * ckpt of the workspace call: whether x is given as its checkpoint.
  */
 int rkb_weight_grad_workspace(int dtype, int64_t rows, int64_t n, int64_t k, int ckpt, int aligned, size_t *bytes);
@@ -126,9 +127,11 @@ int rkb_gated_fwd(int dtype, int act, int keep, int64_t rows, int64_t d, int64_t
  * Its backward, from dh [rows, f] and what the forward kept (RKB_KEEP_NONE makes g and u again from x, wg
  * and wu): with dg = dh u act'(g) and du = dh act(g),
  *   dx = dg wg + du wu,  dwg = dg^T x,  dwu = du^T x.
- * dg and du enter the products rounded to dtype.  dx [rows, d], dwg and dwu [f, d] of dtype, dx or
- * both of dwg and dwu may be NULL.  h: NULL, or [rows, f] of dtype, receives act(g) u of the same g and u, for the weight
- * gradient of the layer that follows.  rows == 0 gives zero weight gradients.
+ * dg and du enter the products rounded to dtype.  That adds as much error to the gradients as their own rounding, and a dg or
+ * du beyond dtype's largest value (65504 in f16) is an infinity, one below its smallest 0.  Where there are at most 4096
+ * of them (rows * f), what the rounding leaves over enters as well, which saves the error but not the range.  dx [rows, d],
+ * dwg and dwu [f, d] of dtype, dx or both of dwg and dwu may be NULL.  h: NULL, or [rows, f] of dtype, receives
+ * act(g) u of the same g and u, for the weight gradient of the layer that follows.  rows == 0 gives zero weight gradients.
  */
 int rkb_gated_bwd_workspace(int dtype, int keep, int64_t rows, int64_t d, int64_t f, int aligned, size_t *bytes);
 int rkb_gated_bwd(int dtype, int act, int keep, int64_t rows, int64_t d, int64_t f, const void *dh,

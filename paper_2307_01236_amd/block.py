@@ -146,7 +146,7 @@ def rkb_ckpt8_load(c: Ckpt8) -> torch.Tensor:
 
 def rkb_weight_grad(dy, x) -> torch.Tensor:
     """dy^T x [n, k], the weight gradient of a linear layer y = x W^T, from dy [..., n] and its input x
-    [..., k], kept as it was or as a Ckpt8.  16-bit types."""
+    [..., k], kept as it was or as a Ckpt8 (loaded whole into a workspace).  16-bit types."""
     return _native().weight_grad(dy, x)
 
 
@@ -160,5 +160,5 @@ def rkb_gated_fwd(x, wg, wu, act: str = "silu", keep: str = "none"):
 
 def rkb_gated_bwd(dh, x, wg, wu, act: str = "silu", kept=None, want_h: bool = False):
     """(dx, dwg, dwu, h) from dh and what rkb_gated_fwd kept; h (None unless want_h) is act(g) * u again, for the
-    weight gradient of the layer that follows."""
+    weight gradient of the layer that follows.  The gradients of g and u are rounded to x's type on the way."""
     return _native().gated_bwd(dh, x, wg, wu, _choice(_ACT, act, "rkb_gated_bwd", "activation"), kept, want_h)

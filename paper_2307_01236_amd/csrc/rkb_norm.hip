@@ -4,7 +4,7 @@
 // checkpoint) and writes dx.  A row stays in the registers of LANES lanes between the sums over it, so
 // each matrix is read once; the mean is formed first and the variance from differences to
 // it, which costs no second read and loses no digits where the mean is large.  At 16384 x 4096 (bf16) the
-// forward takes 54 us (4.9 TB/s), the backward 79 (5.1 TB/s) and 5 for the columns; one row of 1024 takes 2.7 us.
+// forward takes 55 us (4.8 TB/s), the backward 78 (5.2 TB/s) and 5 for the columns; one row of 1024 takes 2.7 us.
 #include <algorithm>
 #include <cmath>
 #include <type_traits>
@@ -319,9 +319,13 @@ __global__ __launch_bounds__(256) void k_norm_cols(int blocks, int cols, const f
     out[blockIdx.x * 64 + c] = (W)all;
 }
 
-// Blocks of a backward pass.  Each leaves a partial row of sums where columns' sums are wanted, so few are better
-// that still keep 8 waves on every compute unit, and each should have several rows in turn: 1000 x 4096 (bf16)
-// took 27 us with 500 blocks of one row at a time.
+// Blocks of a backward pass.  Each leaves a partial row of sums where columns' sums are wanted, so few are better: two of 256
+// lanes or one of 1024 on every compute unit, and each should have several rows in turn: 1000 x 4096 (bf16)
+// took 27 us with 500 blocks of one row at a time.  Not every layout's registers allow that.  64 lanes of 4 chunks in 16
+// bits (1025 to 2048 columns) take 264 to 276, one block a compute unit, and half of the blocks wait: 8192 x 1280 (bf16) takes
+// 37 us and 8192 x 2048 36, where 8192 x 1024 takes 18 and 8192 x 4096 43.  1024 lanes of 2 chunks in 16 bits and of 4 in 32
+// (more than 8192 columns) do not fit 128: 28 to 60 and some 170 registers spill in the row loop, and 2048 x 16384 takes
+// 86 us in bf16 (2.4 TB/s) and 173 in 32 bits.
 int64_t bwd_blocks(int64_t rows, int rows_per_block, int block, bool want)
 {
     const int64_t need = (rows + rows_per_block - 1) / rows_per_block, most = block == 256 ? 512 : 256;
