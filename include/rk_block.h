@@ -10,7 +10,9 @@
  *     16-bit activation), and backward steps that read them;
  *   - the gated feed-forward block h = act(x Wg^T) * (x Wu^T), whose backward reads
  *     g = x Wg^T and u = x Wu^T as they were, from 8-bit checkpoints, or makes them again;
- *   - the weight gradient of a linear layer whose input was kept in 8 bits.
+ *   - the weight gradient of a linear layer whose input was kept in 8 bits;
+ *   - attention to keys and values of another length, forward and backward, with a learned bias by
+ *     relative position, and from a cache of keys and values in 8 bits.
  *
  * Matrices are row-major with neighbouring columns adjacent; `..._stride` is the distance
  * between rows in elements (not read for matrices of at most one row): at least the number of columns
@@ -57,6 +59,10 @@ enum { RKB_KEEP_NONE = 0, RKB_KEEP_FULL = 1, RKB_KEEP_8BIT = 2, RKB_KEEP_16BIT =
 #define RKB_MAX_ROWS ((int64_t)1 << 30)                /* most rows and ...              */
 #define RKB_MAX_COLS ((int64_t)1 << 24)                /* ... columns of any matrix      */
 #define RKB_GROUP 32                                   /* columns that share a scale     */
+#define RKB_MAX_DIM 256                                /* widest head of an attention    */
+#define RKB_MAX_TOKENS ((int64_t)1 << 28)              /* most queries or keys of a sequence */
+#define RKB_MAX_BUCKETS 128                            /* most buckets of a bias and ... */
+#define RKB_MAX_DISTANCE 1024                          /* ... its largest max_distance   */
 
 /*
  * Layer norm of each row: y = (x - mean) rstd w + b with mean and (biased) variance of the
@@ -139,6 +145,104 @@ int rkb_gated_bwd(int dtype, int act, int keep, int64_t rows, int64_t d, int64_t
                   const void *wu, int64_t wu_stride, const void *g, const void *u, const uint8_t *ge,
                   const uint8_t *ue, void *dx, int64_t dx_stride, void *dwg, void *dwu, int64_t dw_stride, void *h,
                   int64_t h_stride, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Attention.  A rkb_heads is a [batch, rows, heads, dim] tensor whose neighbouring columns are adjacent, with its strides in
+ * elements (those of a size of one are not read): 0 to 2^40 for an input; an output's elements must not overlap.
+ */
+typedef struct rkb_heads {
+    void *p;
+    int64_t batch, row, head;
+} rkb_heads;
+
+/*
+ * What a call attends to what.  For each sequence b and head h, whose keys and values are those of head h / (heads / kv_heads):
+ *   s_ij = scale q_i . k_j + table[bucket(j - pos_i), h]   for each key j that lives for query i,
+ *   lse_i = ln sum_j e^s_ij,  p_ij = e^(s_ij - lse_i),  o_i = sum_j p_ij v_j.
+ * pos_i = first + firsts[b] + i is where query i stands among the keys (within 2^30; beyond, as if there).
+ * Key j lives if j < lens[b] (taken to lie in 0 .. k_rows), mask[b * mask_stride + j] is not 0 and, where `causal`, j <= pos_i.
+ * lens, firsts and mask are device memory, or NULL: all keys, 0, all keys.  A query without live keys has o_i = 0 and lse_i = -inf.
+ * What lies at a key that lives for no query (a length or the mask says so) is not looked at, whatever it is; one that
+ * only `causal` hides from a query counts 0 times its value there, which is NaN for an infinity or NaN.
+ *
+ * table: [buckets, heads] of type table_dtype (dtype or RKB_F32), or NULL for none.  Of the relative position n = j - pos_i, a two-sided
+ * bias has half of its buckets for n <= 0 and the other half for n > 0, by distance |n|; a one-sided one has all
+ * for the distance max(-n, 0).  Of nb buckets of a side the first e = nb / 2 (rounded down) are one distance each; from e on,
+ * the bucket is e + floor((nb - e) ln(d / e) / ln(max_distance / e)), at most nb - 1, as exact arithmetic has it.
+ * nb is 2 .. RKB_MAX_BUCKETS (and so is twice nb, where two-sided), e < max_distance <= RKB_MAX_DISTANCE.  An entry of -inf hides its keys as a mask
+ * does; a finite one beyond 2e38 counts as 2.08e38.
+ *
+ * dtype: RKB_F16 or RKB_BF16; 1 <= dim <= RKB_MAX_DIM; heads a multiple of kv_heads; 0 < scale < inf.
+ */
+typedef struct rkb_attn {
+    int dtype, causal;
+    int64_t batch, q_rows, k_rows, heads, kv_heads, dim;
+    float scale;
+    int64_t first;
+    const int32_t *firsts, *lens;
+    const uint8_t *mask;
+    int64_t mask_stride;
+    const void *table;
+    int table_dtype, buckets, max_distance, two_sided;
+} rkb_attn;
+
+/*
+ * A cache of keys and values in 8 bits.  For each sequence and head, RKB_GROUP neighbouring tokens (a block) share 2^e, the least power of
+ * two with max|x| <= 127 * 2^e (e >= -126), over all their columns; values are kept as in the 8-bit checkpoints above:
+ * round-half-even(x 2^-e), at most 63 where 64 * 2^e would pass dtype's largest finite value, and exactly what they stand for in dtype.
+ *   codes [2, batch, kv_heads, room, ld]: keys, then values; room = tokens rounded up to RKB_GROUP, ld = dim rounded up to 16,
+ *         16-byte aligned; columns past dim are 0
+ *   exps  [2, batch, kv_heads, room / RKB_GROUP]: e + 127; 255 for a block that stands for NaN as a whole, because it took an infinity
+ *         or NaN; 0 for a block that stands for zeros, as memory cleared beforehand does
+ */
+typedef struct rkb_kv8 {
+    int8_t *codes;
+    uint8_t *exps;
+    int64_t tokens;  /* most of a sequence */
+} rkb_kv8;
+
+/*
+ * Writes k and v [batch, rows, kv_heads, dim] into a cache: row i of sequence b becomes its token first + firsts[b] + i, if i < counts[b]
+ * (NULL: all rows).  Rows that would lie before token 0 or behind the last are not written.  A block that holds
+ * tokens before the first one written keeps them: where the new ones need a larger step, 2^e', their codes become
+ * round-half-even(code 2^(e - e')).  What a block held from the first token written on is dropped: the places behind the
+ * last one written are zeros.  Other blocks stay as they were.
+ */
+int rkb_kv8_write(int dtype, int64_t batch, int64_t rows, int64_t kv_heads, int64_t dim, const rkb_heads *k, const rkb_heads *v,
+                  int64_t first, const int32_t *firsts, const int32_t *counts, const rkb_kv8 *cache, void *stream);
+
+/* The values that a cache stands for: k and v [batch, tokens, kv_heads, dim], either may have p NULL. */
+int rkb_kv8_load(int dtype, int64_t batch, int64_t kv_heads, int64_t dim, const rkb_kv8 *cache, const rkb_heads *k,
+                 const rkb_heads *v, void *stream);
+
+/*
+ * Attention forward.  q and o [batch, q_rows, heads, dim]; k and v [batch, k_rows, kv_heads, dim], or both NULL and `cache` given, with
+ * k_rows <= cache->tokens (codes of tokens from k_rows on are not read).  o32: NULL, or [batch, q_rows, heads, dim] (contiguous, 16-byte
+ * aligned) receives o in 32 bits, as it was summed; lse: NULL, or [batch, heads, q_rows].  Probabilities are rounded to dtype on their way into the
+ * second product, relative to the row's largest (within 2^8), so that what is lost of one is at most as much as its
+ * rounding; sums are not.
+ * `aligned` of the workspace call: q, k and v start at multiples of 16 bytes, dim and all their strides are multiples of 8 and
+ * row strides at most 2^22; 0 asks for room for copies that are.
+ */
+int rkb_attn_fwd_workspace(const rkb_attn *a, int cache, int aligned, size_t *bytes);
+int rkb_attn_fwd(const rkb_attn *a, const rkb_heads *q, const rkb_heads *k, const rkb_heads *v, const rkb_kv8 *cache,
+                 const rkb_heads *o, float *o32, float *lse, void *workspace, size_t ws_bytes, void *stream);
+
+/*
+ * Its backward, from do [batch, q_rows, heads, dim] and what the forward kept: lse, and o as it was returned (o) or in 32 bits
+ * (o32); with neither (o, o32 and lse NULL) they are made again.  With dp_ij = do_i . v_j and ds_ij = p_ij (dp_ij - do_i . o_i),
+ *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i,
+ *   dtable[c, h] = sum of ds_ij over the i, j of bucket c and all sequences,
+ * dk and dv summed over the heads that share them too.  p and ds enter the products rounded to dtype; in f16, scaled
+ * so that neither overflows nor loses bits that its size would not lose in any type.  Taking o rounded instead of in 32 bits costs about
+ * one more rounding of dtype in do_i . o_i, which is seen in a 32-bit dtable only.
+ * dq, dk, dv of dtype, each may have p NULL (dk and dv both); dtable of table_dtype, NULL for none.
+ * aligned: as above, of do too.
+ */
+int rkb_attn_bwd_workspace(const rkb_attn *a, int again, int aligned, size_t *bytes);
+int rkb_attn_bwd(const rkb_attn *a, const rkb_heads *d_o, const rkb_heads *q, const rkb_heads *k, const rkb_heads *v,
+                 const rkb_heads *o, const float *o32, const float *lse, const rkb_heads *dq, const rkb_heads *dk,
+                 const rkb_heads *dv, void *dtable, void *workspace, size_t ws_bytes, void *stream);
 
 /* Short English description of an RKB_* code. */
 const char *rkb_strerror(int code);

@@ -1,8 +1,8 @@
 """Python binding of librkblock (include/rk_block.h): argument marshalling only.
 
 Operators of the blocks that a re-materialization schedule runs, on torch tensors of the GPU:
-layer norm, checkpoints of activations in 8 bits, the gated feed-forward block and a linear
-layer's weight gradient.  Every step runs in the HIP library; the marshalling itself is native
+layer norm, checkpoints of activations in 8 bits, the gated feed-forward block, a linear
+layer's weight gradient, and attention (with a bias by relative position, and over a cache of keys and values in 8 bits).  Every step runs in the HIP library; the marshalling itself is native
 (csrc/rkb_bind.cpp), because the smallest calls take no longer than marshalling in Python
 does.  The functions keep the C names; non-OK return codes raise ``RKBError``, as do tensors that
 the C call cannot take (off the GPU, on different devices, of different types, or with columns
@@ -35,15 +35,42 @@ RKB_MAX_NORM_COLS = 16384
 RKB_MAX_ROWS = 1 << 30
 RKB_MAX_COLS = 1 << 24
 RKB_GROUP = 32
+RKB_MAX_DIM = 256
+RKB_MAX_TOKENS = 1 << 28
+RKB_MAX_BUCKETS = 128
+RKB_MAX_DISTANCE = 1024
 
 EXPORTS = ("rkb_layer_norm_fwd", "rkb_layer_norm_bwd_workspace", "rkb_layer_norm_bwd", "rkb_ckpt8_save",
            "rkb_ckpt8_load", "rkb_weight_grad_workspace", "rkb_weight_grad", "rkb_gated_fwd_workspace",
-           "rkb_gated_fwd", "rkb_gated_bwd_workspace", "rkb_gated_bwd", "rkb_strerror")
+           "rkb_gated_fwd", "rkb_gated_bwd_workspace", "rkb_gated_bwd", "rkb_kv8_write", "rkb_kv8_load",
+           "rkb_attn_fwd_workspace", "rkb_attn_fwd", "rkb_attn_bwd_workspace", "rkb_attn_bwd", "rkb_strerror")
 
 _ACT = {"silu": RKB_SILU, "gelu": RKB_GELU}
 _KEEP = {"none": RKB_KEEP_NONE, "full": RKB_KEEP_FULL, "8bit": RKB_KEEP_8BIT, "16bit": RKB_KEEP_16BIT}
 
 _lib = _bind = None
+
+
+class CHeads(C.Structure):
+    """rkb_heads: a [batch, rows, heads, dim] tensor's pointer and strides in elements."""
+
+    _fields_ = [("p", C.c_void_p), ("batch", C.c_int64), ("row", C.c_int64), ("head", C.c_int64)]
+
+
+class CAttn(C.Structure):
+    """rkb_attn: what a call attends to what."""
+
+    _fields_ = [("dtype", C.c_int), ("causal", C.c_int), ("batch", C.c_int64), ("q_rows", C.c_int64), ("k_rows", C.c_int64),
+                ("heads", C.c_int64), ("kv_heads", C.c_int64), ("dim", C.c_int64), ("scale", C.c_float), ("first", C.c_int64),
+                ("firsts", C.c_void_p), ("lens", C.c_void_p), ("mask", C.c_void_p), ("mask_stride", C.c_int64),
+                ("table", C.c_void_p), ("table_dtype", C.c_int), ("buckets", C.c_int), ("max_distance", C.c_int),
+                ("two_sided", C.c_int)]
+
+
+class CKv8(C.Structure):
+    """rkb_kv8: a cache's codes and exps, and the most tokens of a sequence."""
+
+    _fields_ = [("codes", C.c_void_p), ("exps", C.c_void_p), ("tokens", C.c_int64)]
 
 
 def load():
@@ -68,6 +95,13 @@ def load():
         lib.rkb_gated_fwd.argtypes = [i, i, i, l, l, l] + [p, l] * 4 + [p] * 4 + [p, sz, p]
         lib.rkb_gated_bwd_workspace.argtypes = [i, i, l, l, l, i, szp]
         lib.rkb_gated_bwd.argtypes = [i, i, i, l, l, l] + [p, l] * 4 + [p] * 4 + [p, l, p, p, l, p, l, p, sz, p]
+        heads, attn, kv8 = C.POINTER(CHeads), C.POINTER(CAttn), C.POINTER(CKv8)
+        lib.rkb_kv8_write.argtypes = [i, l, l, l, l, heads, heads, l, p, p, kv8, p]
+        lib.rkb_kv8_load.argtypes = [i, l, l, l, kv8, heads, heads, p]
+        lib.rkb_attn_fwd_workspace.argtypes = [attn, i, i, szp]
+        lib.rkb_attn_fwd.argtypes = [attn, heads, heads, heads, kv8, heads, p, p, p, sz, p]
+        lib.rkb_attn_bwd_workspace.argtypes = [attn, i, i, szp]
+        lib.rkb_attn_bwd.argtypes = [attn] + [heads] * 5 + [p, p] + [heads] * 3 + [p, p, sz, p]
         lib.rkb_strerror.argtypes = [i]
         lib.rkb_strerror.restype = C.c_char_p
         for n in EXPORTS:
@@ -104,6 +138,41 @@ class Ckpt8:
         return self.codes.numel() + self.exps.numel()
 
 
+class Kv8:
+    """A cache of keys and values in 8 bits: codes [2, batch, heads, tokens rounded up to 32, width rounded up to 16] (int8; keys, then
+    values), one exponent byte for each 32 tokens of a head, the shape (batch, tokens, heads, width) and the 16-bit type of what it holds."""
+
+    __slots__ = ("codes", "exps", "shape", "dtype")
+
+    def __init__(self, codes, exps, shape, dtype):
+        self.codes, self.exps, self.shape, self.dtype = codes, exps, torch.Size(shape), dtype
+
+    @classmethod
+    def zeros(cls, batch: int, tokens: int, heads: int, dim: int, dtype=torch.bfloat16, device="cuda") -> "Kv8":
+        """An empty cache, for up to `tokens` tokens of each sequence."""
+        blocks, ld = -(-tokens // RKB_GROUP), -(-dim // 16) * 16
+        return cls(torch.zeros(2, batch, heads, blocks * RKB_GROUP, ld, dtype=torch.int8, device=device),
+                   torch.zeros(2, batch, heads, blocks, dtype=torch.uint8, device=device), (batch, tokens, heads, dim), dtype)
+
+    @property
+    def device(self):
+        return self.codes.device
+
+    def nbytes(self) -> int:
+        return self.codes.numel() + self.exps.numel()
+
+
+class RelBias:
+    """A learned bias by relative position: table [buckets, heads] (of the queries' type or 32 bits).  two_sided: half of the buckets for
+    keys up to the query and half for those behind it, else all for those up to it.  Half of a side's buckets are
+    one distance each, the others grow with its logarithm up to max_distance."""
+
+    __slots__ = ("table", "max_distance", "two_sided")
+
+    def __init__(self, table, max_distance: int = 128, two_sided: bool = True):
+        self.table, self.max_distance, self.two_sided = table, max_distance, two_sided
+
+
 def _native():
     global _bind
     if _bind is None:
@@ -111,7 +180,7 @@ def _native():
         if not os.path.exists(BIND_PATH):
             raise ImportError(f"{BIND_PATH} is missing: build it with paper_2307_01236_amd.build.build()")
         bind = importlib.import_module("paper_2307_01236_amd._rkblock")
-        bind.init(RKBError, Ckpt8, (torch.float32, torch.float16, torch.bfloat16))
+        bind.init(RKBError, Ckpt8, (torch.float32, torch.float16, torch.bfloat16), Kv8, RelBias)
         _bind = bind
     return _bind
 
@@ -162,3 +231,39 @@ def rkb_gated_bwd(dh, x, wg, wu, act: str = "silu", kept=None, want_h: bool = Fa
     """(dx, dwg, dwu, h) from dh and what rkb_gated_fwd kept; h (None unless want_h) is act(g) * u again, for the
     weight gradient of the layer that follows.  The gradients of g and u are rounded to x's type on the way."""
     return _native().gated_bwd(dh, x, wg, wu, _choice(_ACT, act, "rkb_gated_bwd", "activation"), kept, want_h)
+
+
+def rkb_attn_fwd(q, k, v=None, scale: float | None = None, lens=None, mask=None, causal: bool = False, first=0, bias=None,
+                 keep: str = "none"):
+    """(o, kept): attention of q [batch, queries, heads, width] to k and v [batch, keys, key heads, width], or to a Kv8 given as k.
+    Types are 16-bit, heads a multiple of the key heads, which neighbouring heads share, and scale width ** -0.5 unless given.
+
+    lens (int32 [batch]) is each sequence's number of keys, mask ([batch, keys], bool) says which keys take part, and with causal a
+    query sees the keys up to its own position: first + its row; first is an int or an int32 tensor [batch].  bias is
+    a RelBias.  A query that sees no key has o = 0 (and log-sum -inf).  kept is what rkb_attn_bwd takes: None for
+    keep="none", (o, lse) for "16bit", and for "full" o in 32 bits in its place; lse is [batch, heads, queries] in 32 bits."""
+    where = "rkb_attn_fwd"
+    kind = _choice(_KEEP, keep, where, "keep")
+    if kind == RKB_KEEP_8BIT:
+        raise RKBError(RKB_E_INVAL, f"{where} (keep)")
+    return _native().attn_fwd(q, k, v, scale, lens, mask, causal, first, bias, kind)
+
+
+def rkb_attn_bwd(do, q, k, v, kept=None, scale: float | None = None, lens=None, mask=None, causal: bool = False, first=0,
+                 bias=None):
+    """(dq, dk, dv, dtable) from do and what rkb_attn_fwd kept for the same arguments (None: the forward's output is made again); dtable
+    is the gradient of the bias's table, None without one.  Sums are in 32 bits and in a fixed order; probabilities and the scores'
+    gradients are rounded to q's type on their way into the products."""
+    return _native().attn_bwd(do, q, k, v, kept, scale, lens, mask, causal, first, bias)
+
+
+def rkb_kv8_write(cache: Kv8, k, v, first=0, counts=None) -> None:
+    """Writes k and v [batch, rows, key heads, width] into a cache from token `first` of each sequence on (an int, or an int32 tensor
+    [batch]); counts (int32 [batch]) is each sequence's number of rows, all unless given.  Tokens before stay, rounded again
+    where a block of 32 needs a larger step; rows outside the cache are dropped."""
+    _native().kv8_write(cache, k, v, first, counts)
+
+
+def rkb_kv8_load(cache: Kv8):
+    """(k, v): what a cache stands for, [batch, tokens, key heads, width] of its type."""
+    return _native().kv8_load(cache)

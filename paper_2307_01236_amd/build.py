@@ -8,6 +8,8 @@ import shutil
 import subprocess
 import sys
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -17,7 +19,8 @@ SOURCES = ["rk_api.hip", "rk_kernels.hip", "rk_tile.hip", "rk_host.cpp"]
 CALIB_LIB = os.path.join(PKG, "librkcalib.so")
 CALIB_SOURCES = ["rk_calib.hip"]
 BLOCK_LIB = os.path.join(PKG, "librkblock.so")
-BLOCK_SOURCES = ["rkb_norm.hip", "rkb_ckpt.hip", "rkb_gemm.hip"]
+BLOCK_SOURCES = ["rkb_norm.hip", "rkb_ckpt.hip", "rkb_gemm.hip", "rkb_attn.hip", "rkb_attn_bwd.hip", "rkb_attn_api.hip",
+                 "rkb_kv8.hip"]
 BIND_LIB = os.path.join(PKG, "_rkblock.so")
 BIND_SOURCE = "rkb_bind.cpp"
 ARCH = "gfx950"
@@ -52,8 +55,12 @@ def _run(cmd, out: str, verbose: bool) -> str:
 
 
 def _compile(sources, out: str, verbose: bool) -> str:
-    srcs = [os.path.join(CSRC, s) for s in sources]
-    return _run([hipcc(), *HIPCC_FLAGS, "-I", os.path.join(ROOT, "include"), "-I", CSRC, *srcs], out, verbose)
+    """Every source to an object of its own, side by side (a single call of hipcc takes them in turn), then linked."""
+    with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(os.cpu_count()) as pool:
+        flags = [f for f in HIPCC_FLAGS if f != "-shared"]
+        objects = list(pool.map(lambda s: _run([hipcc(), *flags, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c",
+                                                os.path.join(CSRC, s)], os.path.join(tmp, s + ".o"), verbose), sources))
+        return _run([hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", *objects], out, verbose)
 
 
 def _compile_binding(verbose: bool) -> str:

@@ -1,0 +1,334 @@
+// What the attention kernels share (rkb_attn.hip, rkb_attn_bwd.hip): the layout of tiles in LDS, how they are
+// filled, the matrix instructions' fragments, which keys live, and the bias by relative position.
+//
+// Every kernel has a stationary side, whose 32 rows a wave holds as columns of 32 x 32 x 16 matrix instructions, and
+// a streamed side that passes through LDS in tiles of rows.  A product "streamed x stationary" (scores, dp) leaves a
+// lane with one stationary row and 16 of 32 streamed ones, so that softmax sums are sums within a
+// lane and one exchange; its registers are, converted, the right operand of the next product (o, dq, dk, dv: sums over streamed
+// rows), whose left operand is the tile read through LDS's transposing read.  That operand's k order is the
+// one the registers have: lanes 0 to 31 hold the rows 0-3 and 8-11 of each 16, lanes 32 to 63 the rows 4-7 and 12-15.
+#pragma once
+#include "rkb_common.h"
+#include "rkb_tile.h"
+
+namespace rkb {
+
+using f32x16 = vec<float, 16>;
+
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.693147180559945309417f;
+constexpr float NEG_INF = -__builtin_inff();
+constexpr int MAX_BUCKETS = RKB_MAX_BUCKETS, MAX_FAR = RKB_MAX_DISTANCE;
+
+__device__ inline f32x16 mma32(frag<bf16> a, frag<bf16> b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+__device__ inline f32x16 mma32(frag<f16> a, frag<f16> b, f32x16 c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// Row (of 32) that a lane's register r of a product holds: 8 (r / 4) + r % 4 + this.
+__device__ inline int half_row(int lane) { return lane / 32 * 4; }
+
+// Sum, or maximum, of the two halves' values of one column.
+__device__ inline float half_sum(float v)
+{
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(a[0]) + __uint_as_float(a[1]);
+}
+__device__ inline float half_max(float v)
+{
+    const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
+// ------------------------------------------------------------------ arguments
+
+struct heads_at {  // a [batch, rows, heads, width] tensor; strides in elements
+    char *p;
+    int64_t b, t, h;
+    template <class T>
+    __device__ T *at(int64_t bi, int64_t ti, int64_t hi) const
+    {
+        return (T *)p + bi * b + ti * t + hi * h;
+    }
+};
+
+struct bias_table {
+    const void *table;  // [buckets, heads], NULL: no bias
+    int f32;            // 32-bit, else of the operands' type
+    int sides, count;   // buckets of a side
+    int far;            // the least distance of a side's last bucket
+    int border[MAX_BUCKETS - 1];  // the least distance of buckets 1 ..
+};
+
+struct attn_in {
+    int B, Q, T, H, K, G, D;
+    int causal;
+    float scale, c;  // c = scale log2(e)
+    int64_t first;
+    const int32_t *firsts, *lens;
+    const uint8_t *mask;
+    int64_t mask_stride;
+    heads_at q, k, v;
+    const int8_t *codes;  // [2, B, K, room, ld], or NULL
+    const uint8_t *exps;  // [2, B, K, room / 32]
+    int64_t room, ld;
+    bias_table bias;
+};
+
+constexpr int FAR_POSITION = 1 << 30;
+
+__device__ inline int len_of(const attn_in &p, int b) { return p.lens ? min(max(p.lens[b], 0), p.T) : p.T; }
+
+// The position of a sequence's first query: past 2^30 either way, all keys are as far.
+__device__ inline int first_of(const attn_in &p, int b)
+{
+    const int64_t at = p.first + (p.firsts ? p.firsts[b] : 0);
+    return (int)min(max(at, (int64_t)-FAR_POSITION), (int64_t)FAR_POSITION);
+}
+
+// Workgroups go to the 8 dies in turn; each die gets a run of neighbouring work, so that its L2 holds what they share.
+__device__ inline int die_order(int block, int total)
+{
+    const int die = block % 8, share = total / 8, rest = total % 8;
+    return die * share + min(die, rest) + block / 8;
+}
+
+// ------------------------------------------------------------------ tiles in LDS
+//
+// A tile has rows of DP (64, 128 or 256) 16-bit columns without gaps.  The 16-byte chunks of row r are permuted
+// by fold(r) (xor): the 16 rows that a fragment's lanes read at one chunk fall into different banks, and so do
+// the 64-byte pieces of the 4 rows that a transposing read takes together.
+
+template <int DP>
+struct lay {
+    static_assert(DP == 64 || DP == 128 || DP == 256);
+    static constexpr int PITCH = DP * 2, CHUNKS = DP / 8;
+    static __device__ int fold(int r)
+    {
+        return DP == 64 ? (r >> 1 & 1) << 2 | (r >> 2 & 3) : (r & 3) << 2 | (r >> 2 & 3);
+    }
+    static __device__ int at(int r, int chunk) { return r * PITCH + (chunk ^ fold(r)) * 16; }
+
+    // Where a lane's part of a fragment of rows lies: row lane % 32, columns 16 c + 8 (lane / 32).. are at this ^ 32 c.
+    static __device__ int rows_place(int lane) { return at(lane % 32, lane / 32); }
+    // Where a lane's part of a transposed fragment lies: columns 32 d.. of rows 16 s.. are at (this ^ 64 d) + 16 s PITCH; `up`: the second read, of rows 8 further on.
+    static __device__ int cols_place(int lane, int up)
+    {
+        const int r = lane / 32 * 4 + lane % 16 / 4 + up * 8;
+        return at(r, lane / 16 % 2 * 2 + lane % 4 / 2) + lane % 2 * 8;
+    }
+    template <class T>
+    static __device__ frag<T> rows(lds_byte *tile, int place, int c, int r0)
+    {
+        return *(__attribute__((address_space(3))) frag<T> *)(tile + (place ^ c * 32) + r0 * PITCH);
+    }
+    template <class T>
+    static __device__ frag<T> cols(lds_byte *tile, const int (&place)[2], int d, int r0)
+    {
+        using half_frag = vec<short, 4>;
+        using lds_half = __attribute__((address_space(3))) half_frag;
+        const half_frag lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_half *)(tile + (place[0] ^ d * 64) + r0 * PITCH));
+        const half_frag hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_half *)(tile + (place[1] ^ d * 64) + r0 * PITCH));
+        return __builtin_bit_cast(frag<T>, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+};
+
+// A tile of ROWS rows filled by WAVES waves with direct copies, 16 bytes a lane.  Rows start at multiples of 16 bytes;
+// their columns past `width` (a multiple of 8) and rows that are not live become zeros.
+template <int DP, int ROWS, int WAVES>
+struct tile_copy {
+    static constexpr int PIECES = ROWS * DP * 2 / PIECE, MINE = PIECES / WAVES, ROWS_EACH = PIECE / (DP * 2);
+    static_assert(PIECES % WAVES == 0);
+    uint32_t off[MINE], wide;  // wide: bit i: piece i's columns exist
+
+    static __device__ int row(int piece, int lane) { return piece * ROWS_EACH + lane / (DP / 8); }
+    __device__ void set(int wave, int lane, int64_t stride, int width)
+    {
+        wide = 0;
+#pragma unroll
+        for (int i = 0; i < MINE; ++i) {
+            const int r = row(wave * MINE + i, lane), chunk = lane % (DP / 8) ^ lay<DP>::fold(r);
+            off[i] = (uint32_t)(r * stride * 2 + chunk * 16);
+            wide |= (uint32_t)(chunk * 8 < width) << i;
+        }
+    }
+    // from: the tile's first row; live: bit r: row r exists; all: every row and column does.
+    __device__ void copy(int wave, int lane, const char *from, uint64_t live, bool all, lds_byte *to) const
+    {
+        if (all) {
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) {
+                uint32_t o = off[i];
+                asm volatile("" : "+v"(o));  // stays 32 bits wide: the copy adds it to a scalar address
+                copy_piece(from + o, to + (wave * MINE + i) * PIECE);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < MINE; ++i) {
+                const bool there = (wide >> i & 1) && (live >> row(wave * MINE + i, lane) & 1);
+                copy_piece(there ? from + off[i] : (const char *)&zero_chunk, to + (wave * MINE + i) * PIECE);
+            }
+        }
+    }
+};
+
+// Eight codes as values of T: whole numbers of up to 8 bits times a power of two, exact.
+template <class T>
+__device__ inline frag<T> code_values(uint32_t lo, uint32_t hi, float step)
+{
+    frag<T> f;
+    const uint32_t u[2] = {lo ^ 0x80808080u, hi ^ 0x80808080u};
+    const bool high = step >= 0x1p114f;  // 128 steps may pass 32 bits' range
+    const float back = high ? 0.0f : -128.0f * step;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float v = (float)(u[i / 4] >> i % 4 * 8 & 0xff);
+        f[i] = (T)(high ? (v - 128.0f) * step : __builtin_fmaf(v, step, back));
+    }
+    return f;
+}
+
+// The same tile from a cache's codes, through registers: load, then (later) put.
+template <class T, int DP, int ROWS, int LANES>
+struct tile_codes {
+    static constexpr int EACH = ROWS * DP / 16 / LANES, SPANS = DP / 16;
+    static_assert(ROWS * DP / 16 % LANES == 0);
+    u32x4 q[EACH];
+    float step[EACH];
+
+    // from: the codes of the tile's first row, exps: those of its blocks; rows are 32-aligned.
+    __device__ void load(int t, const int8_t *from, const uint8_t *exps, int64_t ld, uint64_t live)
+    {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int n = t + i * LANES, r = n / SPANS, span = n % SPANS;
+            const bool there = (live >> r & 1) && span * 16 < ld;
+            q[i] = u32x4{0, 0, 0, 0};
+            step[i] = 0.0f;
+            if (there) {
+                q[i] = *(const u32x4 *)(from + r * ld + span * 16);
+                const uint8_t e = exps[r / RKB_GROUP];
+                step[i] = e == 0 ? 0.0f : step_of(e);
+            }
+        }
+    }
+    __device__ void put(int t, lds_byte *to) const
+    {
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) {
+            const int n = t + i * LANES, r = n / SPANS, span = n % SPANS;
+            using lds_frag = __attribute__((address_space(3))) frag<T>;
+            *(lds_frag *)(to + lay<DP>::at(r, span * 2)) = code_values<T>(q[i][0], q[i][1], step[i]);
+            *(lds_frag *)(to + lay<DP>::at(r, span * 2 + 1)) = code_values<T>(q[i][2], q[i][3], step[i]);
+        }
+    }
+};
+
+// All copies and LDS accesses of this wave, and then of the workgroup, are done.
+__device__ inline void wait_all()
+{
+    __builtin_amdgcn_s_waitcnt(wait_copies(0));
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// A stationary row's fragments: columns 16 c + 8 (lane / 32).. of the row.  Rows are 16-byte aligned, width a multiple of 8.
+template <class T, int DP>
+__device__ inline void load_stationary(frag<T> (&f)[DP / 16], const T *row, int lane, int width, bool there)
+{
+#pragma unroll
+    for (int c = 0; c < DP / 16; ++c) {
+        const int col = c * 16 + lane / 32 * 8;
+        frag<T> z = {};
+        if (there && col < width) z = *(const frag<T> *)(row + col);
+        f[c] = z;
+    }
+}
+
+// Two of a product's register groups as a fragment of 16 rows of the next product.
+template <class T>
+__device__ inline frag<T> to_frag(const f32x16 &s, int half)
+{
+    frag<T> f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = (T)s[half * 8 + i];
+    return f;
+}
+
+// ------------------------------------------------------------------ which keys live
+
+// Bits of the 64 keys from k0 on, for the whole workgroup: those before len whose mask byte (of this lane's key) is set.
+__device__ inline uint64_t keys_alive(const attn_in &p, int k0, int len, uint8_t mask_byte)
+{
+    const int n = len - k0;
+    uint64_t bits = n >= 64 ? ~(uint64_t)0 : n <= 0 ? 0 : ((uint64_t)1 << n) - 1;
+    if (p.mask) bits &= __ballot(mask_byte != 0);
+    return bits;
+}
+__device__ inline uint8_t mask_byte(const attn_in &p, int b, int k, int len)
+{
+    return p.mask && k >= 0 && k < len ? p.mask[b * p.mask_stride + k] : (uint8_t)1;
+}
+
+// Registers of a 32-key piece whose key does not live, or lies behind the lane's query, become `to`.  bits: of the 32 keys;
+// ahead: the query's position less the piece's first key, or INT_MAX where order does not matter.
+__device__ inline void kill_dead(f32x16 &s, uint32_t bits, int ahead, int lane, float to)
+{
+    const int h = half_row(lane);
+    if (bits != ~0u) {
+        const uint32_t w = bits >> h;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = w >> (r / 4 * 8 + r % 4) & 1 ? s[r] : to;
+    }
+    if (__any(ahead < 31)) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = r / 4 * 8 + r % 4 <= ahead - h ? s[r] : to;
+    }
+}
+
+// ------------------------------------------------------------------ bias by relative position
+
+__device__ inline int bucket_of(const bias_table &t, int rel)
+{
+    const int d = t.sides == 2 ? abs(rel) : max(-rel, 0);
+    int n = 0;
+    for (int i = 0; i < t.count - 1; ++i) n += d >= t.border[i];
+    return n + (t.sides == 2 && rel > 0 ? t.count : 0);
+}
+
+// A table entry times log2(e); a finite one stays finite.
+template <class T>
+__device__ inline float table_value(const attn_in &p, int bucket, int h)
+{
+    const int64_t i = (int64_t)bucket * p.H + h;
+    const float v = p.bias.f32 ? ((const float *)p.bias.table)[i] : (float)((const T *)p.bias.table)[i];
+    return fabsf(v) <= 3.0e38f / LOG2E || !finite(fabsf(v)) ? v * LOG2E : copysignf(3.0e38f, v);
+}
+
+// One head's bias by distance: entry n is that of relative position n - far.
+template <class T>
+__device__ inline void fill_bias(float *by_distance, const attn_in &p, int h, int t, int lanes)
+{
+    for (int n = t; n <= 2 * p.bias.far; n += lanes) by_distance[n] = table_value<T>(p, bucket_of(p.bias, n - p.bias.far), h);
+}
+
+// Adds a head's bias to a 32-key piece of scores: key0 the piece's first key, pos the lane's query; pos_lo and pos_hi
+// bound the wave's.  s = s c + bias.
+__device__ inline void add_bias(f32x16 &s, float c, const float *by_distance, int far, int key0, int pos, int pos_lo, int pos_hi, int lane)
+{
+    if (key0 - pos_hi >= far || key0 + 31 - pos_lo <= -far) {
+        const float b = by_distance[key0 - pos_hi >= far ? 2 * far : 0];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], c, b);
+    } else {
+        const int d = key0 + half_row(lane) - pos + far;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], c, by_distance[min(max(d + r / 4 * 8 + r % 4, 0), 2 * far)]);
+    }
+}
+
+}  // namespace rkb

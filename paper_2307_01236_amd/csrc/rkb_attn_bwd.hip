@@ -1,0 +1,651 @@
+// Attention backward (rk_block.h).  Probabilities are made again from the row sums that the forward left: dq by a kernel like the
+// forward, with queries stationary, dk and dv by one with keys stationary, so that every sum has one owner and a
+// fixed order.  That makes the scores and dp twice, 7 products instead of 5, and needs no atomics and no [queries, keys] matrix.
+#include <algorithm>
+#include <climits>
+
+#include "rkb_attn.h"
+#include "rkb_attn_args.h"
+
+namespace rkb {
+namespace {
+
+constexpr int ROWS = 128, WAVES = 4;  // stationary rows and waves of a workgroup
+
+struct bwd_in {
+    heads_at d_o, o;
+    const float *o32, *lse;
+    float *delta, *lse2;     // [B, H, stats_rows]: do . o, and lse in steps of log2 (inf: a row without keys, or none)
+    uint32_t *norms;         // f16: [B, K, 2]: bits of the largest |do|^2 and |v|^2
+    int64_t stats_rows;
+    heads_at dq, dk, dv;
+    float *dq_part, *dk_part, *dv_part;  // [splits, rows, D] each, where there are several
+    float *row_part;         // [splits, B, H, stats_rows]: parts of the sums of ds, where there are several
+    float *table_part;       // [H, B key tiles splits, buckets]
+    int wide;                // bit 0: dq, 1: dk and dv take 8-byte stores
+};
+
+// ds enters the products in T.  In f16 a ds of many keys falls below the range (1/4096 of a gradient of 1e-2 is 2e-6), so it is
+// scaled by a power of two from |ds| <= 2 |do| |v|, whose largest values a pass over both finds.
+template <class T>
+__device__ inline float ds_scale(const bwd_in &g, const attn_in &p, int b, int kv)
+{
+    if constexpr (!std::is_same_v<T, f16>) return 1.0f;
+    const uint32_t *n = g.norms + 2 * ((int64_t)b * p.K + kv);
+    const float x = __uint_as_float(n[0]), y = __uint_as_float(n[1]);
+    if (!(x > 0.0f && y > 0.0f && finite(x) && finite(y))) return 1.0f;
+    const float e = 12.0f - ceilf(0.5f * (__builtin_amdgcn_logf(x) + __builtin_amdgcn_logf(y)));
+    return two_to((int)fminf(fmaxf(e, -100.0f), 100.0f));
+}
+// p <= 1 likewise, by a fixed power of two.
+template <class T>
+constexpr float P_LIFT = std::is_same_v<T, f16> ? 14.0f : 0.0f;
+
+// ------------------------------------------------------------------ row sums and norms
+
+__device__ inline float block_max(float v, float *shared)
+{
+#pragma unroll
+    for (int i = 1; i < WAVE; i *= 2) v = fmaxf(v, __shfl_xor(v, i));
+    if (threadIdx.x % WAVE == 0) shared[threadIdx.x / WAVE] = v;
+    __syncthreads();
+    return fmaxf(fmaxf(shared[0], shared[1]), fmaxf(shared[2], shared[3]));
+}
+
+__global__ __launch_bounds__(256) void k_clear(uint32_t *p, int n)
+{
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) p[i] = 0;
+}
+
+// delta = do . o and lse2 of 64 rows of a head; 16 lanes a row.
+template <class T>
+__global__ __launch_bounds__(256) void k_attn_delta(attn_in p, bwd_in g)
+{
+    __shared__ float shared[4];
+    const int chunks = (int)(g.stats_rows / 64), bh = blockIdx.x / chunks, i0 = (blockIdx.x - bh * chunks) * 64;
+    const int b = bh / p.H, h = bh - b * p.H, lane = threadIdx.x % 16;
+    float most = 0.0f;
+    for (int k = 0; k < 4; ++k) {
+        const int i = i0 + k * 16 + threadIdx.x / 16;
+        float sum = 0.0f, norm = 0.0f;
+        if (i < p.Q) {
+            const T *d = g.d_o.at<T>(b, i, h), *o = g.o32 ? nullptr : g.o.at<T>(b, i, h);
+            const float *o32 = g.o32 ? g.o32 + (((int64_t)b * p.Q + i) * p.H + h) * p.D : nullptr;
+            for (int c = lane * 8; c < p.D; c += 128) {
+                float dv[8], ov[8];
+                load8<T>(d + c, p.D - c, dv);
+                if (o32)
+                    load8<float>(o32 + c, p.D - c, ov);
+                else
+                    load8<T>(o + c, p.D - c, ov);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    sum = __builtin_fmaf(dv[e], ov[e], sum);
+                    norm = __builtin_fmaf(dv[e], dv[e], norm);
+                }
+            }
+        }
+        sum = lane_sum<16>(sum);
+        most = fmaxf(most, lane_sum<16>(norm));
+        if (lane == 0) {
+            const int64_t at = (int64_t)bh * g.stats_rows + i;
+            const float l = i < p.Q ? g.lse[(int64_t)bh * p.Q + i] : NEG_INF;
+            g.delta[at] = l == NEG_INF ? 0.0f : sum;
+            g.lse2[at] = l == NEG_INF ? -NEG_INF : l * LOG2E;
+        }
+    }
+    if constexpr (std::is_same_v<T, f16>) {
+        most = block_max(most, shared);
+        if (threadIdx.x == 0) atomicMax(g.norms + 2 * ((int64_t)b * p.K + h / p.G), __float_as_uint(most));
+    }
+}
+
+// The largest |v|^2 of the live ones among 256 keys of a head.
+template <class T>
+__global__ __launch_bounds__(256) void k_attn_vnorm(attn_in p, bwd_in g)
+{
+    __shared__ float shared[4];
+    const int chunks = (p.T + 255) / 256, bk = blockIdx.x / chunks, t0 = (blockIdx.x - bk * chunks) * 256;
+    const int b = bk / p.K, kv = bk - b * p.K, lane = threadIdx.x % 16, len = len_of(p, b);
+    float most = 0.0f;
+    for (int t = t0 + threadIdx.x / 16; t < min(t0 + 256, len); t += 16) {
+        float norm = 0.0f;
+        if (mask_byte(p, b, t, len)) {
+            const T *v = p.v.at<T>(b, t, kv);
+            for (int c = lane * 8; c < p.D; c += 128) {
+                float x[8];
+                load8<T>(v + c, p.D - c, x);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) norm = __builtin_fmaf(x[e], x[e], norm);
+            }
+        }
+        most = fmaxf(most, lane_sum<16>(norm));
+    }
+    most = block_max(most, shared);
+    if (threadIdx.x == 0) atomicMax(g.norms + 2 * (int64_t)bk + 1, __float_as_uint(most));
+}
+
+// ------------------------------------------------------------------ what a lane stores of a row
+
+template <class T, int A>
+__device__ inline void store_grad(T *to, float *part, bool wide, int width, const f32x16 (&acc)[A], float times, bool zero, int lane)
+{
+#pragma unroll
+    for (int a = 0; a < A; ++a)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const int col = a * 32 + q * 8 + half_row(lane);
+            f32x4 w;
+            vec<T, 4> v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                w[e] = zero ? 0.0f : acc[a][q * 4 + e] * times;
+                v[e] = (T)settled<T>(w[e]);
+            }
+            if (part) {
+                if (col + 4 <= width && width % 4 == 0) {
+                    *(f32x4 *)(part + col) = w;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (col + e < width) part[col + e] = w[e];
+                }
+            } else if (col + 4 <= width && wide) {
+                *(vec<T, 4> *)(to + col) = v;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (col + e < width) to[col + e] = v[e];
+            }
+        }
+}
+
+// ------------------------------------------------------------------ dq
+//
+// delta comes from an o that was summed from rounded probabilities (and may be rounded itself), so ds of a row adds up to some r
+// instead of 0.  Then delta + r is what delta should have been, to 32 bits: it is left for dk, dv and the bias's gradient, which
+// are formed from it afterwards; dq keeps an error of r (p k), about as large as the rounding of ds.
+template <class T, int DP>
+__global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, bwd_in g, int splits)
+{
+    using L = lay<DP>;
+    constexpr int TILE = DP == 256 ? 32 : 64, N = TILE / 32, BYTES = TILE * DP * 2, C = DP / 16, A = DP / 32;
+    __shared__ __align__(16) char k0[BYTES], k1[BYTES], v0[BYTES], v1[BYTES];
+    __shared__ float by_distance[2 * MAX_FAR + 1];
+    const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    const int q_tiles = (p.Q + ROWS - 1) / ROWS;
+    int w = die_order(blockIdx.x, gridDim.x);
+    const int qt = q_tiles - 1 - w % q_tiles;
+    w /= q_tiles;
+    const int split = w % splits, bh = w / splits, b = bh / p.H, h = bh - b * p.H, kv = h / p.G;
+    const int len = len_of(p, b), first = first_of(p, b);
+    const int q0 = qt * ROWS, q1 = min(q0 + ROWS, p.Q);
+    const int end = p.causal ? min(len, max(first + q1 - 1, -1) + 1) : len;
+    const int tiles = (end + TILE - 1) / TILE, each = (tiles + splits - 1) / splits;
+    const int t0 = split * each, t1 = min(tiles, t0 + each);
+
+    const int i = q0 + wave * 32 + lane % 32;
+    const bool there = i < p.Q;
+    const int pos = first + i, pos_lo = first + q0 + wave * 32, pos_hi = pos_lo + 31;
+    frag<T> q[C], d[C];
+    load_stationary<T, DP>(q, p.q.at<T>(b, min(i, p.Q - 1), h), lane, p.D, there);
+    load_stationary<T, DP>(d, g.d_o.at<T>(b, min(i, p.Q - 1), h), lane, p.D, there);
+    const int64_t stat = (int64_t)bh * g.stats_rows + min(i, (int)g.stats_rows - 1);
+    const float lse = there ? g.lse2[stat] : -NEG_INF, delta = there ? g.delta[stat] : 0.0f;
+    const float lift = ds_scale<T>(g, p, b, kv);
+    const int far = p.bias.far;
+    if (p.bias.table) fill_bias<T>(by_distance, p, h, threadIdx.x, 256);
+
+    tile_copy<DP, TILE, WAVES> kc, vc;
+    const T *const kp = p.k.at<T>(b, 0, kv), *const vp = p.v.at<T>(b, 0, kv);
+    kc.set(wave, lane, p.k.t, p.D);
+    vc.set(wave, lane, p.v.t, p.D);
+    constexpr uint64_t ALL = N == 2 ? ~(uint64_t)0 : 0xffffffffu;
+    auto fetch = [&](int t, uint64_t live, lds_byte *kto, lds_byte *vto) __attribute__((always_inline)) {
+        const int64_t key = (int64_t)t * TILE;
+        const bool all = (live & ALL) == ALL && p.D == DP;
+        kc.copy(wave, lane, (const char *)(kp + key * p.k.t), live, all, kto);
+        vc.copy(wave, lane, (const char *)(vp + key * p.v.t), live, all, vto);
+    };
+
+    f32x16 acc[A] = {};
+    const int place = L::rows_place(lane), cols[2] = {L::cols_place(lane, 0), L::cols_place(lane, 1)};
+    float row_sum[2] = {0.0f, 0.0f};
+    auto compute = [&](int t, uint64_t live, lds_byte *kt, lds_byte *vt) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int key0 = t * TILE + n * 32;
+            f32x16 s = {}, dp = {};
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                s = mma32(L::template rows<T>(kt, place, c, n * 32), q[c], s);
+                dp = mma32(L::template rows<T>(vt, place, c, n * 32), d[c], dp);
+            }
+            float by = p.c;
+            if (p.bias.table) {
+                by = 1.0f;
+                add_bias(s, p.c, by_distance, far, key0, pos, pos_lo, pos_hi, lane);
+            }
+            kill_dead(s, (uint32_t)(live >> n * 32), p.causal ? pos - key0 : INT_MAX, lane, NEG_INF);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], by, -lse)) * (dp[r] - delta);
+                row_sum[r % 2] += s[r];
+            }
+            if constexpr (std::is_same_v<T, f16>) s *= lift;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const frag<T> f = to_frag<T>(s, half);
+#pragma unroll
+                for (int a = 0; a < A; ++a) acc[a] = mma32(L::template cols<T>(kt, cols, a, n * 32 + half * 16), f, acc[a]);
+            }
+        }
+    };
+
+    if (t0 < t1) {
+        uint8_t byte = mask_byte(p, b, t0 * TILE + lane, len);
+        uint64_t live = keys_alive(p, t0 * TILE, len, byte);
+        fetch(t0, live, (lds_byte *)k0, (lds_byte *)v0);
+        byte = mask_byte(p, b, (t0 + 1) * TILE + lane, len);
+        auto step = [&](int t, char *kh, char *vh, char *kn, char *vn) __attribute__((always_inline)) {
+            wait_all();
+            uint64_t next = 0;
+            if (t + 1 < t1) {
+                next = keys_alive(p, (t + 1) * TILE, len, byte);
+                byte = mask_byte(p, b, (t + 2) * TILE + lane, len);
+                fetch(t + 1, next, (lds_byte *)kn, (lds_byte *)vn);
+            }
+            compute(t, live, (lds_byte *)kh, (lds_byte *)vh);
+            live = next;
+        };
+        for (int t = t0; t < t1; t += 2) {
+            step(t, k0, v0, k1, v1);
+            if (t + 1 < t1) step(t + 1, k1, v1, k0, v0);
+        }
+    }
+    if (there && g.dq.p) {
+        const int64_t row = ((int64_t)b * p.Q + i) * p.H + h, rows = (int64_t)p.B * p.Q * p.H;
+        store_grad<T, A>(g.dq.at<T>(b, i, h), g.dq_part ? g.dq_part + (split * rows + row) * p.D : nullptr, g.wide & 1, p.D,
+                         acc, p.scale / lift, lse == -NEG_INF, lane);
+    }
+    const float r = half_sum(row_sum[0] + row_sum[1]);
+    if (there && lane < 32) {
+        if (g.row_part)
+            g.row_part[(int64_t)split * p.B * p.H * g.stats_rows + stat] = r;
+        else
+            g.delta[stat] = delta + r;
+    }
+}
+
+// delta + r where splits of the keys left parts of r.
+__global__ __launch_bounds__(256) void k_attn_delta_join(attn_in p, bwd_in g, int splits)
+{
+    const int64_t rows = (int64_t)p.B * p.H * g.stats_rows;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < rows; at += (int64_t)gridDim.x * 256) {
+        float r = 0.0f;
+        for (int s = 0; s < splits; ++s) r += g.row_part[s * rows + at];
+        if (at % g.stats_rows < p.Q) g.delta[at] += r;
+    }
+}
+
+// dtable[c, h]: a wave adds up what a head's workgroups found of a bucket.
+template <class T>
+__global__ __launch_bounds__(WAVE) void k_attn_dtable(attn_in p, const float *part, int64_t of_head, void *dtable)
+{
+    const int buckets = p.bias.count * p.bias.sides, h = blockIdx.x / buckets, c = blockIdx.x - h * buckets;
+    float sum = 0.0f;
+    for (int64_t n = threadIdx.x; n < of_head; n += WAVE) sum += part[(h * of_head + n) * buckets + c];
+    sum = lane_sum<64>(sum);
+    if (threadIdx.x) return;
+    const int64_t at = (int64_t)c * p.H + h;
+    if (p.bias.f32)
+        ((float *)dtable)[at] = sum;
+    else
+        ((T *)dtable)[at] = (T)settled<T>(sum);
+}
+
+// ------------------------------------------------------------------ dk and dv
+//
+// A workgroup has 128 keys of one key head, 32 a wave, and passes over the queries of all heads that share it.
+//
+// FAR: the largest distance that the bias looks up (0: no bias).  Its gradient, ds by buckets, is summed over diagonals: a wave lays the 8
+// queries x 32 keys of a register group into LDS at (query, key - query), whose columns are diagonals, and a lane adds up a column.  What no
+// register ever writes there stays 0.  Pieces that lie beyond FAR whole are added up in registers.
+template <class T, int DP, int FAR>
+__global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dkv(attn_in p, bwd_in g, int splits)
+{
+    using L = lay<DP>;
+    constexpr int TILE = DP == 256 ? 32 : 64, N = TILE / 32, BYTES = TILE * DP * 2, C = DP / 16, A = DP / 32, DIAG = 41;
+    __shared__ __align__(16) char q0[BYTES], q1[BYTES], d0[BYTES], d1[BYTES];
+    __shared__ __align__(16) float lse0[64], lse1[64], del0[64], del1[64];
+    __shared__ float by_distance[2 * FAR + 1], sums[FAR ? WAVES : 1][2 * FAR + 1], diag[FAR ? WAVES : 1][FAR ? 8 * DIAG : 1];
+    const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
+    const int k_tiles = (p.T + ROWS - 1) / ROWS;
+    int w = die_order(blockIdx.x, gridDim.x);
+    const int kt = w % k_tiles;
+    w /= k_tiles;
+    const int split = w % splits, bk = w / splits, b = bk / p.K, kv = bk - b * p.K;
+    const int len = len_of(p, b), first = first_of(p, b);
+    const int wave_key = kt * ROWS + wave * 32, key = wave_key + lane % 32;
+    const bool alive = key < len && mask_byte(p, b, key, len);
+
+    // queries that see any of the workgroup's keys: those from `from` on
+    const int from = p.causal ? (int)min((int64_t)p.Q, max((int64_t)0, (int64_t)kt * ROWS - first)) : 0;
+    const int tile0 = from / TILE, q_tiles = (p.Q + TILE - 1) / TILE, of_head = kt * ROWS < len ? max(0, q_tiles - tile0) : 0;
+    const int64_t all = (int64_t)of_head * p.G, each = (all + splits - 1) / splits;
+    const int64_t t0 = split * each, t1 = min(all, t0 + each);
+
+    frag<T> k[C], v[C];
+    load_stationary<T, DP>(k, p.k.at<T>(b, min(key, p.T - 1), kv), lane, p.D, alive);
+    load_stationary<T, DP>(v, p.v.at<T>(b, min(key, p.T - 1), kv), lane, p.D, alive);
+    const float lift = ds_scale<T>(g, p, b, kv);
+    const float ds_times = std::is_same_v<T, f16> ? lift * __builtin_amdgcn_exp2f(-P_LIFT<T>) : 1.0f;
+    const int far = p.bias.far;
+
+    tile_copy<DP, TILE, WAVES> qc, dc;
+    qc.set(wave, lane, p.q.t, p.D);
+    dc.set(wave, lane, g.d_o.t, p.D);
+    auto fetch = [&](int h, int t, char *qto, char *dto, float *lse, float *del) __attribute__((always_inline)) {
+        const int row0 = t * TILE, n = p.Q - row0;
+        const uint64_t live = n >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << n) - 1;
+        const bool whole = n >= TILE && p.D == DP;
+        qc.copy(wave, lane, (const char *)p.q.at<T>(b, row0, h), live, whole, (lds_byte *)qto);
+        dc.copy(wave, lane, (const char *)g.d_o.at<T>(b, row0, h), live, whole, (lds_byte *)dto);
+        const int64_t stat = ((int64_t)b * p.H + h) * g.stats_rows + row0;
+        // 64 of each, of which a tile of 32 rows takes the first ones; rows are padded
+        const int at = min(lane, TILE - 1);
+        if (wave == 0) __builtin_amdgcn_global_load_lds((global_void *)(g.lse2 + stat + at), (lds_void *)(lds_byte *)lse, 4, 0, 0);
+        if (wave == 1) __builtin_amdgcn_global_load_lds((global_void *)(g.delta + stat + at), (lds_void *)(lds_byte *)del, 4, 0, 0);
+    };
+
+    f32x16 dk[A] = {}, dv[A] = {};
+    const int place = L::rows_place(lane), cols[2] = {L::cols_place(lane, 0), L::cols_place(lane, 1)};
+    float far_sum[2] = {0.0f, 0.0f};  // of keys far behind, far ahead
+    auto add_up = [&](const f32x16 &ds, int pos0) __attribute__((always_inline)) {
+        if constexpr (FAR > 0) {
+            if (wave_key - pos0 - 31 >= far || wave_key + 31 - pos0 <= -far) {
+                float sum[2] = {0.0f, 0.0f};
+#pragma unroll
+                for (int r = 0; r < 16; ++r) sum[r % 2] += ds[r];
+                far_sum[wave_key > pos0] += sum[0] + sum[1];
+                return;
+            }
+            float *const mine = diag[wave];
+#pragma unroll
+            for (int r8 = 0; r8 < 4; ++r8) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int row = half_row(lane) + e;
+                    mine[row * DIAG + lane % 32 - row + 7] = ds[r8 * 4 + e];
+                }
+                asm volatile("" ::: "memory");  // other lanes read what this one wrote
+                if (lane < 39) {
+                    float sum = 0.0f;
+#pragma unroll
+                    for (int row = 0; row < 8; ++row) sum += mine[row * DIAG + lane];
+                    const int rel = wave_key - pos0 - r8 * 8 + lane - 7;
+                    if (rel >= far)
+                        far_sum[1] += sum;
+                    else if (rel <= -far)
+                        far_sum[0] += sum;
+                    else
+                        sums[wave][rel + far] += sum;
+                }
+                asm volatile("" ::: "memory");
+            }
+        }
+    };
+    // What this workgroup found of a head's buckets goes to its place; the sums start again.
+    auto flush = [&](int h) __attribute__((always_inline)) {
+        if constexpr (FAR > 0) {
+            if (!g.table_part) return;
+            const float behind = lane_sum<64>(far_sum[0]), ahead = lane_sum<64>(far_sum[1]);
+            far_sum[0] = far_sum[1] = 0.0f;
+            if (lane == 0) {
+                sums[wave][0] = behind;
+                sums[wave][2 * far] = ahead;
+            }
+            __syncthreads();
+            const int count = p.bias.count, buckets = count * p.bias.sides, c = threadIdx.x;
+            if (c < buckets) {
+                const int side = c / count, n = c % count;
+                const int lo = n == 0 ? 0 : p.bias.border[n - 1], hi = n == count - 1 ? far : p.bias.border[n] - 1;
+                float sum = 0.0f;
+                for (int wv = 0; wv < WAVES; ++wv) {
+                    for (int dist = side ? max(lo, 1) : lo; dist <= hi; ++dist) sum += sums[wv][side ? far + dist : far - dist];
+                    if (p.bias.sides == 1 && n == 0)
+                        for (int at = far + 1; at <= 2 * far; ++at) sum += sums[wv][at];
+                }
+                const int64_t of_head = (int64_t)p.B * k_tiles * splits, me = ((int64_t)b * k_tiles + kt) * splits + split;
+                g.table_part[(h * of_head + me) * buckets + c] = sum * __builtin_amdgcn_exp2f(-P_LIFT<T>);
+            }
+            __syncthreads();
+            for (int n = lane; n <= 2 * far; n += WAVE) sums[wave][n] = 0.0f;
+        }
+    };
+    auto compute = [&](int t, lds_byte *qt, lds_byte *dt, const float *lse, const float *del) __attribute__((always_inline)) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const int row0 = t * TILE + n * 32;
+            f32x16 s = {}, dp = {};
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                s = mma32(L::template rows<T>(qt, place, c, n * 32), k[c], s);
+                dp = mma32(L::template rows<T>(dt, place, c, n * 32), v[c], dp);
+            }
+            f32x4 off[4], delta[4];
+#pragma unroll
+            for (int r8 = 0; r8 < 4; ++r8) {
+                off[r8] = *(const f32x4 *)(lse + n * 32 + r8 * 8 + half_row(lane));
+                delta[r8] = *(const f32x4 *)(del + n * 32 + r8 * 8 + half_row(lane));
+            }
+            float by = p.c;
+            if constexpr (FAR > 0) {
+                by = 1.0f;
+                const int pos_lo = first + row0, pos_hi = pos_lo + 31;
+                if (wave_key - pos_hi >= far || wave_key + 31 - pos_lo <= -far) {
+                    const float add = by_distance[wave_key - pos_hi >= far ? 2 * far : 0];
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], p.c, add);
+                } else {
+                    const int rel = key - pos_lo - half_row(lane) + far;
+#pragma unroll
+                    for (int r = 0; r < 16; ++r)
+                        s[r] = __builtin_fmaf(s[r], p.c, by_distance[min(max(rel - r / 4 * 8 - r % 4, 0), 2 * far)]);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], by, P_LIFT<T> - off[r / 4][r % 4]));
+            if constexpr (FAR > 0)
+                if (!__all(alive)) {  // a dead key's own sums are not stored, but the bias's would have it
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[r] = alive ? s[r] : 0.0f;
+                }
+            if (p.causal && __any(first + row0 < key)) {
+                const int ahead = key - first - row0 - half_row(lane);  // rows before this do not see the key
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] = r / 4 * 8 + r % 4 >= ahead ? s[r] : 0.0f;
+            }
+#pragma unroll
+            for (int r = 0; r < 16; ++r) dp[r] = s[r] * (dp[r] - delta[r / 4][r % 4]);
+            if (FAR > 0) add_up(dp, first + row0);
+            if constexpr (std::is_same_v<T, f16>) dp *= ds_times;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const frag<T> fp = to_frag<T>(s, half), fd = to_frag<T>(dp, half);
+#pragma unroll
+                for (int a = 0; a < A; ++a) {
+                    dv[a] = mma32(L::template cols<T>(dt, cols, a, n * 32 + half * 16), fp, dv[a]);
+                    dk[a] = mma32(L::template cols<T>(qt, cols, a, n * 32 + half * 16), fd, dk[a]);
+                }
+            }
+        }
+    };
+
+    int heads_done[2] = {0, 0};  // heads that this workgroup left sums of
+    if constexpr (FAR > 0) {
+        for (int n = lane; n <= 2 * far; n += WAVE) sums[wave][n] = 0.0f;
+        for (int n = lane; n < 8 * DIAG; n += WAVE) diag[wave][n] = 0.0f;
+    }
+    if (t0 < t1) {
+        int hg = (int)(t0 / of_head), t = (int)(t0 - (int64_t)hg * of_head) + tile0, filled = -1;
+        heads_done[0] = hg;
+        heads_done[1] = (int)((t1 - 1) / of_head) + 1;
+        fetch(kv * p.G + hg, t, q0, d0, lse0, del0);
+        auto step = [&](int64_t s, char *qh, char *dh, float *lh, float *eh, char *qn, char *dn, float *ln, float *en) __attribute__((always_inline)) {
+            if constexpr (FAR > 0)
+                if (filled != hg) {  // another head's bias, once all waves are done with the last one's
+                    __syncthreads();
+                    if (filled >= 0) flush(kv * p.G + filled);
+                    fill_bias<T>(by_distance, p, kv * p.G + hg, threadIdx.x, 256);
+                    filled = hg;
+                }
+            wait_all();
+            const int here = t;
+            if (s + 1 < t1) {
+                if (++t == q_tiles) {
+                    t = tile0;
+                    ++hg;
+                }
+                fetch(kv * p.G + hg, t, qn, dn, ln, en);
+            }
+            compute(here, (lds_byte *)qh, (lds_byte *)dh, lh, eh);
+        };
+        for (int64_t s = t0; s < t1; s += 2) {
+            step(s, q0, d0, lse0, del0, q1, d1, lse1, del1);
+            if (s + 1 < t1) step(s + 1, q1, d1, lse1, del1, q0, d0, lse0, del0);
+        }
+        flush(kv * p.G + filled);
+    }
+    if constexpr (FAR > 0)
+        if (g.table_part) {
+            const int buckets = p.bias.count * p.bias.sides;
+            const int64_t of_head = (int64_t)p.B * k_tiles * splits, me = ((int64_t)b * k_tiles + kt) * splits + split;
+            for (int hg = 0; hg < p.G; ++hg)
+                if ((hg < heads_done[0] || hg >= heads_done[1]) && threadIdx.x < buckets)
+                    g.table_part[((kv * p.G + hg) * of_head + me) * buckets + threadIdx.x] = 0.0f;
+        }
+    if (key >= p.T) return;
+    const int64_t row = ((int64_t)b * p.T + key) * p.K + kv, rows = (int64_t)p.B * p.T * p.K, at = (split * rows + row) * p.D;
+    if (!g.dk.p) return;
+    store_grad<T, A>(g.dk.at<T>(b, key, kv), g.dk_part ? g.dk_part + at : nullptr, g.wide >> 1 & 1, p.D, dk, p.scale / lift,
+                     !alive, lane);
+    store_grad<T, A>(g.dv.at<T>(b, key, kv), g.dv_part ? g.dv_part + at : nullptr, g.wide >> 1 & 1, p.D, dv,
+                     __builtin_amdgcn_exp2f(-P_LIFT<T>), !alive, lane);
+}
+
+// ------------------------------------------------------------------ splits joined
+
+struct grad_join {
+    const float *part;
+    heads_at to;
+    int64_t rows;  // batch * n * heads
+    int n, heads;
+};
+
+// A lane has one element; splits are added in order.
+template <class T>
+__global__ __launch_bounds__(256) void k_attn_grads(grad_join j0, grad_join j1, int D, int splits)
+{
+    const grad_join &j = blockIdx.y ? j1 : j0;
+    const int64_t size = j.rows * D;
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < size; at += (int64_t)gridDim.x * 256) {
+        float sum = 0.0f;
+        for (int s = 0; s < splits; ++s) sum += j.part[s * size + at];
+        const int64_t row = at / D, t = row / j.heads;
+        j.to.at<T>(t / j.n, t % j.n, row % j.heads)[at - row * D] = (T)settled<T>(sum);
+    }
+}
+
+bool takes_8_bytes(const rkb_heads &h, int64_t dim)
+{
+    return dim % 4 == 0 && (uintptr_t)h.p % 8 == 0 && h.batch % 4 == 0 && h.row % 4 == 0 && h.head % 4 == 0;
+}
+
+struct bwd_memory {
+    size_t stats, norms, dq, rows, dkv, table;
+    bwd_memory(const attn_bwd_plan &plan, const rkb_attn &a)
+    {
+        auto up = [](size_t n) { return (size_t)round_up((int64_t)n, 256); };
+        stats = up((size_t)a.batch * a.heads * plan.stats_rows * 4);
+        norms = a.dtype == RKB_F16 ? up((size_t)a.batch * a.kv_heads * 8) : 0;
+        dq = plan.q_splits > 1 ? up((size_t)plan.q_splits * a.batch * a.q_rows * a.heads * a.dim * 4) : 0;
+        dkv = plan.k_splits > 1 ? up((size_t)plan.k_splits * a.batch * a.k_rows * a.kv_heads * a.dim * 4) : 0;
+        rows = plan.q_splits > 1 ? plan.q_splits * stats : 0;
+        table = a.table ? up((size_t)plan.k_blocks * plan.k_splits * (a.heads / a.kv_heads) * a.buckets * 4) : 0;
+    }
+    size_t all() const { return 2 * stats + norms + dq + rows + 2 * dkv + table; }
+};
+
+}  // namespace
+
+size_t attn_bwd_bytes(const attn_bwd_plan &plan, const rkb_attn &a) { return bwd_memory(plan, a).all(); }
+
+int run_attn_bwd(const attn_in &p, const rkb_attn &a, const attn_bwd_plan &plan, const attn_grads &gr, char *ws, hipStream_t st)
+{
+    const bwd_memory mem(plan, a);
+    bwd_in g{at_of(gr.d_o), at_of(gr.o), gr.o32, gr.lse};
+    g.stats_rows = plan.stats_rows;
+    auto take = [&](size_t n) {
+        char *const at = ws;
+        ws += n;
+        return n ? at : nullptr;
+    };
+    g.delta = (float *)take(mem.stats);
+    g.lse2 = (float *)take(mem.stats);
+    g.norms = (uint32_t *)take(mem.norms);
+    g.dq = at_of(gr.dq);
+    g.dk = at_of(gr.dk);
+    g.dv = at_of(gr.dv);
+    g.dq_part = (float *)take(mem.dq);
+    g.row_part = (float *)take(mem.rows);
+    g.dk_part = (float *)take(mem.dkv);
+    g.dv_part = (float *)take(mem.dkv);
+    g.table_part = gr.dtable ? (float *)take(mem.table) : nullptr;
+    g.wide = takes_8_bytes(gr.dq, a.dim) | (takes_8_bytes(gr.dk, a.dim) && takes_8_bytes(gr.dv, a.dim)) << 1;
+    return with_attn_type(a.dtype, [&](auto *tp) {
+        using T = std::remove_pointer_t<decltype(tp)>;
+        int rc = RKB_OK;
+        const int64_t rows = a.batch * a.heads, keys = a.batch * a.kv_heads;
+        if (g.norms && keys > 0) rc = launch(k_clear, dim3(1), dim3(256), st, g.norms, (int)(2 * keys));
+        if (rc == RKB_OK && rows * a.q_rows > 0) rc = launch(k_attn_delta<T>, dim3((uint32_t)(rows * (plan.stats_rows / 64))), dim3(256), st, p, g);
+        if (rc == RKB_OK && g.norms && keys * a.k_rows > 0)
+            rc = launch(k_attn_vnorm<T>, dim3((uint32_t)(keys * ((a.k_rows + 255) / 256))), dim3(256), st, p, g);
+        if (rc != RKB_OK) return rc;
+        return with_width(a.dim, [&](auto dp) {
+            constexpr int DP = dp();
+            const dim3 q_grid((uint32_t)(plan.q_blocks * plan.q_splits)), k_grid((uint32_t)(plan.k_blocks * plan.k_splits));
+            int rc = RKB_OK;
+            auto join = [&](const grad_join &x, const grad_join &y, int splits, int jobs) {
+                const int64_t blocks = std::min<int64_t>((x.rows * a.dim + 255) / 256, 1 << 16);
+                return launch(k_attn_grads<T>, dim3((uint32_t)blocks, jobs), dim3(256), st, x, y, (int)a.dim, splits);
+            };
+            if (plan.q_blocks) rc = launch(k_attn_dq<T, DP>, q_grid, dim3(256), st, p, g, plan.q_splits);
+            if (rc == RKB_OK && g.row_part && plan.q_blocks)
+                rc = launch(k_attn_delta_join, dim3((uint32_t)std::min<int64_t>((rows * plan.stats_rows + 255) / 256, 1 << 16)), dim3(256), st, p, g,
+                            plan.q_splits);
+            if (rc == RKB_OK && plan.q_splits > 1 && gr.dq.p) {
+                const grad_join j{g.dq_part, g.dq, a.batch * a.q_rows * a.heads, (int)a.q_rows, (int)a.heads};
+                rc = join(j, j, plan.q_splits, 1);
+            }
+            if (rc == RKB_OK && plan.k_blocks && (gr.dk.p || gr.dtable)) {
+                if (!p.bias.table)
+                    rc = launch(k_attn_dkv<T, DP, 0>, k_grid, dim3(256), st, p, g, plan.k_splits);
+                else if (p.bias.far <= 128)
+                    rc = launch(k_attn_dkv<T, DP, 128>, k_grid, dim3(256), st, p, g, plan.k_splits);
+                else
+                    rc = launch(k_attn_dkv<T, DP, MAX_FAR>, k_grid, dim3(256), st, p, g, plan.k_splits);
+            }
+            if (rc == RKB_OK && gr.dtable)
+                rc = launch(k_attn_dtable<T>, dim3((uint32_t)(a.heads * a.buckets)), dim3(WAVE), st, p, (const float *)g.table_part,
+                            a.batch * ((a.k_rows + ROWS - 1) / ROWS) * plan.k_splits, gr.dtable);
+            if (rc == RKB_OK && plan.k_splits > 1 && gr.dk.p) {
+                const int64_t n = a.batch * a.k_rows * a.kv_heads;
+                rc = join({g.dk_part, g.dk, n, (int)a.k_rows, (int)a.kv_heads}, {g.dv_part, g.dv, n, (int)a.k_rows, (int)a.kv_heads}, plan.k_splits, 2);
+            }
+            return rc;
+        });
+    });
+}
+
+}  // namespace rkb

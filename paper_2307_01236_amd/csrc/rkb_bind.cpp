@@ -7,6 +7,8 @@
 #include <Python.h>
 #include <hip/hip_runtime_api.h>
 
+#include <cmath>
+
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
 #include <c10/hip/HIPStream.h>
@@ -17,8 +19,8 @@
 
 namespace {
 
-PyObject *g_error = nullptr, *g_ckpt = nullptr;     // block.RKBError, block.Ckpt8
-PyObject *n_codes, *n_exps, *n_dtype, *n_shape;     // attribute names
+PyObject *g_error = nullptr, *g_ckpt = nullptr, *g_kv8 = nullptr, *g_bias = nullptr;  // block.RKBError, Ckpt8, Kv8, RelBias
+PyObject *n_codes, *n_exps, *n_dtype, *n_shape, *n_table, *n_max_distance, *n_two_sided;  // attribute names
 PyObject *g_dtypes[3];                              // torch.float32, float16, bfloat16 by RKB_F32 ..
 
 struct refused {};  // thrown within this file once the Python error is set
@@ -517,17 +519,285 @@ PyObject *gated_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// init(RKBError, Ckpt8, (float32, float16, bfloat16))
+// ------------------------------------------------------------------ attention
+
+// A [batch, rows, heads, dim] tensor that goes with another one: of its device, of type `type`, and of the sizes given (-1: any).
+rkb_heads as_heads(const at::Tensor &t, const char *where, const at::Tensor &like, at::ScalarType type, int64_t batch, int64_t rows,
+                   int64_t heads, int64_t dim)
+{
+    if (t.scalar_type() != type || t.get_device() != like.get_device()) fail(RKB_E_INVAL, where, "types or devices differ");
+    if (t.dim() != 4 || (batch >= 0 && t.size(0) != batch) || (rows >= 0 && t.size(1) != rows) || (heads >= 0 && t.size(2) != heads) ||
+        (dim >= 0 && t.size(3) != dim))
+        fail(RKB_E_INVAL, where, "sizes do not match");
+    if (t.size(3) > 1 && t.stride(3) != 1) fail(RKB_E_INVAL, where, "columns that are not adjacent");
+    return {t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)};
+}
+
+bool aligned(const at::Tensor &t, const rkb_heads &h)
+{
+    auto good = [&](int i, int64_t s) { return t.size(i) <= 1 || s % 8 == 0; };
+    return (uintptr_t)h.p % 16 == 0 && good(0, h.batch) && good(1, h.row) && good(2, h.head) && (t.size(1) <= 1 || h.row <= (int64_t)1 << 22);
+}
+
+// None, or a contiguous int32 tensor with one element per sequence.
+const int32_t *as_counts(PyObject *o, const char *where, const at::Tensor &like, int64_t batch)
+{
+    return (const int32_t *)as_vector(o, where, like, at::kInt, batch);
+}
+
+// An int, or a tensor of an int32 per sequence.
+void as_first(PyObject *o, const char *where, const at::Tensor &like, int64_t batch, int64_t *first, const int32_t **firsts)
+{
+    *first = 0;
+    *firsts = nullptr;
+    if (THPVariable_Check(o))
+        *firsts = as_counts(o, where, like, batch);
+    else
+        *first = as_int(o);
+}
+
+struct kv8 {
+    rkb_kv8 c;
+    int64_t batch, tokens, heads, dim;
+    int type;
+    const at::Tensor *codes;
+};
+
+kv8 as_kv8(PyObject *o, const char *where, const at::Tensor *like)
+{
+    owned codes(PyObject_GetAttr(o, n_codes)), exps(PyObject_GetAttr(o, n_exps)), dtype(PyObject_GetAttr(o, n_dtype)), shape(PyObject_GetAttr(o, n_shape));
+    const at::Tensor &c = tensor(codes.o, where), &e = tensor(exps.o, where);
+    kv8 k{};
+    while (k.type < 3 && g_dtypes[k.type] != dtype.o) ++k.type;
+    if ((k.type != RKB_F16 && k.type != RKB_BF16) || c.scalar_type() != at::kChar || e.scalar_type() != at::kByte ||
+        e.get_device() != c.get_device() || (like && like->get_device() != c.get_device()))
+        fail(RKB_E_INVAL, where, "types or devices differ");
+    if (!PyTuple_Check(shape.o) || PyTuple_GET_SIZE(shape.o) != 4) fail(RKB_E_INVAL, where, "sizes do not match");
+    int64_t *const to[] = {&k.batch, &k.tokens, &k.heads, &k.dim};
+    for (int i = 0; i < 4; ++i) {
+        *to[i] = as_int(PyTuple_GET_ITEM(shape.o, i));
+        if (*to[i] < 0 || *to[i] > RKB_MAX_TOKENS) fail(RKB_E_INVAL, where, "sizes do not match");
+    }
+    const int64_t blocks = (k.tokens + RKB_GROUP - 1) / RKB_GROUP, ld = (k.dim + 15) / 16 * 16;
+    if (c.sizes() != at::IntArrayRef({2, k.batch, k.heads, blocks * RKB_GROUP, ld}) || e.sizes() != at::IntArrayRef({2, k.batch, k.heads, blocks}) ||
+        !c.is_contiguous() || !e.is_contiguous())
+        fail(RKB_E_INVAL, where, "sizes do not match");
+    k.c = {(int8_t *)c.data_ptr(), (uint8_t *)e.data_ptr(), k.tokens};
+    k.codes = &THPVariable_Unpack(codes.o);  // the cache object holds it while the call runs
+    return k;
+}
+
+// scale, lens, mask, causal, first and bias: a[0] .. a[5].
+struct attn_args {
+    rkb_attn a{};
+    const at::Tensor *table = nullptr;
+    attn_args(PyObject *const *o, const char *where, const at::Tensor &q, int64_t k_rows, int64_t kv_heads)
+    {
+        a.dtype = dtype_of(q, where, true);
+        a.batch = q.size(0);
+        a.q_rows = q.size(1);
+        a.k_rows = k_rows;
+        a.heads = q.size(2);
+        a.kv_heads = kv_heads;
+        a.dim = q.size(3);
+        if (o[0] == Py_None) {
+            a.scale = a.dim > 0 ? 1.0f / std::sqrt((float)a.dim) : 1.0f;
+        } else {
+            const double s = PyFloat_AsDouble(o[0]);
+            if (s == -1.0 && PyErr_Occurred()) throw refused();
+            a.scale = (float)s;
+        }
+        a.lens = as_counts(o[1], where, q, a.batch);
+        if (o[2] != Py_None) {
+            const at::Tensor &m = tensor(o[2], where);
+            if ((m.scalar_type() != at::kBool && m.scalar_type() != at::kByte) || m.get_device() != q.get_device())
+                fail(RKB_E_INVAL, where, "types or devices differ");
+            if (m.dim() != 2 || m.size(0) != a.batch || m.size(1) != k_rows) fail(RKB_E_INVAL, where, "sizes do not match");
+            if (k_rows > 1 && m.stride(1) != 1) fail(RKB_E_INVAL, where, "columns that are not adjacent");
+            a.mask = (const uint8_t *)m.data_ptr();
+            a.mask_stride = m.stride(0);
+        }
+        a.causal = as_bool(o[3]);
+        as_first(o[4], where, q, a.batch, &a.first, &a.firsts);
+        if (o[5] != Py_None) {
+            if (!PyObject_TypeCheck(o[5], (PyTypeObject *)g_bias)) fail(RKB_E_INVAL, where, "bias");
+            owned t(PyObject_GetAttr(o[5], n_table)), far(PyObject_GetAttr(o[5], n_max_distance)), two(PyObject_GetAttr(o[5], n_two_sided));
+            table = &tensor(t.o, where);
+            if ((table->scalar_type() != q.scalar_type() && table->scalar_type() != at::kFloat) || table->get_device() != q.get_device())
+                fail(RKB_E_INVAL, where, "types or devices differ");
+            if (table->dim() != 2 || table->size(1) != a.heads || table->size(0) > RKB_MAX_BUCKETS || !table->is_contiguous())
+                fail(RKB_E_INVAL, where, "sizes do not match");
+            const long most = as_int(far.o);
+            if (most < 0 || most > RKB_MAX_DISTANCE) fail(RKB_E_INVAL, where, "max_distance");
+            a.table = table->data_ptr();
+            a.table_dtype = dtype_of(*table, where);
+            a.buckets = (int)table->size(0);
+            a.max_distance = (int)most;
+            a.two_sided = as_bool(two.o);
+            if (a.buckets == 0) fail(RKB_E_INVAL, where, "sizes do not match");
+        }
+    }
+};
+
+rkb_heads heads_of(const at::Tensor &t)
+{
+    if (!t.defined()) return {nullptr, 0, 0, 0};
+    return {t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)};
+}
+
+// attn_fwd(q, k or cache, v, scale, lens, mask, causal, first, bias, keep)
+PyObject *attn_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(10, n, [&] {
+        const char *where = "rkb_attn_fwd";
+        const at::Tensor &q = tensor(a[0], where);
+        const int type = dtype_of(q, where, true);
+        const rkb_heads qh = as_heads(q, where, q, q.scalar_type(), -1, -1, -1, -1);
+        const bool cached = PyObject_TypeCheck(a[1], (PyTypeObject *)g_kv8);
+        kv8 cache{};
+        rkb_heads kh{}, vh{};
+        int64_t tokens, heads;
+        bool fits = aligned(q, qh);
+        if (cached) {
+            if (a[2] != Py_None) fail(RKB_E_INVAL, where, "a cache and values");
+            cache = as_kv8(a[1], where, &q);
+            if (cache.type != type || cache.batch != q.size(0) || cache.dim != q.size(3)) fail(RKB_E_INVAL, where, "sizes do not match");
+            tokens = cache.tokens;
+            heads = cache.heads;
+        } else {
+            const at::Tensor &k = tensor(a[1], where), &v = tensor(a[2], where);
+            kh = as_heads(k, where, q, q.scalar_type(), q.size(0), -1, -1, q.size(3));
+            tokens = k.size(1);
+            heads = k.size(2);
+            vh = as_heads(v, where, q, q.scalar_type(), q.size(0), tokens, heads, q.size(3));
+            fits = fits && aligned(k, kh) && aligned(v, vh);
+        }
+        const attn_args args(a + 3, where, q, tokens, heads);
+        const long keep = as_int(a[9]);
+        const on_device on(q, where);
+        const at::Tensor o = like_of(q, q.sizes());
+        at::Tensor o32, lse;
+        if (keep != RKB_KEEP_NONE) lse = like_of(q, {q.size(0), q.size(2), q.size(1)}, at::kFloat);
+        if (keep == RKB_KEEP_FULL) o32 = like_of(q, q.sizes(), at::kFloat);
+        size_t bytes = 0;
+        check(rkb_attn_fwd_workspace(&args.a, cached, fits, &bytes), where);
+        workspace ws;
+        ws.need(q, bytes);
+        const rkb_heads oh = heads_of(o);
+        check(rkb_attn_fwd(&args.a, &qh, cached ? nullptr : &kh, cached ? nullptr : &vh, cached ? &cache.c : nullptr, &oh,
+                           o32.defined() ? (float *)o32.data_ptr() : nullptr, lse.defined() ? (float *)lse.data_ptr() : nullptr, ws.p, ws.bytes,
+                           on.stream), where);
+        owned out(PyTuple_New(2));
+        PyTuple_SET_ITEM(out.o, 0, owned(wrap(o)).release());
+        if (lse.defined()) {
+            PyTuple_SET_ITEM(out.o, 1, wrap_all({o32.defined() ? &o32 : &o, &lse}));
+        } else {
+            Py_INCREF(Py_None);
+            PyTuple_SET_ITEM(out.o, 1, Py_None);
+        }
+        return out.release();
+    });
+}
+
+// attn_bwd(do, q, k, v, kept, scale, lens, mask, causal, first, bias)
+PyObject *attn_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(11, n, [&] {
+        const char *where = "rkb_attn_bwd";
+        const at::Tensor &q = tensor(a[1], where);
+        dtype_of(q, where, true);
+        const rkb_heads qh = as_heads(q, where, q, q.scalar_type(), -1, -1, -1, -1);
+        const at::Tensor &d = tensor(a[0], where), &k = tensor(a[2], where), &v = tensor(a[3], where);
+        const rkb_heads dh = as_heads(d, where, q, q.scalar_type(), q.size(0), q.size(1), q.size(2), q.size(3));
+        const rkb_heads kh = as_heads(k, where, q, q.scalar_type(), q.size(0), -1, -1, q.size(3));
+        const rkb_heads vh = as_heads(v, where, q, q.scalar_type(), q.size(0), k.size(1), k.size(2), q.size(3));
+        const attn_args args(a + 5, where, q, k.size(1), k.size(2));
+        rkb_heads oh{};
+        const float *o32 = nullptr, *lse = nullptr;
+        if (a[4] != Py_None) {
+            if (!PyTuple_Check(a[4]) || PyTuple_GET_SIZE(a[4]) != 2) fail(RKB_E_INVAL, where, "kept");
+            const at::Tensor &o = tensor(PyTuple_GET_ITEM(a[4], 0), where), &l = tensor(PyTuple_GET_ITEM(a[4], 1), where);
+            const bool full = o.scalar_type() == at::kFloat;
+            oh = as_heads(o, where, q, full ? at::kFloat : q.scalar_type(), q.size(0), q.size(1), q.size(2), q.size(3));
+            if (l.scalar_type() != at::kFloat || l.get_device() != q.get_device() || l.sizes() != at::IntArrayRef({q.size(0), q.size(2), q.size(1)}) ||
+                !l.is_contiguous() || (full && !o.is_contiguous()))
+                fail(RKB_E_INVAL, where, "kept");
+            if (full) {
+                o32 = (const float *)oh.p;
+                oh.p = nullptr;
+            }
+            lse = (const float *)l.data_ptr();
+        }
+        const on_device on(q, where);
+        const at::Tensor dq = like_of(q, q.sizes()), dk = like_of(k, k.sizes()), dv = like_of(v, v.sizes());
+        at::Tensor dtable;
+        if (args.table) dtable = like_of(*args.table, args.table->sizes());
+        const bool again = a[4] == Py_None, fits = aligned(q, qh) && aligned(d, dh) && aligned(k, kh) && aligned(v, vh);
+        size_t bytes = 0;
+        check(rkb_attn_bwd_workspace(&args.a, again, fits, &bytes), where);
+        workspace ws;
+        ws.need(q, bytes);
+        // an empty tensor may have no memory at all
+        static const float nothing = 0.0f;
+        if (!again && !lse) lse = &nothing;
+        const rkb_heads dqh = heads_of(dq), dkh = heads_of(dk), dvh = heads_of(dv);
+        check(rkb_attn_bwd(&args.a, &dh, &qh, &kh, &vh, &oh, o32, lse, &dqh, &dkh, &dvh, dtable.defined() ? dtable.data_ptr() : nullptr, ws.p,
+                           ws.bytes, on.stream), where);
+        return wrap_all({&dq, &dk, &dv, &dtable});
+    });
+}
+
+// kv8_write(cache, k, v, first, counts)
+PyObject *kv8_write(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(5, n, [&] {
+        const char *where = "rkb_kv8_write";
+        if (!PyObject_TypeCheck(a[0], (PyTypeObject *)g_kv8)) fail(RKB_E_INVAL, where, "not a cache on the GPU");
+        const at::Tensor &k = tensor(a[1], where), &v = tensor(a[2], where);
+        const kv8 c = as_kv8(a[0], where, &k);
+        if (dtype_of(k, where, true) != c.type) fail(RKB_E_INVAL, where, "types or devices differ");
+        const rkb_heads kh = as_heads(k, where, k, k.scalar_type(), c.batch, -1, c.heads, c.dim);
+        const rkb_heads vh = as_heads(v, where, k, k.scalar_type(), c.batch, k.size(1), c.heads, c.dim);
+        int64_t first;
+        const int32_t *firsts;
+        as_first(a[3], where, k, c.batch, &first, &firsts);
+        const int32_t *counts = as_counts(a[4], where, k, c.batch);
+        const on_device on(k, where);
+        check(rkb_kv8_write(c.type, c.batch, k.size(1), c.heads, c.dim, &kh, &vh, first, firsts, counts, &c.c, on.stream), where);
+        Py_RETURN_NONE;
+    });
+}
+
+PyObject *kv8_load(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(1, n, [&] {
+        const char *where = "rkb_kv8_load";
+        if (!PyObject_TypeCheck(a[0], (PyTypeObject *)g_kv8)) fail(RKB_E_INVAL, where, "not a cache on the GPU");
+        const kv8 c = as_kv8(a[0], where, nullptr);
+        const on_device on(*c.codes, where);
+        const at::ScalarType type = c.type == RKB_F16 ? at::kHalf : at::kBFloat16;
+        const at::Tensor k = like_of(*c.codes, {c.batch, c.tokens, c.heads, c.dim}, type), v = like_of(k, k.sizes());
+        const rkb_heads kh = heads_of(k), vh = heads_of(v);
+        check(rkb_kv8_load(c.type, c.batch, c.heads, c.dim, &c.c, &kh, &vh, on.stream), where);
+        return wrap_all({&k, &v});
+    });
+}
+
+// init(RKBError, Ckpt8, (float32, float16, bfloat16), Kv8, RelBias)
 PyObject *init(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
-    if (n != 3 || !PyTuple_Check(a[2]) || PyTuple_GET_SIZE(a[2]) != 3) {
-        PyErr_SetString(PyExc_TypeError, "init(RKBError, Ckpt8, dtypes)");
+    if (n != 5 || !PyTuple_Check(a[2]) || PyTuple_GET_SIZE(a[2]) != 3) {
+        PyErr_SetString(PyExc_TypeError, "init(RKBError, Ckpt8, dtypes, Kv8, RelBias)");
         return nullptr;
     }
     Py_INCREF(a[0]);
     Py_INCREF(a[1]);
+    Py_INCREF(a[3]);
+    Py_INCREF(a[4]);
     g_error = a[0];
     g_ckpt = a[1];
+    g_kv8 = a[3];
+    g_bias = a[4];
     for (int i = 0; i < 3; ++i) {
         g_dtypes[i] = PyTuple_GET_ITEM(a[2], i);
         Py_INCREF(g_dtypes[i]);
@@ -536,12 +806,16 @@ PyObject *init(PyObject *, PyObject *const *a, Py_ssize_t n)
     n_exps = PyUnicode_InternFromString("exps");
     n_dtype = PyUnicode_InternFromString("dtype");
     n_shape = PyUnicode_InternFromString("shape");
+    n_table = PyUnicode_InternFromString("table");
+    n_max_distance = PyUnicode_InternFromString("max_distance");
+    n_two_sided = PyUnicode_InternFromString("two_sided");
     Py_RETURN_NONE;
 }
 
 #define RKB_CALL(name) {#name, (PyCFunction)(void *)name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {RKB_CALL(init),        RKB_CALL(layer_norm_fwd), RKB_CALL(layer_norm_bwd), RKB_CALL(ckpt8_save),
                          RKB_CALL(ckpt8_load),  RKB_CALL(weight_grad),    RKB_CALL(gated_fwd),      RKB_CALL(gated_bwd),
+                         RKB_CALL(attn_fwd),    RKB_CALL(attn_bwd),       RKB_CALL(kv8_write),      RKB_CALL(kv8_load),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_rkblock", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
