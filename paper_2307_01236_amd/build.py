@@ -21,6 +21,9 @@ CALIB_SOURCES = ["rk_calib.hip"]
 BLOCK_LIB = os.path.join(PKG, "librkblock.so")
 BLOCK_SOURCES = ["rkb_norm.hip", "rkb_ckpt.hip", "rkb_gemm.hip", "rkb_attn.hip", "rkb_attn_bwd.hip", "rkb_attn_api.hip",
                  "rkb_kv8.hip"]
+# Sums of the attention kernels stay in vector registers past 256 of them, where vector instructions reach them: kept in the
+# accumulation registers, every tile of k_attn copied 128 of them to and fro.
+SOURCE_FLAGS = {s: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for s in ("rkb_attn.hip",)}
 BIND_LIB = os.path.join(PKG, "_rkblock.so")
 BIND_SOURCE = "rkb_bind.cpp"
 ARCH = "gfx950"
@@ -58,7 +61,7 @@ def _compile(sources, out: str, verbose: bool) -> str:
     """Every source to an object of its own, side by side (a single call of hipcc takes them in turn), then linked."""
     with tempfile.TemporaryDirectory() as tmp, ThreadPoolExecutor(os.cpu_count()) as pool:
         flags = [f for f in HIPCC_FLAGS if f != "-shared"]
-        objects = list(pool.map(lambda s: _run([hipcc(), *flags, "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c",
+        objects = list(pool.map(lambda s: _run([hipcc(), *flags, *SOURCE_FLAGS.get(s, []), "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-c",
                                                 os.path.join(CSRC, s)], os.path.join(tmp, s + ".o"), verbose), sources))
         return _run([hipcc(), f"--offload-arch={ARCH}", "-shared", "-fPIC", *objects], out, verbose)
 

@@ -60,7 +60,7 @@ struct bias_table {
     int f32;            // 32-bit, else of the operands' type
     int sides, count;   // buckets of a side
     int far;            // the least distance of a side's last bucket
-    int border[MAX_BUCKETS - 1];  // the least distance of buckets 1 ..
+    int border[MAX_BUCKETS];  // the least distance of buckets 1 .., then INT_MAX
 };
 
 struct attn_in {
@@ -89,11 +89,18 @@ __device__ inline int first_of(const attn_in &p, int b)
     return (int)min(max(at, (int64_t)-FAR_POSITION), (int64_t)FAR_POSITION);
 }
 
-// Workgroups go to the 8 dies in turn; each die gets a run of neighbouring work, so that its L2 holds what they share.
-__device__ inline int die_order(int block, int total)
+// Which of units x each workgroups a block is.  Workgroups go to the 8 dies in turn.  A unit (a key head of a sequence) is one die's, so that its
+// L2 holds what they share, and units are dealt out in turn, so that sequences of different lengths are, too; those left over
+// when every die has as many are cut into runs.
+__device__ inline int unit_order(int block, int units, int each)
 {
-    const int die = block % 8, share = total / 8, rest = total % 8;
-    return die * share + min(die, rest) + block / 8;
+    const int dealt = units / 8 * 8 * each;
+    if (block < dealt) {
+        const int i = block / 8, round = i / each;
+        return (round * 8 + block % 8) * each + (i - round * each);
+    }
+    const int left = units * each - dealt, share = left / 8, rest = left % 8, die = block % 8;
+    return dealt + die * share + min(die, rest) + (block - dealt) / 8;
 }
 
 // ------------------------------------------------------------------ tiles in LDS
@@ -191,38 +198,46 @@ __device__ inline frag<T> code_values(uint32_t lo, uint32_t hi, float step)
     return f;
 }
 
-// The same tile from a cache's codes, through registers: load, then (later) put.
+// The same tile from a cache's codes, through registers: load, then (later) put.  Nothing is decided between the loads: rows and
+// columns that do not exist are read from where the last ones that do lie, and become zeros when they are put.
 template <class T, int DP, int ROWS, int LANES>
 struct tile_codes {
-    static constexpr int EACH = ROWS * DP / 16 / LANES, SPANS = DP / 16;
+    static constexpr int EACH = ROWS * DP / 16 / LANES, SPANS = DP / 16, BLOCKS = ROWS / RKB_GROUP;
     static_assert(ROWS * DP / 16 % LANES == 0);
     u32x4 q[EACH];
-    float step[EACH];
+    uint8_t exp[BLOCKS];
+    uint64_t live;
+    int spans;
 
-    // from: the codes of the tile's first row, exps: those of its blocks; rows are 32-aligned.
-    __device__ void load(int t, const int8_t *from, const uint8_t *exps, int64_t ld, uint64_t live)
+    // from: the codes of the tile's first row, exps: those of its blocks; rows: how many exist (at least one).
+    __device__ void load(int t, const int8_t *from, const uint8_t *exps, int64_t ld, uint64_t alive, int rows)
     {
+        live = alive;
+        spans = (int)ld / 16;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
-            const int n = t + i * LANES, r = n / SPANS, span = n % SPANS;
-            const bool there = (live >> r & 1) && span * 16 < ld;
-            q[i] = u32x4{0, 0, 0, 0};
-            step[i] = 0.0f;
-            if (there) {
-                q[i] = *(const u32x4 *)(from + r * ld + span * 16);
-                const uint8_t e = exps[r / RKB_GROUP];
-                step[i] = e == 0 ? 0.0f : step_of(e);
-            }
+            const int n = t + i * LANES, r = min(n / SPANS, rows - 1), span = min(n % SPANS, spans - 1);
+            q[i] = *(const u32x4 *)(from + r * (int)ld + span * 16);
         }
+#pragma unroll
+        for (int k = 0; k < BLOCKS; ++k) exp[k] = exps[min(k, (rows - 1) / RKB_GROUP)];
     }
     __device__ void put(int t, lds_byte *to) const
     {
+        float step[BLOCKS];
+#pragma unroll
+        for (int k = 0; k < BLOCKS; ++k) step[k] = exp[k] == 0 ? 0.0f : step_of(exp[k]);
+        constexpr uint64_t ALL = ROWS == 64 ? ~(uint64_t)0 : ((uint64_t)1 << ROWS % 64) - 1;
+        const bool all = (live & ALL) == ALL && spans == SPANS;
 #pragma unroll
         for (int i = 0; i < EACH; ++i) {
             const int n = t + i * LANES, r = n / SPANS, span = n % SPANS;
+            const bool there = all || ((live >> r & 1) && span < spans);
+            // which block: the same for all lanes, as a tile of 32 rows has one and 32 rows or more are between two lanes' rows
+            const float by = there ? step[i * BLOCKS / EACH] : 0.0f;
             using lds_frag = __attribute__((address_space(3))) frag<T>;
-            *(lds_frag *)(to + lay<DP>::at(r, span * 2)) = code_values<T>(q[i][0], q[i][1], step[i]);
-            *(lds_frag *)(to + lay<DP>::at(r, span * 2 + 1)) = code_values<T>(q[i][2], q[i][3], step[i]);
+            *(lds_frag *)(to + lay<DP>::at(r, span * 2)) = code_values<T>(there ? q[i][0] : 0u, there ? q[i][1] : 0u, by);
+            *(lds_frag *)(to + lay<DP>::at(r, span * 2 + 1)) = code_values<T>(there ? q[i][2] : 0u, there ? q[i][3] : 0u, by);
         }
     }
 };
@@ -292,11 +307,15 @@ __device__ inline void kill_dead(f32x16 &s, uint32_t bits, int ahead, int lane, 
 
 // ------------------------------------------------------------------ bias by relative position
 
+// Borders are counted 16 at a time, so that a wave waits for one wide scalar load instead of 16.
 __device__ inline int bucket_of(const bias_table &t, int rel)
 {
     const int d = t.sides == 2 ? abs(rel) : max(-rel, 0);
     int n = 0;
-    for (int i = 0; i < t.count - 1; ++i) n += d >= t.border[i];
+    for (int i = 0; i < t.count - 1; i += 16) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) n += d >= t.border[i + k];
+    }
     return n + (t.sides == 2 && rel > 0 ? t.count : 0);
 }
 

@@ -137,8 +137,9 @@ __device__ inline int keys_end(const attn_in &p, int len, int last_pos)
 
 // ------------------------------------------------------------------ many rows
 //
-// A workgroup has 128 queries of one head, 32 a wave, and passes over the keys in tiles of 64 that all
-// four waves share, two tiles of keys and values in LDS in turn.
+// A wave has 32 queries of one head, a workgroup 128, and passes over the keys in tiles of 64 that its four waves
+// share, two tiles of keys and values in LDS in turn.  While the matrix units form the scores of the next 32 keys and add
+// these ones' values, the vector units make probabilities of these keys' scores.
 template <class T, int DP, bool CACHE>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn(attn_in p, attn_out out, int splits)
 {
@@ -148,22 +149,27 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn(attn_in p, attn
     __shared__ float by_distance[2 * MAX_FAR + 1];
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int q_tiles = (p.Q + ROWS - 1) / ROWS;
-    int w = die_order(blockIdx.x, gridDim.x);
+    int w = unit_order(blockIdx.x, p.B * p.K, p.G * splits * q_tiles);
     const int qt = q_tiles - 1 - w % q_tiles;  // the longest first, where queries see the keys before them
     w /= q_tiles;
     const int split = w % splits, bh = w / splits, b = bh / p.H, h = bh - b * p.H, kv = h / p.G;
     const int len = len_of(p, b), first = first_of(p, b);
-    const int q0 = qt * ROWS, q1 = min(q0 + ROWS, p.Q);
+    const int q0 = qt * ROWS, q1 = min(q0 + ROWS, p.Q), row0 = q0 + wave * 32;
     const int tiles = (keys_end(p, len, first + q1 - 1) + TILE - 1) / TILE, each = (tiles + splits - 1) / splits;
     const int t0 = split * each, t1 = min(tiles, t0 + each);
+    const int pos_lo = first + row0, pos_hi = pos_lo + 31;
 
-    const int i = q0 + wave * 32 + lane % 32;
-    const bool there = i < p.Q;
-    const int pos = first + i, pos_lo = first + q0 + wave * 32, pos_hi = pos_lo + 31;
+    const int i = row0 + lane % 32;
     frag<T> q[C];
-    load_stationary<T, DP>(q, p.q.at<T>(b, min(i, p.Q - 1), h), lane, p.D, there);
+    load_stationary<T, DP>(q, p.q.at<T>(b, min(i, p.Q - 1), h), lane, p.D, i < p.Q);
     const int far = p.bias.far;
-    if (p.bias.table) fill_bias<T>(by_distance, p, h, threadIdx.x, 256);
+    float far_behind = 0.0f, far_ahead = 0.0f;
+    if (p.bias.table) {
+        fill_bias<T>(by_distance, p, h, threadIdx.x, 256);
+        __syncthreads();
+        far_behind = by_distance[0];
+        far_ahead = by_distance[2 * far];
+    }
 
     tile_copy<DP, TILE, WAVES> kc, vc;
     tile_codes<T, DP, TILE, 256> kq, vq;
@@ -182,71 +188,180 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn(attn_in p, attn
         kc.set(wave, lane, p.k.t, p.D);
         vc.set(wave, lane, p.v.t, p.D);
     }
-    auto fetch = [&](int t, uint64_t live, lds_byte *kto, lds_byte *vto) __attribute__((always_inline)) {
-        const int64_t key = (int64_t)t * TILE;
-        if constexpr (CACHE) {
-            kq.load(threadIdx.x, ck + key * p.ld, ek + key / RKB_GROUP, p.ld, live);
-            vq.load(threadIdx.x, cv + key * p.ld, ev + key / RKB_GROUP, p.ld, live);
-        } else {
-            const bool all = live == ~(uint64_t)0 && p.D == DP;
-            kc.copy(wave, lane, (const char *)(kp + key * p.k.t), live, all, kto);
-            vc.copy(wave, lane, (const char *)(vp + key * p.v.t), live, all, vto);
-        }
+    // Keys come to LDS in tiles that start 32 keys after the tiles of values: the 64 from `key` on, which is no key before the first.
+    auto fetch_k = [&](int key, lds_byte *to) __attribute__((always_inline)) {
+        const int n = len - key;
+        if (n <= 0) return;
+        const uint64_t live = n >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << n) - 1;
+        if constexpr (CACHE)
+            kq.load(threadIdx.x, ck + (int64_t)key * p.ld, ek + key / RKB_GROUP, p.ld, live, n);
+        else
+            kc.copy(wave, lane, (const char *)(kp + (int64_t)key * p.k.t), live, n >= 64 && p.D == DP, to);
     };
-    auto settle = [&](lds_byte *kto, lds_byte *vto) __attribute__((always_inline)) {
-        if constexpr (CACHE) {
-            kq.put(threadIdx.x, kto);
-            vq.put(threadIdx.x, vto);
-        }
+    auto fetch_v = [&](int t, uint64_t live, lds_byte *to) __attribute__((always_inline)) {
+        const int64_t key = (int64_t)t * TILE;
+        if constexpr (CACHE)
+            vq.load(threadIdx.x, cv + key * p.ld, ev + key / RKB_GROUP, p.ld, live, len - (int)key);
+        else
+            vc.copy(wave, lane, (const char *)(vp + key * p.v.t), live, live == ~(uint64_t)0 && p.D == DP, to);
     };
 
-    f32x16 acc[A] = {};
+    f32x16 acc[A] = {}, sa, sb;
     running run;
+    float top = NEG_INF, by = p.c, add = 0.0f;  // of the piece that waits: x by + add are its scores in steps of log2, top the largest x
     const int k_place = L::rows_place(lane), v_place[2] = {L::cols_place(lane, 0), L::cols_place(lane, 1)};
-    auto compute = [&](int t, uint64_t live, lds_byte *kt, lds_byte *vt) __attribute__((always_inline)) {
-        const int key0 = t * TILE;
-        f32x16 s[2] = {};
-#pragma unroll
-        for (int c = 0; c < C; ++c)
-#pragma unroll
-            for (int n = 0; n < 2; ++n) s[n] = mma32(L::template rows<T>(kt, k_place, c, n * 32), q[c], s[n]);
-        float by = p.c;
-        if (p.bias.table) {
-            by = 1.0f;
-#pragma unroll
-            for (int n = 0; n < 2; ++n) add_bias(s[n], p.c, by_distance, far, key0 + n * 32, pos, pos_lo, pos_hi, lane);
+    // A piece that not all queries see alike: bias by distance, dead keys.  Then x are steps of log2 themselves.
+    // Before simple_end all queries see all keys of a piece, from as far as the bias tells apart.
+    const float add_simple = p.bias.table ? far_behind : 0.0f;
+    const int simple_end = p.mask ? INT_MIN : min(min(len, p.causal ? pos_lo + 1 : INT_MAX), p.bias.table ? pos_lo - far + 1 : INT_MAX) - 31;
+    auto adjust = [&](int key0, uint32_t live, f32x16 &s) __attribute__((always_inline)) {
+        if (key0 < simple_end) {
+            by = p.c;
+            add = add_simple;
+            return;
         }
+        const bool behind = key0 + 31 - pos_lo <= -far, ahead = key0 - pos_hi >= far, near = p.bias.table && !behind && !ahead;
+        by = p.c;
+        add = !p.bias.table || near ? 0.0f : behind ? far_behind : far_ahead;
+        if (!near && live == ~0u && !(p.causal && key0 + 31 > pos_lo)) return;
+        int me = lane;
+        asm volatile("" : "+v"(me));  // nothing of this is worked out ahead of the loop: it would hold registers in every turn
+        const int pos = pos_lo + me % 32;
+        if (near)
+            add_bias(s, p.c, by_distance, far, key0, pos, pos_lo, pos_hi, me);
+        else
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
-            kill_dead(s[n], (uint32_t)(live >> n * 32), p.causal ? pos - key0 - n * 32 : INT_MAX, lane, NEG_INF);
-        soften<T>(s, by, run, acc);
+            for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], p.c, add);
+        kill_dead(s, live, p.causal ? pos - key0 : INT_MAX, me, NEG_INF);
+        top = s[0];
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int r = 1; r < 16; ++r) top = fmaxf(top, s[r]);
+        by = 1.0f;
+        add = 0.0f;
+    };
+    // One turn: softens the piece `now`, adds its values (rows vn.. of vt), and forms the next piece's scores (rows kn.. of kt).
+    // What the vector units do is dealt out between the matrix instructions, in this order and no other.
+    auto turn = [&](lds_byte *kt, int kn, lds_byte *vt, int vn, f32x16 &now, f32x16 &then) __attribute__((always_inline)) {
+        constexpr int AHEAD = 4, EARLY = C / 4, N = C - EARLY, SKEW = 2;
+        auto pin = [] { __builtin_amdgcn_sched_barrier(0); };
+        frag<T> kf[AHEAD + 1], vf[AHEAD + 1], f[2];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const frag<T> f = to_frag<T>(s[n], half);
+        for (int c = 0; c < AHEAD; ++c) kf[c] = L::template rows<T>(kt, k_place, c, kn);
+        auto values = [&](int n) __attribute__((always_inline)) {  // the n-th fragment of both halves
+            return L::template cols<T>(vt, v_place, n % A, vn + n / A * 16);
+        };
+        auto read_ahead = [&](int c) __attribute__((always_inline)) {
+            if (c + AHEAD < C)
+                kf[(c + AHEAD) % (AHEAD + 1)] = L::template rows<T>(kt, k_place, c + AHEAD, kn);
+            else
+                vf[c + AHEAD - C] = values(c + AHEAD - C);
+        };
+        // the first products run while the maximum is looked at
 #pragma unroll
-                for (int a = 0; a < A; ++a) acc[a] = mma32(L::template cols<T>(vt, v_place, a, n * 32 + half * 16), f, acc[a]);
+        for (int c = 0; c < EARLY; ++c) {
+            read_ahead(c);
+            then = mma32(kf[c], q[c], c == 0 ? f32x16{} : then);
+        }
+        pin();
+        top = __builtin_fmaf(half_max(top), by, add);
+        if (__any(top > run.m + SLACK)) {
+            const float m = fmaxf(run.m, top), x = __builtin_amdgcn_exp2f(run.m - (m == NEG_INF ? 0.0f : m));
+            run.m = m;
+            run.l *= x;
+#pragma unroll
+            for (int a = 0; a < A; ++a) acc[a] *= x;
+        }
+        const float off = LIFT<T> + add - run.base();
+        // The 16 probabilities, in three steps that run SKEW of them apart, so that no instruction waits for the one before it.
+        float x[16], sum[2] = {};
+        auto scale = [&](int e) __attribute__((always_inline)) { x[e] = __builtin_fmaf(now[e], by, off); };
+        auto power = [&](int e) __attribute__((always_inline)) { x[e] = __builtin_amdgcn_exp2f(x[e]); };
+        auto soften = [&](int from, int to) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = from; e < to; ++e) {
+                if (e + 2 * SKEW < 16) scale(e + 2 * SKEW);
+                if (e + SKEW < 16) power(e + SKEW);
+                sum[e % 2] += x[e];
+                asm volatile("" : "+v"(sum[e % 2]));  // here, and not behind all products
+                f[e / 8][e % 8] = (T)x[e];
             }
+        };
+#pragma unroll
+        for (int e = 0; e < 2 * SKEW; ++e) scale(e);
+#pragma unroll
+        for (int e = 0; e < SKEW; ++e) power(e);
+        pin();
+#pragma unroll
+        for (int c = EARLY; c < C; ++c) {
+            read_ahead(c);
+            then = mma32(kf[c % (AHEAD + 1)], q[c], then);
+            soften((c - EARLY) * 8 / N, (c - EARLY + 1) * 8 / N);
+            pin();
+        }
+        float big[2];  // largest scores of the next piece
+        auto largest = [&](int from, int to) __attribute__((always_inline)) {
+            if (from == 0) big[0] = then[0], big[1] = then[1];
+#pragma unroll
+            for (int r = max(from, 2); r < to; ++r) {
+                big[r / 2 % 2] = fmaxf(big[r / 2 % 2], then[r]);
+                if (r % 4 == 3) asm volatile("" : "+v"(big[r / 2 % 2]));
+            }
+        };
+#pragma unroll
+        for (int n = 0; n < 2 * A; ++n) {
+            if (n + AHEAD < 2 * A) vf[(n + AHEAD) % (AHEAD + 1)] = values(n + AHEAD);
+            acc[n % A] = mma32(vf[n % (AHEAD + 1)], f[n / A], acc[n % A]);
+            if (n < A)
+                soften(8 + n * 8 / A, 8 + (n + 1) * 8 / A);
+            else
+                largest((n - A) * 16 / A, (n - A + 1) * 16 / A);
+            pin();
+        }
+        run.l += sum[0] + sum[1];
+        top = fmaxf(big[0], big[1]);
+        asm volatile("" : "+v"(run.l), "+v"(top));
     };
 
     if (t0 < t1) {
         uint8_t byte = mask_byte(p, b, t0 * TILE + lane, len);
-        uint64_t live = keys_alive(p, t0 * TILE, len, byte);
-        fetch(t0, live, (lds_byte *)k0, (lds_byte *)v0);
-        settle((lds_byte *)k0, (lds_byte *)v0);
+        uint64_t live = keys_alive(p, t0 * TILE, len, byte), next = 0;
         byte = mask_byte(p, b, (t0 + 1) * TILE + lane, len);
-        // One tile: the next one's copies go where the last one was, which all waves have read when they pass the barrier.
+        fetch_k(t0 * TILE, (lds_byte *)k1);  // whose first half is the first piece
+        if constexpr (CACHE) kq.put(threadIdx.x, (lds_byte *)k1);
+        fetch_k(t0 * TILE + 32, (lds_byte *)k0);
+        fetch_v(t0, live, (lds_byte *)v0);
+        if constexpr (CACHE) {
+            if (t0 * TILE + 32 < len) kq.put(threadIdx.x, (lds_byte *)k0);
+            vq.put(threadIdx.x, (lds_byte *)v0);
+        }
+        wait_all();
+        sa = f32x16{};
+#pragma unroll
+        for (int c = 0; c < C; ++c) sa = mma32(L::template rows<T>((lds_byte *)k1, k_place, c, 0), q[c], sa);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, sa[r]);
+        adjust(t0 * TILE, (uint32_t)live, sa);
+        // One tile of values, kh: the keys of its second piece and the next tile's first.  The next tiles go where the last ones
+        // were, which all waves have read when they pass the barrier.
         auto step = [&](int t, char *kh, char *vh, char *kn, char *vn) __attribute__((always_inline)) {
             wait_all();
-            uint64_t next = 0;
-            if (t + 1 < t1) {
+            const bool more = t + 1 < t1;
+            next = 0;
+            if (more) {
                 next = keys_alive(p, (t + 1) * TILE, len, byte);
                 byte = mask_byte(p, b, (t + 2) * TILE + lane, len);
-                fetch(t + 1, next, (lds_byte *)kn, (lds_byte *)vn);
+                fetch_k((t + 1) * TILE + 32, (lds_byte *)kn);
+                fetch_v(t + 1, next, (lds_byte *)vn);
             }
-            compute(t, live, (lds_byte *)kh, (lds_byte *)vh);
-            if (t + 1 < t1) settle((lds_byte *)kn, (lds_byte *)vn);
+            turn((lds_byte *)kh, 0, (lds_byte *)vh, 0, sa, sb);
+            adjust(t * TILE + 32, (uint32_t)(live >> 32), sb);
+            turn((lds_byte *)kh, 32, (lds_byte *)vh, 32, sb, sa);  // behind the last tile: scores of whatever lies there, not used
+            adjust((t + 1) * TILE, (uint32_t)next, sa);
+            if constexpr (CACHE)
+                if (more) {
+                    if ((t + 1) * TILE + 32 < len) kq.put(threadIdx.x, (lds_byte *)kn);
+                    vq.put(threadIdx.x, (lds_byte *)vn);
+                }
             live = next;
         };
         for (int t = t0; t < t1; t += 2) {
@@ -254,7 +369,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn(attn_in p, attn
             if (t + 1 < t1) step(t + 1, k1, v1, k0, v0);
         }
     }
-    finish<T, A>(p, out, split, b, i, h, there, run, half_sum(run.l), acc, lane);
+    finish<T, A>(p, out, split, b, i, h, i < p.Q, run, half_sum(run.l), acc, lane);
 }
 
 // ------------------------------------------------------------------ few rows
@@ -278,7 +393,7 @@ __global__ __launch_bounds__((DP == 256 ? 2 : 4) * WAVE, (FEW_BLOCKS<DP, CACHE, 
     __shared__ float ml[W][2][32];
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int rows = p.Q * p.G, row_tiles = (rows + 31) / 32;
-    int w = die_order(blockIdx.x, gridDim.x);
+    int w = unit_order(blockIdx.x, p.B * p.K, splits * row_tiles);
     const int rt = w % row_tiles;
     w /= row_tiles;
     const int split = w % splits, bk = w / splits, b = bk / p.K, kv = bk - b * p.K;
@@ -323,8 +438,8 @@ __global__ __launch_bounds__((DP == 256 ? 2 : 4) * WAVE, (FEW_BLOCKS<DP, CACHE, 
     auto fetch = [&](int t, uint32_t live, lds_byte *kto, lds_byte *vto) __attribute__((always_inline)) {
         const int64_t key = (int64_t)t * KEYS;
         if constexpr (CACHE) {
-            kq.load(lane, ck + key * p.ld, ek + t, p.ld, live);
-            vq.load(lane, cv + key * p.ld, ev + t, p.ld, live);
+            kq.load(lane, ck + key * p.ld, ek + t, p.ld, live, len - (int)key);
+            vq.load(lane, cv + key * p.ld, ev + t, p.ld, live, len - (int)key);
         } else {
             const bool all = live == ~0u && p.D == DP;
             kc.copy(0, lane, (const char *)(kp + key * p.k.t), live, all, kto);

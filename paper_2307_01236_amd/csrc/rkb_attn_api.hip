@@ -1,4 +1,5 @@
 // Attention's C entry points (rk_block.h): arguments checked, operands that are not aligned copied, launches cut.
+#include <climits>
 #include <cmath>
 #include <cstring>
 
@@ -61,6 +62,7 @@ void set_borders(bias_table &t, int max_distance)
         t.border[exact + i - 1] = n;
     }
     t.far = t.border[t.count - 2];
+    for (int i = t.count - 1; i < MAX_BUCKETS; ++i) t.border[i] = INT_MAX;
 }
 
 // ------------------------------------------------------------------ checks
@@ -239,7 +241,7 @@ static int split_of(int64_t blocks, int64_t want, int64_t most)
 attn_plan plan_fwd(const rkb_attn &a)
 {
     const int64_t rows = a.q_rows * (a.heads / a.kv_heads);
-    attn_plan plan;
+    attn_plan plan{};
     plan.few = rows <= 64;
     if (plan.few) {
         plan.blocks = a.batch * a.kv_heads * ((rows + 31) / 32);

@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
     __shared__ float by_distance[2 * MAX_FAR + 1];
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int q_tiles = (p.Q + ROWS - 1) / ROWS;
-    int w = die_order(blockIdx.x, gridDim.x);
+    int w = unit_order(blockIdx.x, p.B * p.K, p.G * splits * q_tiles);
     const int qt = q_tiles - 1 - w % q_tiles;
     w /= q_tiles;
     const int split = w % splits, bh = w / splits, b = bh / p.H, h = bh - b * p.H, kv = h / p.G;
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dk
     __shared__ float by_distance[2 * FAR + 1], sums[FAR ? WAVES : 1][2 * FAR + 1], diag[FAR ? WAVES : 1][FAR ? 8 * DIAG : 1];
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int k_tiles = (p.T + ROWS - 1) / ROWS;
-    int w = die_order(blockIdx.x, gridDim.x);
+    int w = unit_order(blockIdx.x, p.B * p.K, splits * k_tiles);
     const int kt = w % k_tiles;
     w /= k_tiles;
     const int split = w % splits, bk = w / splits, b = bk / p.K, kv = bk - b * p.K;
