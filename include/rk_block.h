@@ -169,8 +169,8 @@ typedef struct rkb_heads {
  * bias has half of its buckets for n <= 0 and the other half for n > 0, by distance |n|; a one-sided one has all
  * for the distance max(-n, 0).  Of nb buckets of a side the first e = nb / 2 (rounded down) are one distance each; from e on,
  * the bucket is e + floor((nb - e) ln(d / e) / ln(max_distance / e)), at most nb - 1, as exact arithmetic has it.
- * nb is 2 .. RKB_MAX_BUCKETS (and so is twice nb, where two-sided), e < max_distance <= RKB_MAX_DISTANCE.  An entry of -inf hides its keys as a mask
- * does; a finite one beyond 2e38 counts as 2.08e38.
+ * nb is 2 .. RKB_MAX_BUCKETS (and so is twice nb, where two-sided), e < max_distance <= RKB_MAX_DISTANCE.  An entry of -1e30 or less, -inf
+ * among them, hides its keys as a mask does, and its gradient is 0.
  *
  * dtype: RKB_F16 or RKB_BF16; 1 <= dim <= RKB_MAX_DIM; heads a multiple of kv_heads; 0 < scale < inf.
  */

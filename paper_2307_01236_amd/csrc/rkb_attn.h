@@ -203,7 +203,7 @@ __device__ inline frag<T> code_values(uint32_t lo, uint32_t hi, float step)
 template <class T, int DP, int ROWS, int LANES>
 struct tile_codes {
     static constexpr int EACH = ROWS * DP / 16 / LANES, SPANS = DP / 16, BLOCKS = ROWS / RKB_GROUP;
-    static_assert(ROWS * DP / 16 % LANES == 0);
+    static_assert(ROWS * DP / 16 % LANES == 0 && BLOCKS <= 2);
     u32x4 q[EACH];
     uint8_t exp[BLOCKS];
     uint64_t live;
@@ -233,8 +233,7 @@ struct tile_codes {
         for (int i = 0; i < EACH; ++i) {
             const int n = t + i * LANES, r = n / SPANS, span = n % SPANS;
             const bool there = all || ((live >> r & 1) && span < spans);
-            // which block: the same for all lanes, as a tile of 32 rows has one and 32 rows or more are between two lanes' rows
-            const float by = there ? step[i * BLOCKS / EACH] : 0.0f;
+            const float by = !there ? 0.0f : BLOCKS == 1 || r < RKB_GROUP ? step[0] : step[BLOCKS - 1];
             using lds_frag = __attribute__((address_space(3))) frag<T>;
             *(lds_frag *)(to + lay<DP>::at(r, span * 2)) = code_values<T>(there ? q[i][0] : 0u, there ? q[i][1] : 0u, by);
             *(lds_frag *)(to + lay<DP>::at(r, span * 2 + 1)) = code_values<T>(there ? q[i][2] : 0u, there ? q[i][3] : 0u, by);
@@ -319,13 +318,14 @@ __device__ inline int bucket_of(const bias_table &t, int rel)
     return n + (t.sides == 2 && rel > 0 ? t.count : 0);
 }
 
-// A table entry times log2(e); a finite one stays finite.
+// A table entry times log2(e).  One that is meant to hide its keys does: next to it a score, and the logarithm of a
+// row's sum, would be lost in 32 bits.
 template <class T>
 __device__ inline float table_value(const attn_in &p, int bucket, int h)
 {
     const int64_t i = (int64_t)bucket * p.H + h;
     const float v = p.bias.f32 ? ((const float *)p.bias.table)[i] : (float)((const T *)p.bias.table)[i];
-    return fabsf(v) <= 3.0e38f / LOG2E || !finite(fabsf(v)) ? v * LOG2E : copysignf(3.0e38f, v);
+    return v <= -1e30f ? NEG_INF : v * LOG2E;
 }
 
 // One head's bias by distance: entry n is that of relative position n - far.

@@ -1,69 +1,16 @@
 // Attention's C entry points (rk_block.h): arguments checked, operands that are not aligned copied, launches cut.
-#include <climits>
 #include <cmath>
 #include <cstring>
 
 #include "rkb_attn.h"
 #include "rkb_attn_args.h"
+#include "rkb_buckets.h"
 
 namespace rkb {
 namespace {
 
 constexpr int64_t MOST_BLOCKS = (int64_t)1 << 22;  // workgroups of a launch
 constexpr size_t WS_ALIGN_ATTN = 256;
-
-// ------------------------------------------------------------------ buckets of a bias
-
-// n^a m^b as 32-bit limbs, the lowest first.
-struct big {
-    uint32_t limb[64] = {1};
-    int size = 1;
-    void times(uint32_t m, int power)
-    {
-        for (; power > 0; --power) {
-            uint64_t carry = 0;
-            for (int i = 0; i < size; ++i) {
-                carry += (uint64_t)limb[i] * m;
-                limb[i] = (uint32_t)carry;
-                carry >>= 32;
-            }
-            if (carry) limb[size++] = (uint32_t)carry;
-        }
-    }
-    bool reaches(const big &o) const
-    {
-        if (size != o.size) return size > o.size;
-        for (int i = size - 1; i >= 0; --i)
-            if (limb[i] != o.limb[i]) return limb[i] > o.limb[i];
-        return true;
-    }
-};
-
-// The least distances of buckets 1 .. count - 1: of bucket exact + i, the least n with (n / exact)^wide >= (far / exact)^i.  A
-// product of roots is within 1e-16 of that power's root; a whole number as near as 1e-12 is decided by whole numbers.
-void set_borders(bias_table &t, int max_distance)
-{
-    const int exact = t.count / 2, wide = t.count - exact;
-    for (int i = 0; i < exact; ++i) t.border[i] = i + 1;
-    const double root = std::pow((double)max_distance / exact, 1.0 / wide);
-    double at = exact;
-    for (int i = 1; i < wide; ++i) {
-        at *= root;
-        const double whole = std::nearbyint(at);
-        int n = (int)std::ceil(at);
-        if (std::fabs(at - whole) < 1e-12 * at) {
-            big a, b;
-            a.times((uint32_t)whole, wide);
-            a.times((uint32_t)exact, i);
-            b.times((uint32_t)max_distance, i);
-            b.times((uint32_t)exact, wide);
-            n = (int)whole + (a.reaches(b) ? 0 : 1);
-        }
-        t.border[exact + i - 1] = n;
-    }
-    t.far = t.border[t.count - 2];
-    for (int i = t.count - 1; i < MAX_BUCKETS; ++i) t.border[i] = INT_MAX;
-}
 
 // ------------------------------------------------------------------ checks
 
@@ -144,7 +91,8 @@ attn_in make_in(const rkb_attn &a)
         p.bias.f32 = a.table_dtype == RKB_F32;
         p.bias.sides = a.two_sided ? 2 : 1;
         p.bias.count = a.buckets / p.bias.sides;
-        set_borders(p.bias, a.max_distance);
+        set_borders(p.bias.border, MAX_BUCKETS, p.bias.count, a.max_distance);
+        p.bias.far = p.bias.border[p.bias.count - 2];
     }
     return p;
 }
