@@ -15,7 +15,7 @@ constexpr int ROWS = 128, WAVES = 4;  // stationary rows and waves of a workgrou
 struct bwd_in {
     heads_at d_o, o;
     const float *o32, *lse;
-    float *delta, *lse2;     // [B, H, stats_rows]: do . o, and lse in steps of log2 (inf: a row without keys, or none)
+    float *delta, *lse2;     // [B, H, stats_rows]: do . o, and -lse in steps of log2 (-inf: a row without keys, or none)
     uint32_t *norms;         // f16: [B, K, 2]: bits of the largest |do|^2 and |v|^2
     int64_t stats_rows;
     heads_at dq, dk, dv;
@@ -91,7 +91,7 @@ __global__ __launch_bounds__(256) void k_attn_delta(attn_in p, bwd_in g)
             const int64_t at = (int64_t)bh * g.stats_rows + i;
             const float l = i < p.Q ? g.lse[(int64_t)bh * p.Q + i] : NEG_INF;
             g.delta[at] = l == NEG_INF ? 0.0f : sum;
-            g.lse2[at] = l == NEG_INF ? -NEG_INF : l * LOG2E;
+            g.lse2[at] = l == NEG_INF ? NEG_INF : -l * LOG2E;
         }
     }
     if constexpr (std::is_same_v<T, f16>) {
@@ -191,7 +191,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
     load_stationary<T, DP>(q, p.q.at<T>(b, min(i, p.Q - 1), h), lane, p.D, there);
     load_stationary<T, DP>(d, g.d_o.at<T>(b, min(i, p.Q - 1), h), lane, p.D, there);
     const int64_t stat = (int64_t)bh * g.stats_rows + min(i, (int)g.stats_rows - 1);
-    const float lse = there ? g.lse2[stat] : -NEG_INF, delta = there ? g.delta[stat] : 0.0f;
+    const float lse = there ? g.lse2[stat] : NEG_INF, delta = there ? g.delta[stat] : 0.0f;
     const float lift = ds_scale<T>(g, p, b, kv);
     const int far = p.bias.far;
     if (p.bias.table) fill_bias<T>(by_distance, p, h, threadIdx.x, 256);
@@ -229,7 +229,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
             kill_dead(s, (uint32_t)(live >> n * 32), p.causal ? pos - key0 : INT_MAX, lane, NEG_INF);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], by, -lse)) * (dp[r] - delta);
+                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], by, lse)) * (dp[r] - delta);
                 row_sum[r % 2] += s[r];
             }
             if constexpr (std::is_same_v<T, f16>) s *= lift;
@@ -266,7 +266,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
     if (there && g.dq.p) {
         const int64_t row = ((int64_t)b * p.Q + i) * p.H + h, rows = (int64_t)p.B * p.Q * p.H;
         store_grad<T, A>(g.dq.at<T>(b, i, h), g.dq_part ? g.dq_part + (split * rows + row) * p.D : nullptr, g.wide & 1, p.D,
-                         acc, p.scale / lift, lse == -NEG_INF, lane);
+                         acc, p.scale / lift, lse == NEG_INF, lane);
     }
     const float r = half_sum(row_sum[0] + row_sum[1]);
     if (there && lane < 32) {
@@ -306,28 +306,40 @@ __global__ __launch_bounds__(WAVE) void k_attn_dtable(attn_in p, const float *pa
 
 // ------------------------------------------------------------------ dk and dv
 //
-// A workgroup has 128 keys of one key head, 32 a wave, and passes over the queries of all heads that share it.
+// A workgroup has 128 keys of one key head, 32 a wave, and passes over the queries of all heads that share it in tiles of 32 (of q and do), RING of
+// them in LDS in turn.  While the matrix units form the next tile's scores and dp, the vector units make this tile's probabilities and ds, which
+// then enter dv and dk.  Heads of more than 128 columns are two workgroups', each with half of dk's and dv's columns: all of them do not fit
+// into registers.
 //
 // FAR: the largest distance that the bias looks up (0: no bias).  Its gradient, ds by buckets, is summed over diagonals: a wave lays the 8
 // queries x 32 keys of a register group into LDS at (query, key - query), whose columns are diagonals, and a lane adds up a column.  What no
-// register ever writes there stays 0.  Pieces that lie beyond FAR whole are added up in registers.
+// register ever writes there stays 0.  Tiles that lie beyond FAR whole are added up in registers.
 template <class T, int DP, int FAR>
 __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dkv(attn_in p, bwd_in g, int splits)
 {
     using L = lay<DP>;
-    constexpr int TILE = DP == 256 ? 32 : 64, N = TILE / 32, BYTES = TILE * DP * 2, C = DP / 16, A = DP / 32, DIAG = 41;
-    __shared__ __align__(16) char q0[BYTES], q1[BYTES], d0[BYTES], d1[BYTES];
-    __shared__ __align__(16) float lse0[64], lse1[64], del0[64], del1[64];
-    __shared__ float by_distance[2 * FAR + 1], sums[FAR ? WAVES : 1][2 * FAR + 1], diag[FAR ? WAVES : 1][FAR ? 8 * DIAG : 1];
+    constexpr int TILE = 32, BYTES = TILE * DP * 2, C = DP / 16, HALVES = DP / 128 > 1 ? 2 : 1, A = DP / 32 / HALVES, DIAG = 41;
+    // CARRY: the first fragments of the next turn are read at this one's end, so that its products need not wait for them.
+    constexpr bool CARRY = DP == 128;
+    // Tiles that LDS holds; of them a turn copies the one AHEAD further on, and finds that of NEED further on landed.
+    constexpr int RING = DP == 256 ? 3 : CARRY ? 6 : 4, AHEAD = DP == 256 ? 2 : CARRY ? 4 : 3, NEED = CARRY ? 2 : 1;
+    constexpr int FLYING = (AHEAD - 1 - NEED) * (2 * tile_copy<DP, TILE, WAVES>::MINE + 1);  // copies that may be on their way beyond those
+    constexpr int B3 = RING > 3 ? BYTES : 16, B5 = RING > 5 ? BYTES : 16;
+    __shared__ __align__(16) char q0[BYTES], q1[BYTES], q2[BYTES], q3[B3], q4[B5], q5[B5], d0[BYTES], d1[BYTES], d2[BYTES], d3[B3], d4[B5], d5[B5];
+    char *const qs[6] = {q0, q1, q2, q3, q4, q5}, *const ds[6] = {d0, d1, d2, d3, d4, d5};
+    __shared__ __align__(16) float stats[RING][WAVES][64];  // of each wave: 32 rows' -lse2, then their delta
+    __shared__ float by_distance[2][2 * FAR + 1], sums[FAR ? WAVES : 1][2 * FAR + 1], diag[FAR ? WAVES : 1][FAR ? 8 * DIAG : 1];
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int k_tiles = (p.T + ROWS - 1) / ROWS;
-    int w = unit_order(blockIdx.x, p.B * p.K, splits * k_tiles);
+    int w = unit_order(blockIdx.x, p.B * p.K, splits * k_tiles * HALVES);
+    const int a0 = w % HALVES * A;  // the first of this workgroup's column blocks of 32
+    w /= HALVES;
     const int kt = w % k_tiles;
     w /= k_tiles;
     const int split = w % splits, bk = w / splits, b = bk / p.K, kv = bk - b * p.K;
     const int len = len_of(p, b), first = first_of(p, b);
     const int wave_key = kt * ROWS + wave * 32, key = wave_key + lane % 32;
-    const bool alive = key < len && mask_byte(p, b, key, len);
+    const bool alive = key < len && mask_byte(p, b, key, len), all_alive = __all(alive);
 
     // queries that see any of the workgroup's keys: those from `from` on
     const int from = p.causal ? (int)min((int64_t)p.Q, max((int64_t)0, (int64_t)kt * ROWS - first)) : 0;
@@ -345,20 +357,25 @@ __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dk
     tile_copy<DP, TILE, WAVES> qc, dc;
     qc.set(wave, lane, p.q.t, p.D);
     dc.set(wave, lane, g.d_o.t, p.D);
-    auto fetch = [&](int h, int t, char *qto, char *dto, float *lse, float *del) __attribute__((always_inline)) {
-        const int row0 = t * TILE, n = p.Q - row0;
-        const uint64_t live = n >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << n) - 1;
+    // the next tile to be copied: head and tile of it
+    int copy_h = 0, copy_t = tile0;
+    auto fetch = [&](char *qto, char *dto, float *sto) __attribute__((always_inline)) {
+        const int h = kv * p.G + copy_h, row0 = copy_t * TILE, n = p.Q - row0;
+        const uint64_t live = n >= TILE ? 0xffffffffu : ((uint64_t)1 << n) - 1;
         const bool whole = n >= TILE && p.D == DP;
         qc.copy(wave, lane, (const char *)p.q.at<T>(b, row0, h), live, whole, (lds_byte *)qto);
         dc.copy(wave, lane, (const char *)g.d_o.at<T>(b, row0, h), live, whole, (lds_byte *)dto);
-        const int64_t stat = ((int64_t)b * p.H + h) * g.stats_rows + row0;
-        // 64 of each, of which a tile of 32 rows takes the first ones; rows are padded
-        const int at = min(lane, TILE - 1);
-        if (wave == 0) __builtin_amdgcn_global_load_lds((global_void *)(g.lse2 + stat + at), (lds_void *)(lds_byte *)lse, 4, 0, 0);
-        if (wave == 1) __builtin_amdgcn_global_load_lds((global_void *)(g.delta + stat + at), (lds_void *)(lds_byte *)del, 4, 0, 0);
+        const int64_t stat = ((int64_t)b * p.H + h) * g.stats_rows + row0 + lane % 32;  // rows are padded
+        const float *const from = lane < 32 ? g.lse2 + stat : g.delta + stat;
+        __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)(lds_byte *)(sto + wave * 64), 4, 0, 0);
+        if (++copy_t == q_tiles) {
+            copy_t = tile0;
+            ++copy_h;
+        }
     };
 
-    f32x16 dk[A] = {}, dv[A] = {};
+    f32x16 dk[A] = {}, dv[A] = {}, sa, sb, pa, pb;  // scores and dp of two tiles
+    float by = p.c, add = 0.0f;                     // of the tile that waits: its scores are x by + add in steps of log2
     const int place = L::rows_place(lane), cols[2] = {L::cols_place(lane, 0), L::cols_place(lane, 1)};
     float far_sum[2] = {0.0f, 0.0f};  // of keys far behind, far ahead
     auto add_up = [&](const f32x16 &ds, int pos0) __attribute__((always_inline)) {
@@ -367,23 +384,28 @@ __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dk
                 float sum[2] = {0.0f, 0.0f};
 #pragma unroll
                 for (int r = 0; r < 16; ++r) sum[r % 2] += ds[r];
-                far_sum[wave_key > pos0] += sum[0] + sum[1];
+                if (wave_key > pos0)
+                    far_sum[1] += sum[0] + sum[1];
+                else
+                    far_sum[0] += sum[0] + sum[1];
                 return;
             }
             float *const mine = diag[wave];
+            int me = lane;
+            asm volatile("" : "+v"(me));  // nothing of this is worked out ahead of the loop
 #pragma unroll
             for (int r8 = 0; r8 < 4; ++r8) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const int row = half_row(lane) + e;
-                    mine[row * DIAG + lane % 32 - row + 7] = ds[r8 * 4 + e];
+                    const int row = half_row(me) + e;
+                    mine[row * DIAG + me % 32 - row + 7] = ds[r8 * 4 + e];
                 }
                 asm volatile("" ::: "memory");  // other lanes read what this one wrote
-                if (lane < 39) {
+                if (me < 39) {
                     float sum = 0.0f;
 #pragma unroll
-                    for (int row = 0; row < 8; ++row) sum += mine[row * DIAG + lane];
-                    const int rel = wave_key - pos0 - r8 * 8 + lane - 7;
+                    for (int row = 0; row < 8; ++row) sum += mine[row * DIAG + me];
+                    const int rel = wave_key - pos0 - r8 * 8 + me - 7;
                     if (rel >= far)
                         far_sum[1] += sum;
                     else if (rel <= -far)
@@ -396,7 +418,7 @@ __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dk
         }
     };
     // What this workgroup found of a head's buckets goes to its place; the sums start again.
-    auto flush = [&](int h) __attribute__((always_inline)) {
+    auto flush = [&](int h) {
         if constexpr (FAR > 0) {
             if (!g.table_part) return;
             const float behind = lane_sum<64>(far_sum[0]), ahead = lane_sum<64>(far_sum[1]);
@@ -407,7 +429,7 @@ __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dk
             }
             __syncthreads();
             const int count = p.bias.count, buckets = count * p.bias.sides, c = threadIdx.x;
-            if (c < buckets) {
+            if (c < buckets && a0 == 0) {
                 const int side = c / count, n = c % count;
                 const int lo = n == 0 ? 0 : p.bias.border[n - 1], hi = n == count - 1 ? far : p.bias.border[n] - 1;
                 float sum = 0.0f;
@@ -423,62 +445,104 @@ __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dk
             for (int n = lane; n <= 2 * far; n += WAVE) sums[wave][n] = 0.0f;
         }
     };
-    auto compute = [&](int t, lds_byte *qt, lds_byte *dt, const float *lse, const float *del) __attribute__((always_inline)) {
+    // Scores of a tile that its lanes do not see alike: bias by distance, keys behind the query, dead keys (whose own sums are not stored, but the
+    // bias's would have them).  Then x are steps of log2 themselves.
+    auto adjust = [&](int hg, int t, f32x16 &s) __attribute__((always_inline)) {
+        const int pos0 = first + t * TILE;
+        by = p.c;
+        add = 0.0f;
+        bool near = false;
+        if constexpr (FAR > 0) {
+            const bool ahead = wave_key - pos0 - 31 >= far, behind = wave_key + 31 - pos0 <= -far;
+            near = !ahead && !behind;
+            if (!near) add = by_distance[hg & 1][ahead ? 2 * far : 0];
+        }
+        const bool hidden = p.causal && pos0 < wave_key + 31;
+        if (!near && !hidden && (FAR == 0 || all_alive)) return;
+        int me = lane;
+        asm volatile("" : "+v"(me));  // nothing of this is worked out ahead of the loop
+        const int rel = wave_key + me % 32 - pos0 - half_row(me);  // of register 0
 #pragma unroll
-        for (int n = 0; n < N; ++n) {
-            const int row0 = t * TILE + n * 32;
-            f32x16 s = {}, dp = {};
-#pragma unroll
-            for (int c = 0; c < C; ++c) {
-                s = mma32(L::template rows<T>(qt, place, c, n * 32), k[c], s);
-                dp = mma32(L::template rows<T>(dt, place, c, n * 32), v[c], dp);
-            }
-            f32x4 off[4], delta[4];
-#pragma unroll
-            for (int r8 = 0; r8 < 4; ++r8) {
-                off[r8] = *(const f32x4 *)(lse + n * 32 + r8 * 8 + half_row(lane));
-                delta[r8] = *(const f32x4 *)(del + n * 32 + r8 * 8 + half_row(lane));
-            }
-            float by = p.c;
-            if constexpr (FAR > 0) {
-                by = 1.0f;
-                const int pos_lo = first + row0, pos_hi = pos_lo + 31;
-                if (wave_key - pos_hi >= far || wave_key + 31 - pos_lo <= -far) {
-                    const float add = by_distance[wave_key - pos_hi >= far ? 2 * far : 0];
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], p.c, add);
-                } else {
-                    const int rel = key - pos_lo - half_row(lane) + far;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r)
-                        s[r] = __builtin_fmaf(s[r], p.c, by_distance[min(max(rel - r / 4 * 8 - r % 4, 0), 2 * far)]);
-                }
-            }
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], by, P_LIFT<T> - off[r / 4][r % 4]));
+        for (int r = 0; r < 16; ++r) {
+            const int d = rel - r / 4 * 8 - r % 4;
+            float x = __builtin_fmaf(s[r], p.c, add);
             if constexpr (FAR > 0)
-                if (!__all(alive)) {  // a dead key's own sums are not stored, but the bias's would have it
+                if (near) x = __builtin_fmaf(s[r], p.c, by_distance[hg & 1][min(max(d + far, 0), 2 * far)]);
+            s[r] = (hidden && d > 0) || (FAR > 0 && !alive) ? NEG_INF : x;
+        }
+        by = 1.0f;
+        add = 0.0f;
+    };
+    constexpr int READS = DP == 128 ? 4 : 3;  // fragments that are read ahead of their products
+    frag<T> rf[READS + 1];
+    f32x4 off[4], delta[4];
+    auto read_rows = [&](char *qn, char *dn, int n) __attribute__((always_inline)) {  // fragments of q and do in turn
+        return L::template rows<T>((lds_byte *)(n % 2 ? dn : qn), place, n / 2, 0);
+    };
+    // What a turn starts with: its tile's row sums, the next tile's first fragments.
+    auto start = [&](const float *stat, char *qn, char *dn) __attribute__((always_inline)) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) s[r] = alive ? s[r] : 0.0f;
-                }
-            if (p.causal && __any(first + row0 < key)) {
-                const int ahead = key - first - row0 - half_row(lane);  // rows before this do not see the key
+        for (int n = 0; n < READS; ++n) rf[n] = read_rows(qn, dn, n);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = r / 4 * 8 + r % 4 >= ahead ? s[r] : 0.0f;
+        for (int r8 = 0; r8 < 4; ++r8) {
+            off[r8] = *(const f32x4 *)(stat + r8 * 8 + half_row(lane));
+            delta[r8] = *(const f32x4 *)(stat + 32 + r8 * 8 + half_row(lane));
+        }
+    };
+    // One turn, started.  s and dp: this tile's, which lies in qh and dh; s2, dp2: the next one's, in qn and dn.  What the vector units do is
+    // dealt out between the matrix instructions: the first 16 queries' during the next tile's products, the others' during the first
+    // 16 queries' own.
+    auto turn = [&](char *qh, char *dh, char *qn, char *dn, f32x16 &s, f32x16 &dp, f32x16 &s2, f32x16 &dp2) __attribute__((always_inline)) {
+        constexpr int SKEW = 2, EARLY = 2, N = 2 * C - EARLY;  // EARLY: products that run before the row sums are there
+        auto pin = [] { __builtin_amdgcn_sched_barrier(0); };
+        auto here = [&](int n) __attribute__((always_inline)) {  // fragments of do and q in turn, of both halves
+            return L::template cols<T>((lds_byte *)(n % 2 ? qh : dh), cols, a0 + n / 2 % A, n / 2 / A * 16);
+        };
+        frag<T> cf[READS + 1], fp[2], fd[2];
+        float x[16];
+        auto scale = [&](int e) __attribute__((always_inline)) {
+            x[e] = __builtin_fmaf(s[e], by, FAR > 0 || P_LIFT<T> != 0.0f ? off[e / 4][e % 4] + (add + P_LIFT<T>) : off[e / 4][e % 4]);
+            dp[e] -= delta[e / 4][e % 4];
+        };
+        auto power = [&](int e) __attribute__((always_inline)) { x[e] = __builtin_amdgcn_exp2f(x[e]); };
+        auto soften = [&](int from, int to) __attribute__((always_inline)) {
+#pragma unroll
+            for (int e = from; e < to; ++e) {
+                if (e + 2 * SKEW < 16) scale(e + 2 * SKEW);
+                if (e + SKEW < 16) power(e + SKEW);
+                dp[e] *= x[e];
+                fp[e / 8][e % 8] = (T)x[e];
+                fd[e / 8][e % 8] = (T)(std::is_same_v<T, f16> ? dp[e] * ds_times : dp[e]);
             }
+        };
 #pragma unroll
-            for (int r = 0; r < 16; ++r) dp[r] = s[r] * (dp[r] - delta[r / 4][r % 4]);
-            if (FAR > 0) add_up(dp, first + row0);
-            if constexpr (std::is_same_v<T, f16>) dp *= ds_times;
+        for (int n = 0; n < 2 * C; ++n) {
+            if (n + READS < 2 * C)
+                rf[(n + READS) % (READS + 1)] = read_rows(qn, dn, n + READS);
+            else
+                cf[n + READS - 2 * C] = here(n + READS - 2 * C);
+            if (n % 2)
+                dp2 = mma32(rf[n % (READS + 1)], v[n / 2], n == 1 ? f32x16{} : dp2);
+            else
+                s2 = mma32(rf[n % (READS + 1)], k[n / 2], n == 0 ? f32x16{} : s2);
+            if (n == EARLY - 1) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const frag<T> fp = to_frag<T>(s, half), fd = to_frag<T>(dp, half);
+                for (int e = 0; e < 2 * SKEW; ++e) scale(e);
 #pragma unroll
-                for (int a = 0; a < A; ++a) {
-                    dv[a] = mma32(L::template cols<T>(dt, cols, a, n * 32 + half * 16), fp, dv[a]);
-                    dk[a] = mma32(L::template cols<T>(qt, cols, a, n * 32 + half * 16), fd, dk[a]);
-                }
+                for (int e = 0; e < SKEW; ++e) power(e);
             }
+            if (n >= EARLY) soften((n - EARLY) * 8 / N, (n - EARLY + 1) * 8 / N);
+            pin();
+        }
+#pragma unroll
+        for (int n = 0; n < 4 * A; ++n) {
+            if (n + READS < 4 * A) cf[(n + READS) % (READS + 1)] = here(n + READS);
+            if (n % 2)
+                dk[n / 2 % A] = mma32(cf[n % (READS + 1)], fd[n / 2 / A], dk[n / 2 % A]);
+            else
+                dv[n / 2 % A] = mma32(cf[n % (READS + 1)], fp[n / 2 / A], dv[n / 2 % A]);
+            if (n < 2 * A) soften(8 + n * 8 / (2 * A), 8 + (n + 1) * 8 / (2 * A));
+            pin();
         }
     };
 
@@ -488,49 +552,81 @@ __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dk
         for (int n = lane; n < 8 * DIAG; n += WAVE) diag[wave][n] = 0.0f;
     }
     if (t0 < t1) {
-        int hg = (int)(t0 / of_head), t = (int)(t0 - (int64_t)hg * of_head) + tile0, filled = -1;
+        int hg = (int)(t0 / of_head), t = (int)(t0 - (int64_t)hg * of_head) + tile0, filled = hg;
+        copy_h = hg;
+        copy_t = t;
         heads_done[0] = hg;
         heads_done[1] = (int)((t1 - 1) / of_head) + 1;
-        fetch(kv * p.G + hg, t, q0, d0, lse0, del0);
-        auto step = [&](int64_t s, char *qh, char *dh, float *lh, float *eh, char *qn, char *dn, float *ln, float *en) __attribute__((always_inline)) {
+        if constexpr (FAR > 0) {
+            fill_bias<T>(by_distance[hg & 1], p, kv * p.G + hg, threadIdx.x, 256);
+            if (hg + 1 < heads_done[1]) fill_bias<T>(by_distance[hg + 1 & 1], p, kv * p.G + hg + 1, threadIdx.x, 256);
+        }
+#pragma unroll
+        for (int n = 0; n < AHEAD; ++n)
+            if (t0 + n < t1) fetch(qs[n], ds[n], stats[n][0]);
+        wait_all();
+        sa = pa = f32x16{};
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            sa = mma32(L::template rows<T>((lds_byte *)q0, place, c, 0), k[c], sa);
+            pa = mma32(L::template rows<T>((lds_byte *)d0, place, c, 0), v[c], pa);
+        }
+        adjust(hg, t, sa);
+        if constexpr (CARRY) start(stats[0][wave], q1, d1);
+        // Tile `at`, the ring's n-th.  The one AHEAD further on goes where one was that all waves have read when they pass the barrier.  Copies land in
+        // order, so those of later tiles need not be waited for.
+        auto step = [&](int64_t at, auto place_in_ring) __attribute__((always_inline)) {
+            constexpr int n = place_in_ring(), HERE = n % RING, NEXT = (n + 1) % RING, THEN = (n + 2) % RING, COPY = (n + AHEAD) % RING;
+            f32x16 &s = n % 2 ? sb : sa, &dp = n % 2 ? pb : pa, &s2 = n % 2 ? sa : sb, &dp2 = n % 2 ? pa : pb;
             if constexpr (FAR > 0)
-                if (filled != hg) {  // another head's bias, once all waves are done with the last one's
-                    __syncthreads();
-                    if (filled >= 0) flush(kv * p.G + filled);
-                    fill_bias<T>(by_distance, p, kv * p.G + hg, threadIdx.x, 256);
+                if (filled != hg) {
+                    flush(kv * p.G + filled);
                     filled = hg;
+                    if (hg + 1 < heads_done[1]) fill_bias<T>(by_distance[hg + 1 & 1], p, kv * p.G + hg + 1, threadIdx.x, 256);
                 }
-            wait_all();
-            const int here = t;
-            if (s + 1 < t1) {
-                if (++t == q_tiles) {
-                    t = tile0;
-                    ++hg;
-                }
-                fetch(kv * p.G + hg, t, qn, dn, ln, en);
+            if (FLYING > 0 && at + AHEAD - 1 < t1)
+                __builtin_amdgcn_s_waitcnt(wait_copies(FLYING));
+            else
+                __builtin_amdgcn_s_waitcnt(wait_copies(0));
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (at + AHEAD < t1) fetch(qs[COPY], ds[COPY], stats[COPY][0]);
+            if constexpr (!CARRY) start(stats[HERE][wave], qs[NEXT], ds[NEXT]);
+            turn(qs[HERE], ds[HERE], qs[NEXT], ds[NEXT], s, dp, s2, dp2);
+            // behind the last tile: whatever lies there, not used
+            if constexpr (CARRY) start(stats[NEXT][wave], qs[THEN], ds[THEN]);
+            add_up(dp, first + t * TILE);
+            if (++t == q_tiles) {
+                t = tile0;
+                ++hg;
             }
-            compute(here, (lds_byte *)qh, (lds_byte *)dh, lh, eh);
+            if (at + 1 < t1) adjust(hg, t, s2);
         };
-        for (int64_t s = t0; s < t1; s += 2) {
-            step(s, q0, d0, lse0, del0, q1, d1, lse1, del1);
-            if (s + 1 < t1) step(s + 1, q1, d1, lse1, del1, q0, d0, lse0, del0);
+        for (int64_t at = t0; at < t1; at += RING == 4 ? 4 : 6) {
+            step(at, std::integral_constant<int, 0>());
+            if (at + 1 < t1) step(at + 1, std::integral_constant<int, 1>());
+            if (at + 2 < t1) step(at + 2, std::integral_constant<int, 2>());
+            if (at + 3 < t1) step(at + 3, std::integral_constant<int, 3>());
+            if constexpr (RING != 4) {
+                if (at + 4 < t1) step(at + 4, std::integral_constant<int, 4>());
+                if (at + 5 < t1) step(at + 5, std::integral_constant<int, 5>());
+            }
         }
         flush(kv * p.G + filled);
     }
     if constexpr (FAR > 0)
-        if (g.table_part) {
+        if (g.table_part && a0 == 0) {
             const int buckets = p.bias.count * p.bias.sides;
             const int64_t of_head = (int64_t)p.B * k_tiles * splits, me = ((int64_t)b * k_tiles + kt) * splits + split;
             for (int hg = 0; hg < p.G; ++hg)
                 if ((hg < heads_done[0] || hg >= heads_done[1]) && threadIdx.x < buckets)
                     g.table_part[((kv * p.G + hg) * of_head + me) * buckets + threadIdx.x] = 0.0f;
         }
-    if (key >= p.T) return;
-    const int64_t row = ((int64_t)b * p.T + key) * p.K + kv, rows = (int64_t)p.B * p.T * p.K, at = (split * rows + row) * p.D;
-    if (!g.dk.p) return;
-    store_grad<T, A>(g.dk.at<T>(b, key, kv), g.dk_part ? g.dk_part + at : nullptr, g.wide >> 1 & 1, p.D, dk, p.scale / lift,
-                     !alive, lane);
-    store_grad<T, A>(g.dv.at<T>(b, key, kv), g.dv_part ? g.dv_part + at : nullptr, g.wide >> 1 & 1, p.D, dv,
+    if (key >= p.T || !g.dk.p) return;
+    const int64_t row = ((int64_t)b * p.T + key) * p.K + kv, rows = (int64_t)p.B * p.T * p.K, at = (split * rows + row) * p.D + a0 * 32;
+    store_grad<T, A>(g.dk.at<T>(b, key, kv) + a0 * 32, g.dk_part ? g.dk_part + at : nullptr, g.wide >> 1 & 1, p.D - a0 * 32, dk, p.scale / lift, !alive, lane);
+    store_grad<T, A>(g.dv.at<T>(b, key, kv) + a0 * 32, g.dv_part ? g.dv_part + at : nullptr, g.wide >> 1 & 1, p.D - a0 * 32, dv,
                      __builtin_amdgcn_exp2f(-P_LIFT<T>), !alive, lane);
 }
 
@@ -614,7 +710,7 @@ int run_attn_bwd(const attn_in &p, const rkb_attn &a, const attn_bwd_plan &plan,
         if (rc != RKB_OK) return rc;
         return with_width(a.dim, [&](auto dp) {
             constexpr int DP = dp();
-            const dim3 q_grid((uint32_t)(plan.q_blocks * plan.q_splits)), k_grid((uint32_t)(plan.k_blocks * plan.k_splits));
+            const dim3 q_grid((uint32_t)(plan.q_blocks * plan.q_splits)), k_grid((uint32_t)(plan.k_blocks * plan.k_splits * (DP == 256 ? 2 : 1)));
             int rc = RKB_OK;
             auto join = [&](const grad_join &x, const grad_join &y, int splits, int jobs) {
                 const int64_t blocks = std::min<int64_t>((x.rows * a.dim + 255) / 256, 1 << 16);
