@@ -328,11 +328,14 @@ __device__ inline float table_value(const attn_in &p, int bucket, int h)
     return v <= -1e30f ? NEG_INF : v * LOG2E;
 }
 
-// One head's bias by distance: entry n is that of relative position n - far.
+// One head's bias by distance: entry n is that of relative position n - far - PAD.  Beyond far the last buckets go on for as
+// much as 32 queries x 32 keys that reach nearer than far can pass it, so that nothing is clamped.
+constexpr int PAD = 64;
+
 template <class T>
 __device__ inline void fill_bias(float *by_distance, const attn_in &p, int h, int t, int lanes)
 {
-    for (int n = t; n <= 2 * p.bias.far; n += lanes) by_distance[n] = table_value<T>(p, bucket_of(p.bias, n - p.bias.far), h);
+    for (int n = t; n <= 2 * (p.bias.far + PAD); n += lanes) by_distance[n] = table_value<T>(p, bucket_of(p.bias, n - p.bias.far - PAD), h);
 }
 
 // Adds a head's bias to a 32-key piece of scores: key0 the piece's first key, pos the lane's query; pos_lo and pos_hi
@@ -340,13 +343,13 @@ __device__ inline void fill_bias(float *by_distance, const attn_in &p, int h, in
 __device__ inline void add_bias(f32x16 &s, float c, const float *by_distance, int far, int key0, int pos, int pos_lo, int pos_hi, int lane)
 {
     if (key0 - pos_hi >= far || key0 + 31 - pos_lo <= -far) {
-        const float b = by_distance[key0 - pos_hi >= far ? 2 * far : 0];
+        const float b = by_distance[key0 - pos_hi >= far ? 2 * (far + PAD) : 0];
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], c, b);
     } else {
-        const int d = key0 + half_row(lane) - pos + far;
+        const float *const at = by_distance + key0 + half_row(lane) - pos + far + PAD;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], c, by_distance[min(max(d + r / 4 * 8 + r % 4, 0), 2 * far)]);
+        for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], c, at[r / 4 * 8 + r % 4]);
     }
 }
 

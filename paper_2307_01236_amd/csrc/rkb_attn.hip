@@ -146,7 +146,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn(attn_in p, attn
     using L = lay<DP>;
     constexpr int BYTES = TILE * DP * 2, C = DP / 16, A = DP / 32;
     __shared__ __align__(16) char k0[BYTES], k1[BYTES], v0[BYTES], v1[BYTES];
-    __shared__ float by_distance[2 * MAX_FAR + 1];
+    __shared__ float by_distance[2 * (MAX_FAR + PAD) + 1];
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int q_tiles = (p.Q + ROWS - 1) / ROWS;
     int w = unit_order(blockIdx.x, p.B * p.K, p.G * splits * q_tiles);
@@ -168,7 +168,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn(attn_in p, attn
         fill_bias<T>(by_distance, p, h, threadIdx.x, 256);
         __syncthreads();
         far_behind = by_distance[0];
-        far_ahead = by_distance[2 * far];
+        far_ahead = by_distance[2 * (far + PAD)];
     }
 
     tile_copy<DP, TILE, WAVES> kc, vc;

@@ -171,7 +171,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
     using L = lay<DP>;
     constexpr int TILE = DP == 256 ? 32 : 64, N = TILE / 32, BYTES = TILE * DP * 2, C = DP / 16, A = DP / 32;
     __shared__ __align__(16) char k0[BYTES], k1[BYTES], v0[BYTES], v1[BYTES];
-    __shared__ float by_distance[2 * MAX_FAR + 1];
+    __shared__ float by_distance[2 * (MAX_FAR + PAD) + 1];
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int q_tiles = (p.Q + ROWS - 1) / ROWS;
     int w = unit_order(blockIdx.x, p.B * p.K, p.G * splits * q_tiles);
@@ -311,16 +311,18 @@ __global__ __launch_bounds__(WAVE) void k_attn_dtable(attn_in p, const float *pa
 // then enter dv and dk.  Heads of more than 128 columns are two workgroups', each with half of dk's and dv's columns: all of them do not fit
 // into registers.
 //
-// FAR: the largest distance that the bias looks up (0: no bias).  Its gradient, ds by buckets, is summed over diagonals: a wave lays the 8
-// queries x 32 keys of a register group into LDS at (query, key - query), whose columns are diagonals, and a lane adds up a column.  What no
+// FAR: the largest distance that the bias looks up (0: no bias).  Its gradient, ds by buckets, is summed over diagonals: a wave lays the
+// queries x 32 keys of some registers into LDS at (query, key - query), whose columns are diagonals, and a lane adds up a column.  What no
 // register ever writes there stays 0.  Tiles that lie beyond FAR whole are added up in registers.
 template <class T, int DP, int FAR>
 __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dkv(attn_in p, bwd_in g, int splits)
 {
     using L = lay<DP>;
-    constexpr int TILE = 32, BYTES = TILE * DP * 2, C = DP / 16, HALVES = DP / 128 > 1 ? 2 : 1, A = DP / 32 / HALVES, DIAG = 41;
+    constexpr int TILE = 32, BYTES = TILE * DP * 2, C = DP / 16, HALVES = DP / 128 > 1 ? 2 : 1, A = DP / 32 / HALVES;
+    // DIAG queries are laid out at a time, in AREAS places in turn (the fewer where little LDS is left); the pitch keeps a wave's writes in different banks
+    constexpr int DIAG = DP == 256 && FAR > 128 ? 8 : 16, AREAS = DIAG == 16 ? 2 : 1, PITCH = DIAG == 16 ? 57 : 41;
     // CARRY: the first fragments of the next turn are read at this one's end, so that its products need not wait for them.
-    constexpr bool CARRY = DP == 128;
+    constexpr bool CARRY = DP == 128 && FAR <= 128;
     // Tiles that LDS holds; of them a turn copies the one AHEAD further on, and finds that of NEED further on landed.
     constexpr int RING = DP == 256 ? 3 : CARRY ? 6 : 4, AHEAD = DP == 256 ? 2 : CARRY ? 4 : 3, NEED = CARRY ? 2 : 1;
     constexpr int FLYING = (AHEAD - 1 - NEED) * (2 * tile_copy<DP, TILE, WAVES>::MINE + 1);  // copies that may be on their way beyond those
@@ -328,7 +330,7 @@ __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dk
     __shared__ __align__(16) char q0[BYTES], q1[BYTES], q2[BYTES], q3[B3], q4[B5], q5[B5], d0[BYTES], d1[BYTES], d2[BYTES], d3[B3], d4[B5], d5[B5];
     char *const qs[6] = {q0, q1, q2, q3, q4, q5}, *const ds[6] = {d0, d1, d2, d3, d4, d5};
     __shared__ __align__(16) float stats[RING][WAVES][64];  // of each wave: 32 rows' -lse2, then their delta
-    __shared__ float by_distance[2][2 * FAR + 1], sums[FAR ? WAVES : 1][2 * FAR + 1], diag[FAR ? WAVES : 1][FAR ? 8 * DIAG : 1];
+    __shared__ float by_distance[2][FAR ? 2 * (FAR + PAD) + 1 : 1], sums[FAR ? WAVES : 1][2 * FAR + 1], diag[FAR ? WAVES : 1][FAR ? AREAS : 1][FAR ? DIAG * PITCH : 1];
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int k_tiles = (p.T + ROWS - 1) / ROWS;
     int w = unit_order(blockIdx.x, p.B * p.K, splits * k_tiles * HALVES);
@@ -357,21 +359,28 @@ __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dk
     tile_copy<DP, TILE, WAVES> qc, dc;
     qc.set(wave, lane, p.q.t, p.D);
     dc.set(wave, lane, g.d_o.t, p.D);
-    // the next tile to be copied: head and tile of it
-    int copy_h = 0, copy_t = tile0;
+    // the next tile to be copied: its tile, and where its rows and row sums are
+    int copy_t = 0, copy_h = 0;
+    const char *copy_q = nullptr, *copy_d = nullptr;
+    const float *copy_s = nullptr;
+    const int64_t q_step = TILE * p.q.t * 2, d_step = TILE * g.d_o.t * 2;
+    auto copy_from = [&](int h, int t) __attribute__((always_inline)) {
+        copy_t = t;
+        copy_q = (const char *)p.q.at<T>(b, (int64_t)t * TILE, h);
+        copy_d = (const char *)g.d_o.at<T>(b, (int64_t)t * TILE, h);
+        copy_s = (lane < 32 ? g.lse2 : g.delta) + ((int64_t)b * p.H + h) * g.stats_rows + t * TILE + lane % 32;  // rows are padded
+    };
     auto fetch = [&](char *qto, char *dto, float *sto) __attribute__((always_inline)) {
-        const int h = kv * p.G + copy_h, row0 = copy_t * TILE, n = p.Q - row0;
+        const int n = p.Q - copy_t * TILE;
         const uint64_t live = n >= TILE ? 0xffffffffu : ((uint64_t)1 << n) - 1;
         const bool whole = n >= TILE && p.D == DP;
-        qc.copy(wave, lane, (const char *)p.q.at<T>(b, row0, h), live, whole, (lds_byte *)qto);
-        dc.copy(wave, lane, (const char *)g.d_o.at<T>(b, row0, h), live, whole, (lds_byte *)dto);
-        const int64_t stat = ((int64_t)b * p.H + h) * g.stats_rows + row0 + lane % 32;  // rows are padded
-        const float *const from = lane < 32 ? g.lse2 + stat : g.delta + stat;
-        __builtin_amdgcn_global_load_lds((global_void *)from, (lds_void *)(lds_byte *)(sto + wave * 64), 4, 0, 0);
-        if (++copy_t == q_tiles) {
-            copy_t = tile0;
-            ++copy_h;
-        }
+        qc.copy(wave, lane, copy_q, live, whole, (lds_byte *)qto);
+        dc.copy(wave, lane, copy_d, live, whole, (lds_byte *)dto);
+        __builtin_amdgcn_global_load_lds((global_void *)copy_s, (lds_void *)(lds_byte *)(sto + wave * 64), 4, 0, 0);
+        copy_q += q_step;
+        copy_d += d_step;
+        copy_s += TILE;
+        if (++copy_t == q_tiles) copy_from(++copy_h, tile0);
     };
 
     f32x16 dk[A] = {}, dv[A] = {}, sa, sb, pa, pb;  // scores and dp of two tiles
@@ -390,30 +399,47 @@ __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dk
                     far_sum[0] += sum[0] + sum[1];
                 return;
             }
-            float *const mine = diag[wave];
             int me = lane;
             asm volatile("" : "+v"(me));  // nothing of this is worked out ahead of the loop
+            constexpr int PARTS = 32 / DIAG;
+            auto lay_out = [&](int part) __attribute__((always_inline)) {
+                float *const to = diag[wave][part % AREAS] + half_row(me) * (PITCH - 1) + me % 32 + DIAG - 1;
 #pragma unroll
-            for (int r8 = 0; r8 < 4; ++r8) {
+                for (int r = 0; r < DIAG / 2; ++r) to[(r / 4 * 8 + r % 4) * (PITCH - 1)] = ds[part * (DIAG / 2) + r];
+            };
+            auto collect = [&](int part) __attribute__((always_inline)) {
+                if (me < 31 + DIAG) {
+                    const float *const from = diag[wave][part % AREAS] + me;
+                    float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int row = half_row(me) + e;
-                    mine[row * DIAG + me % 32 - row + 7] = ds[r8 * 4 + e];
-                }
-                asm volatile("" ::: "memory");  // other lanes read what this one wrote
-                if (me < 39) {
-                    float sum = 0.0f;
-#pragma unroll
-                    for (int row = 0; row < 8; ++row) sum += mine[row * DIAG + me];
-                    const int rel = wave_key - pos0 - r8 * 8 + me - 7;
+                    for (int row = 0; row < DIAG; ++row) sum[row % 2] += from[row * PITCH];
+                    const int rel = wave_key - pos0 - part * DIAG + me - (DIAG - 1);
                     if (rel >= far)
-                        far_sum[1] += sum;
+                        far_sum[1] += sum[0] + sum[1];
                     else if (rel <= -far)
-                        far_sum[0] += sum;
+                        far_sum[0] += sum[0] + sum[1];
                     else
-                        sums[wave][rel + far] += sum;
+                        sums[wave][rel + far] += sum[0] + sum[1];
                 }
+            };
+            // what one lane writes others read: in this order
+            if constexpr (AREAS == PARTS) {
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part) lay_out(part);
                 asm volatile("" ::: "memory");
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part) {
+                    collect(part);
+                    asm volatile("" ::: "memory");
+                }
+            } else {
+#pragma unroll
+                for (int part = 0; part < PARTS; ++part) {
+                    lay_out(part);
+                    asm volatile("" ::: "memory");
+                    collect(part);
+                    asm volatile("" ::: "memory");
+                }
             }
         }
     };
@@ -455,25 +481,29 @@ __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dk
         if constexpr (FAR > 0) {
             const bool ahead = wave_key - pos0 - 31 >= far, behind = wave_key + 31 - pos0 <= -far;
             near = !ahead && !behind;
-            if (!near) add = by_distance[hg & 1][ahead ? 2 * far : 0];
+            if (!near) add = by_distance[hg & 1][ahead ? 2 * (far + PAD) : 0];
         }
         const bool hidden = p.causal && pos0 < wave_key + 31;
         if (!near && !hidden && (FAR == 0 || all_alive)) return;
         int me = lane;
         asm volatile("" : "+v"(me));  // nothing of this is worked out ahead of the loop
         const int rel = wave_key + me % 32 - pos0 - half_row(me);  // of register 0
+        if (FAR > 0 && near) {
+            const float *const at = by_distance[hg & 1] + rel + far + PAD;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int d = rel - r / 4 * 8 - r % 4;
-            float x = __builtin_fmaf(s[r], p.c, add);
-            if constexpr (FAR > 0)
-                if (near) x = __builtin_fmaf(s[r], p.c, by_distance[hg & 1][min(max(d + far, 0), 2 * far)]);
-            s[r] = (hidden && d > 0) || (FAR > 0 && !alive) ? NEG_INF : x;
+            for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], p.c, at[-(r / 4 * 8 + r % 4)]);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = __builtin_fmaf(s[r], p.c, add);
+        }
+        if (hidden || (FAR > 0 && !all_alive)) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[r] = (hidden && rel > r / 4 * 8 + r % 4) || (FAR > 0 && !alive) ? NEG_INF : s[r];
         }
         by = 1.0f;
         add = 0.0f;
     };
-    constexpr int READS = DP == 128 ? 4 : 3;  // fragments that are read ahead of their products
+    constexpr int READS = CARRY ? 4 : DP == 256 ? 2 : 3;  // fragments that are read ahead of their products
     frag<T> rf[READS + 1];
     f32x4 off[4], delta[4];
     auto read_rows = [&](char *qn, char *dn, int n) __attribute__((always_inline)) {  // fragments of q and do in turn
@@ -549,12 +579,12 @@ __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dk
     int heads_done[2] = {0, 0};  // heads that this workgroup left sums of
     if constexpr (FAR > 0) {
         for (int n = lane; n <= 2 * far; n += WAVE) sums[wave][n] = 0.0f;
-        for (int n = lane; n < 8 * DIAG; n += WAVE) diag[wave][n] = 0.0f;
+        for (int n = lane; n < AREAS * DIAG * PITCH; n += WAVE) diag[wave][0][n] = 0.0f;
     }
     if (t0 < t1) {
         int hg = (int)(t0 / of_head), t = (int)(t0 - (int64_t)hg * of_head) + tile0, filled = hg;
-        copy_h = hg;
-        copy_t = t;
+        copy_h = kv * p.G + hg;
+        copy_from(copy_h, t);
         heads_done[0] = hg;
         heads_done[1] = (int)((t1 - 1) / of_head) + 1;
         if constexpr (FAR > 0) {
