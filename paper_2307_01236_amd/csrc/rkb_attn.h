@@ -182,19 +182,27 @@ struct tile_copy {
     }
 };
 
+// A word's n-th byte as a signed whole number.  (One instruction; written out it becomes two or three, which the compiler also
+// moves ahead of a loop's turn, where four words wait instead of one.)
+template <int n>
+__device__ inline float code_of(uint32_t word)
+{
+    float v;
+    if constexpr (n == 0) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_0" : "=v"(v) : "v"(word));
+    if constexpr (n == 1) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_1" : "=v"(v) : "v"(word));
+    if constexpr (n == 2) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_2" : "=v"(v) : "v"(word));
+    if constexpr (n == 3) asm("v_cvt_f32_i32_sdwa %0, sext(%1) dst_sel:DWORD dst_unused:UNUSED_PAD src0_sel:BYTE_3" : "=v"(v) : "v"(word));
+    return v;
+}
+
 // Eight codes as values of T: whole numbers of up to 8 bits times a power of two, exact.
 template <class T>
 __device__ inline frag<T> code_values(uint32_t lo, uint32_t hi, float step)
 {
+    const float v[8] = {code_of<0>(lo), code_of<1>(lo), code_of<2>(lo), code_of<3>(lo), code_of<0>(hi), code_of<1>(hi), code_of<2>(hi), code_of<3>(hi)};
     frag<T> f;
-    const uint32_t u[2] = {lo ^ 0x80808080u, hi ^ 0x80808080u};
-    const bool high = step >= 0x1p114f;  // 128 steps may pass 32 bits' range
-    const float back = high ? 0.0f : -128.0f * step;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float v = (float)(u[i / 4] >> i % 4 * 8 & 0xff);
-        f[i] = (T)(high ? (v - 128.0f) * step : __builtin_fmaf(v, step, back));
-    }
+    for (int i = 0; i < 8; ++i) f[i] = (T)(v[i] * step);
     return f;
 }
 

@@ -375,7 +375,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn(attn_in p, attn
 // ------------------------------------------------------------------ few rows
 //
 // A workgroup has up to 32 rows of one key head: queries and the heads that share it, queries first.  Each wave takes keys of its
-// own, in tiles of 32 that no other wave waits for, and the waves' sums are joined at the end.
+// own, in tiles of 32 that no other wave waits for, and the waves' sums are joined at the end.  A cache's keys go from
+// memory to the matrix units' registers (a lane has 16 neighbouring columns of a key, and all keys' and queries' columns are taken in that
+// order), its values through LDS, to be read by columns; two tiles of both wait in registers until they are due.
 template <int DP, bool CACHE, bool BIAS>
 constexpr int FEW_BLOCKS = (DP == 256 ? 2 : 4) * 32 * DP * 2 * (CACHE ? 2 : 4) + (BIAS ? 32 * (MAX_BUCKETS + 1) * 4 + 2 * MAX_FAR + 1 : 0) + 2048 <=
                                    80 * 1024 && DP < 256 ? 2 : 1;  // workgroups of a compute unit, by LDS
@@ -385,7 +387,7 @@ __global__ __launch_bounds__((DP == 256 ? 2 : 4) * WAVE, (FEW_BLOCKS<DP, CACHE, 
 {
     using L = lay<DP>;
     constexpr int W = DP == 256 ? 2 : 4, KEYS = 32, BYTES = KEYS * DP * 2, C = DP / 16, A = DP / 32;
-    // what a wave copies ahead of its work; a cache's tiles wait in registers instead
+    // what a wave copies ahead of its work; a cache's tiles wait in registers instead.  (k0 takes part in the join of the waves.)
     constexpr int SPARE = CACHE ? 16 : W * BYTES;
     __shared__ __align__(16) char k0[W * BYTES], v0[W * BYTES], k1[SPARE], v1[SPARE];
     __shared__ float table[BIAS ? 32 * (MAX_BUCKETS + 1) : 1];
@@ -406,7 +408,14 @@ __global__ __launch_bounds__((DP == 256 ? 2 : 4) * WAVE, (FEW_BLOCKS<DP, CACHE, 
     const int t0 = (split * W + wave) * each, t1 = min(tiles, t0 + each);
 
     frag<T> q[C];
-    load_stationary<T, DP>(q, p.q.at<T>(b, i, h), lane, p.D, there);
+    const T *const row = p.q.at<T>(b, i, h);
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int col = c / 2 * 32 + lane / 32 * 16 + c % 2 * 8;
+        frag<T> z = {};
+        if (there && col < p.D) z = *(const frag<T> *)(row + col);
+        q[c] = z;
+    }
     const int buckets = p.bias.sides * p.bias.count, far = p.bias.far;
     if constexpr (BIAS) {
         for (int n = threadIdx.x; n <= 2 * far; n += W * WAVE) bucket[n] = (uint8_t)bucket_of(p.bias, n - far);
@@ -419,7 +428,12 @@ __global__ __launch_bounds__((DP == 256 ? 2 : 4) * WAVE, (FEW_BLOCKS<DP, CACHE, 
     const float *mine = table + lane % 32 * (buckets + 1);
 
     tile_copy<DP, KEYS, 1> kc, vc;
-    tile_codes<T, DP, KEYS, WAVE> kq, vq;
+    struct waiting {  // a cache's tile: this lane's codes of its key, and the values'
+        u32x4 k[C / 2];
+        uint8_t exp;
+        tile_codes<T, DP, KEYS, WAVE> v;
+        uint32_t live;
+    } first_tile, second_tile;
     const T *kp = nullptr, *vp = nullptr;
     const int8_t *ck = nullptr, *cv = nullptr;
     const uint8_t *ek = nullptr, *ev = nullptr;
@@ -435,11 +449,18 @@ __global__ __launch_bounds__((DP == 256 ? 2 : 4) * WAVE, (FEW_BLOCKS<DP, CACHE, 
         kc.set(0, lane, p.k.t, p.D);
         vc.set(0, lane, p.v.t, p.D);
     }
-    auto fetch = [&](int t, uint32_t live, lds_byte *kto, lds_byte *vto) __attribute__((always_inline)) {
+    // A tile on its way: copied to LDS, or a cache's to registers.  Of rows and columns that do not exist the last ones that do are
+    // read instead: such scores are replaced, such columns meet zeros of the query.
+    auto fetch = [&](int t, uint32_t live, waiting &to, lds_byte *kto, lds_byte *vto) __attribute__((always_inline)) {
         const int64_t key = (int64_t)t * KEYS;
         if constexpr (CACHE) {
-            kq.load(lane, ck + key * p.ld, ek + t, p.ld, live, len - (int)key);
-            vq.load(lane, cv + key * p.ld, ev + t, p.ld, live, len - (int)key);
+            const int rows = len - (int)key, spans = (int)p.ld / 16;
+            const int8_t *const from = ck + (key + min(lane % 32, rows - 1)) * p.ld;
+#pragma unroll
+            for (int c = 0; c < C / 2; ++c) to.k[c] = *(const u32x4 *)(from + min(c * 2 + lane / 32, spans - 1) * 16);
+            to.exp = ek[t];
+            to.live = live;
+            to.v.load(lane, cv + key * p.ld, ev + t, p.ld, live, rows);
         } else {
             const bool all = live == ~0u && p.D == DP;
             kc.copy(0, lane, (const char *)(kp + key * p.k.t), live, all, kto);
@@ -449,12 +470,24 @@ __global__ __launch_bounds__((DP == 256 ? 2 : 4) * WAVE, (FEW_BLOCKS<DP, CACHE, 
 
     f32x16 acc[A] = {};
     running run;
-    const int k_place = L::rows_place(lane), v_place[2] = {L::cols_place(lane, 0), L::cols_place(lane, 1)};
-    auto compute = [&](int t, uint32_t live, lds_byte *kt, lds_byte *vt) __attribute__((always_inline)) {
-        const int key0 = t * KEYS;
-        f32x16 s[1] = {};
+    const int k_place = L::at(lane % 32, lane / 32 * 2), v_place[2] = {L::cols_place(lane, 0), L::cols_place(lane, 1)};
+    auto score = [&](const waiting &w, lds_byte *kt) __attribute__((always_inline)) {
+        f32x16 s = {};
+        const float step = !CACHE || w.exp == 0 ? 0.0f : step_of(w.exp);
 #pragma unroll
-        for (int c = 0; c < C; ++c) s[0] = mma32(L::template rows<T>(kt, k_place, c, 0), q[c], s[0]);
+        for (int c = 0; c < C; ++c) {
+            frag<T> f;
+            if constexpr (CACHE)
+                f = code_values<T>(w.k[c / 2][c % 2 * 2], w.k[c / 2][c % 2 * 2 + 1], step);
+            else
+                f = *(__attribute__((address_space(3))) frag<T> *)(kt + (k_place ^ (c / 2 * 64 + c % 2 * 16)));
+            s = mma32(f, q[c], s);
+        }
+        return s;
+    };
+    auto compute = [&](int t, uint32_t live, const f32x16 &raw, lds_byte *vt) __attribute__((always_inline)) {
+        const int key0 = t * KEYS;
+        f32x16 s[1] = {raw};
         float by = p.c;
         if constexpr (BIAS) {
             by = 1.0f;
@@ -482,39 +515,50 @@ __global__ __launch_bounds__((DP == 256 ? 2 : 4) * WAVE, (FEW_BLOCKS<DP, CACHE, 
     auto byte_of = [&](int t) { return mask_byte(p, b, t * KEYS + lane % 32, len); };
     if (t0 < t1) {
         lds_byte *const kh0 = (lds_byte *)k0 + wave * BYTES, *const vh0 = (lds_byte *)v0 + wave * BYTES;
-        uint32_t live = alive(t0, byte_of(t0));
-        uint8_t byte = byte_of(t0 + 1);
-        fetch(t0, live, kh0, vh0);
         if constexpr (CACHE) {
-            for (int t = t0; t < t1; ++t) {
-                kq.put(lane, kh0);
-                vq.put(lane, vh0);
+            uint8_t byte = byte_of(t0);
+            auto ahead = [&](int t, waiting &w) __attribute__((always_inline)) {
+                const uint32_t live = alive(t, byte);
+                byte = byte_of(min(t + 1, t1 - 1));
+                fetch(t, live, w, kh0, vh0);
+            };
+            // Behind the end the last tile is loaded again: how many loads are on their way is always the same, so that the older ones can be
+            // waited for alone.
+            auto step = [&](int t, waiting &w) __attribute__((always_inline)) {
+                const f32x16 s = score(w, kh0);
+                w.v.put(lane, vh0);
+                const uint32_t live = w.live;
                 asm volatile("" ::: "memory");  // other lanes read what this one wrote
-                uint32_t next = 0;
-                if (t + 1 < t1) {
-                    next = alive(t + 1, byte);
-                    byte = byte_of(t + 2);
-                    fetch(t + 1, next, kh0, vh0);
-                }
-                compute(t, live, kh0, vh0);
+                ahead(min(t + 2, t1 - 1), w);
+                compute(t, live, s, vh0);
                 asm volatile("" ::: "memory");
-                live = next;
+            };
+            ahead(t0, first_tile);
+            ahead(min(t0 + 1, t1 - 1), second_tile);
+            for (int t = t0;;) {
+                step(t, first_tile);
+                if (++t == t1) break;
+                step(t, second_tile);
+                if (++t == t1) break;
             }
         } else {
             lds_byte *const kh1 = (lds_byte *)k1 + wave * BYTES, *const vh1 = (lds_byte *)v1 + wave * BYTES;
+            uint32_t live = alive(t0, byte_of(t0));
+            uint8_t byte = byte_of(t0 + 1);
+            fetch(t0, live, first_tile, kh0, vh0);
             auto step = [&](int t, lds_byte *kh, lds_byte *vh, lds_byte *kn, lds_byte *vn) __attribute__((always_inline)) {
                 uint32_t next = 0;
                 if (t + 1 < t1) {
                     next = alive(t + 1, byte);
                     byte = byte_of(t + 2);
-                    fetch(t + 1, next, kn, vn);
+                    fetch(t + 1, next, first_tile, kn, vn);
                     // copies land in order: all but the next tile's have
                     __builtin_amdgcn_s_waitcnt(wait_copies(2 * tile_copy<DP, KEYS, 1>::MINE));
                 } else {
                     __builtin_amdgcn_s_waitcnt(wait_copies(0));
                 }
                 asm volatile("" ::: "memory");
-                compute(t, live, kh, vh);
+                compute(t, live, score(first_tile, kh), vh);
                 asm volatile("" ::: "memory");
                 live = next;
             };

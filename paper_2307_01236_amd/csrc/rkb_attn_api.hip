@@ -193,7 +193,7 @@ attn_plan plan_fwd(const rkb_attn &a)
     plan.few = rows <= 64;
     if (plan.few) {
         plan.blocks = a.batch * a.kv_heads * ((rows + 31) / 32);
-        plan.splits = split_of(plan.blocks, 512, a.k_rows / 256);
+        plan.splits = split_of(plan.blocks, 512, a.k_rows / 1024);
     } else {
         plan.blocks = a.batch * a.heads * ((a.q_rows + 127) / 128);
         plan.splits = split_of(plan.blocks, 512, a.k_rows / 256);

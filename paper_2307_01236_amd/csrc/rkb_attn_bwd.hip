@@ -11,12 +11,13 @@ namespace rkb {
 namespace {
 
 constexpr int ROWS = 128, WAVES = 4;  // stationary rows and waves of a workgroup
+constexpr int NORM_ROWS = 64;         // rows whose largest norm is kept
 
 struct bwd_in {
     heads_at d_o, o;
     const float *o32, *lse;
     float *delta, *lse2;     // [B, H, stats_rows]: do . o, and -lse in steps of log2 (-inf: a row without keys, or none)
-    uint32_t *norms;         // f16: [B, K, 2]: bits of the largest |do|^2 and |v|^2
+    uint32_t *do_norms, *v_norms;  // f16: bits of the largest |do|^2 and |v|^2 of NORM_ROWS rows: [B, H, stats_rows / NORM_ROWS] and [B, K, ..]
     int64_t stats_rows;
     heads_at dq, dk, dv;
     float *dq_part, *dk_part, *dv_part;  // [splits, rows, D] each, where there are several
@@ -26,13 +27,21 @@ struct bwd_in {
 };
 
 // ds enters the products in T.  In f16 a ds of many keys falls below the range (1/4096 of a gradient of 1e-2 is 2e-6), so it is
-// scaled by a power of two from |ds| <= 2 |do| |v|, whose largest values a pass over both finds.
+// scaled by a power of two from |ds| <= 2 |do| |v|, whose largest values of a key head a pass over both finds.
 template <class T>
 __device__ inline float ds_scale(const bwd_in &g, const attn_in &p, int b, int kv)
 {
     if constexpr (!std::is_same_v<T, f16>) return 1.0f;
-    const uint32_t *n = g.norms + 2 * ((int64_t)b * p.K + kv);
-    const float x = __uint_as_float(n[0]), y = __uint_as_float(n[1]);
+    const int64_t rows = g.stats_rows / NORM_ROWS * p.G, keys = (p.T + NORM_ROWS - 1) / NORM_ROWS, at = (int64_t)b * p.K + kv;
+    uint32_t most[2] = {0, 0};
+    for (int64_t n = threadIdx.x % WAVE; n < rows; n += WAVE) most[0] = max(most[0], g.do_norms[at * rows + n]);
+    for (int64_t n = threadIdx.x % WAVE; n < keys; n += WAVE) most[1] = max(most[1], g.v_norms[at * keys + n]);
+#pragma unroll
+    for (int i = 1; i < WAVE; i *= 2) {
+        most[0] = max(most[0], (uint32_t)__shfl_xor((int)most[0], i));
+        most[1] = max(most[1], (uint32_t)__shfl_xor((int)most[1], i));
+    }
+    const float x = __uint_as_float(most[0]), y = __uint_as_float(most[1]);
     if (!(x > 0.0f && y > 0.0f && finite(x) && finite(y))) return 1.0f;
     const float e = 12.0f - ceilf(0.5f * (__builtin_amdgcn_logf(x) + __builtin_amdgcn_logf(y)));
     return two_to((int)fminf(fmaxf(e, -100.0f), 100.0f));
@@ -41,88 +50,39 @@ __device__ inline float ds_scale(const bwd_in &g, const attn_in &p, int b, int k
 template <class T>
 constexpr float P_LIFT = std::is_same_v<T, f16> ? 14.0f : 0.0f;
 
-// ------------------------------------------------------------------ row sums and norms
+// ------------------------------------------------------------------ norms (f16)
 
-__device__ inline float block_max(float v, float *shared)
-{
-#pragma unroll
-    for (int i = 1; i < WAVE; i *= 2) v = fmaxf(v, __shfl_xor(v, i));
-    if (threadIdx.x % WAVE == 0) shared[threadIdx.x / WAVE] = v;
-    __syncthreads();
-    return fmaxf(fmaxf(shared[0], shared[1]), fmaxf(shared[2], shared[3]));
-}
-
-__global__ __launch_bounds__(256) void k_clear(uint32_t *p, int n)
-{
-    for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) p[i] = 0;
-}
-
-// delta = do . o and lse2 of 64 rows of a head; 16 lanes a row.
+// The largest |do|^2 of NORM_ROWS queries of a head, or |v|^2 of the live ones among as many keys of a key head; 16 lanes a row.
 template <class T>
-__global__ __launch_bounds__(256) void k_attn_delta(attn_in p, bwd_in g)
+__global__ __launch_bounds__(256) void k_attn_norms(attn_in p, bwd_in g)
 {
-    __shared__ float shared[4];
-    const int chunks = (int)(g.stats_rows / 64), bh = blockIdx.x / chunks, i0 = (blockIdx.x - bh * chunks) * 64;
-    const int b = bh / p.H, h = bh - b * p.H, lane = threadIdx.x % 16;
-    float most = 0.0f;
-    for (int k = 0; k < 4; ++k) {
-        const int i = i0 + k * 16 + threadIdx.x / 16;
-        float sum = 0.0f, norm = 0.0f;
-        if (i < p.Q) {
-            const T *d = g.d_o.at<T>(b, i, h), *o = g.o32 ? nullptr : g.o.at<T>(b, i, h);
-            const float *o32 = g.o32 ? g.o32 + (((int64_t)b * p.Q + i) * p.H + h) * p.D : nullptr;
-            for (int c = lane * 8; c < p.D; c += 128) {
-                float dv[8], ov[8];
-                load8<T>(d + c, p.D - c, dv);
-                if (o32)
-                    load8<float>(o32 + c, p.D - c, ov);
-                else
-                    load8<T>(o + c, p.D - c, ov);
+    __shared__ uint32_t shared[4];
+    const int q_chunks = (int)(g.stats_rows / NORM_ROWS), k_chunks = (p.T + NORM_ROWS - 1) / NORM_ROWS, of_q = p.B * p.H * q_chunks;
+    const bool keys = (int)blockIdx.x >= of_q;
+    const int n = (int)blockIdx.x - (keys ? of_q : 0), chunks = keys ? k_chunks : q_chunks, heads = keys ? p.K : p.H;
+    const int bh = n / chunks, r0 = (n - bh * chunks) * NORM_ROWS, b = bh / heads, h = bh - b * heads, lane = threadIdx.x % 16;
+    const int rows = keys ? len_of(p, b) : p.Q;
+    uint32_t most = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    sum = __builtin_fmaf(dv[e], ov[e], sum);
-                    norm = __builtin_fmaf(dv[e], dv[e], norm);
-                }
-            }
-        }
-        sum = lane_sum<16>(sum);
-        most = fmaxf(most, lane_sum<16>(norm));
-        if (lane == 0) {
-            const int64_t at = (int64_t)bh * g.stats_rows + i;
-            const float l = i < p.Q ? g.lse[(int64_t)bh * p.Q + i] : NEG_INF;
-            g.delta[at] = l == NEG_INF ? 0.0f : sum;
-            g.lse2[at] = l == NEG_INF ? NEG_INF : -l * LOG2E;
-        }
-    }
-    if constexpr (std::is_same_v<T, f16>) {
-        most = block_max(most, shared);
-        if (threadIdx.x == 0) atomicMax(g.norms + 2 * ((int64_t)b * p.K + h / p.G), __float_as_uint(most));
-    }
-}
-
-// The largest |v|^2 of the live ones among 256 keys of a head.
-template <class T>
-__global__ __launch_bounds__(256) void k_attn_vnorm(attn_in p, bwd_in g)
-{
-    __shared__ float shared[4];
-    const int chunks = (p.T + 255) / 256, bk = blockIdx.x / chunks, t0 = (blockIdx.x - bk * chunks) * 256;
-    const int b = bk / p.K, kv = bk - b * p.K, lane = threadIdx.x % 16, len = len_of(p, b);
-    float most = 0.0f;
-    for (int t = t0 + threadIdx.x / 16; t < min(t0 + 256, len); t += 16) {
+    for (int k = 0; k < NORM_ROWS / 16; ++k) {
+        const int r = r0 + k * 16 + threadIdx.x / 16;
         float norm = 0.0f;
-        if (mask_byte(p, b, t, len)) {
-            const T *v = p.v.at<T>(b, t, kv);
+        if (r < rows && (!keys || mask_byte(p, b, r, rows))) {
+            const T *row = keys ? p.v.at<T>(b, r, h) : g.d_o.at<T>(b, r, h);
             for (int c = lane * 8; c < p.D; c += 128) {
                 float x[8];
-                load8<T>(v + c, p.D - c, x);
+                load8<T>(row + c, p.D - c, x);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) norm = __builtin_fmaf(x[e], x[e], norm);
             }
         }
-        most = fmaxf(most, lane_sum<16>(norm));
+        most = max(most, __float_as_uint(lane_sum<16>(norm)) & 0x7fffffffu);
     }
-    most = block_max(most, shared);
-    if (threadIdx.x == 0) atomicMax(g.norms + 2 * (int64_t)bk + 1, __float_as_uint(most));
+#pragma unroll
+    for (int i = 1; i < WAVE; i *= 2) most = max(most, (uint32_t)__shfl_xor((int)most, i));
+    if (threadIdx.x % WAVE == 0) shared[threadIdx.x / WAVE] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) (keys ? g.v_norms : g.do_norms)[n] = max(max(shared[0], shared[1]), max(shared[2], shared[3]));
 }
 
 // ------------------------------------------------------------------ what a lane stores of a row
@@ -162,7 +122,7 @@ __device__ inline void store_grad(T *to, float *part, bool wide, int width, cons
 
 // ------------------------------------------------------------------ dq
 //
-// delta comes from an o that was summed from rounded probabilities (and may be rounded itself), so ds of a row adds up to some r
+// A row's delta = do . o and -lse are formed here, where its do is in registers, and left for dk and dv.  delta comes from an o that was summed from rounded probabilities (and may be rounded itself), so ds of a row adds up to some r
 // instead of 0.  Then delta + r is what delta should have been, to 32 bits: it is left for dk, dv and the bias's gradient, which
 // are formed from it afterwards; dq keeps an error of r (p k), about as large as the rounding of ds.
 template <class T, int DP>
@@ -190,8 +150,32 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
     frag<T> q[C], d[C];
     load_stationary<T, DP>(q, p.q.at<T>(b, min(i, p.Q - 1), h), lane, p.D, there);
     load_stationary<T, DP>(d, g.d_o.at<T>(b, min(i, p.Q - 1), h), lane, p.D, there);
-    const int64_t stat = (int64_t)bh * g.stats_rows + min(i, (int)g.stats_rows - 1);
-    const float lse = there ? g.lse2[stat] : NEG_INF, delta = there ? g.delta[stat] : 0.0f;
+    const bool counted = i < g.stats_rows;  // rows past the last query are left as rows without keys, for tiles that reach there
+    const int64_t stat = (int64_t)bh * g.stats_rows + i;
+    float lse = NEG_INF, delta = 0.0f;
+    if (there) {
+        const float l = g.lse[(int64_t)bh * p.Q + i];
+        const T *o = g.o32 ? nullptr : g.o.at<T>(b, i, h);
+        const float *o32 = g.o32 ? g.o32 + (((int64_t)b * p.Q + i) * p.H + h) * p.D : nullptr;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            const int col = c * 16 + lane / 32 * 8;
+            float v[8];
+            if (o32)
+                load8<float>(o32 + col, p.D - col, v);
+            else
+                load8<T>(o + col, p.D - col, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) delta = __builtin_fmaf((float)d[c][e], v[e], delta);
+        }
+        lse = l == NEG_INF ? NEG_INF : -l * LOG2E;
+    }
+    delta = half_sum(delta);
+    if (lse == NEG_INF) delta = 0.0f;
+    if (counted && lane < 32 && split == 0) {
+        g.lse2[stat] = lse;
+        if (g.row_part) g.delta[stat] = delta;
+    }
     const float lift = ds_scale<T>(g, p, b, kv);
     const int far = p.bias.far;
     if (p.bias.table) fill_bias<T>(by_distance, p, h, threadIdx.x, 256);
@@ -269,11 +253,11 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
                          acc, p.scale / lift, lse == NEG_INF, lane);
     }
     const float r = half_sum(row_sum[0] + row_sum[1]);
-    if (there && lane < 32) {
+    if (counted && lane < 32) {
         if (g.row_part)
-            g.row_part[(int64_t)split * p.B * p.H * g.stats_rows + stat] = r;
+            g.row_part[(int64_t)split * p.B * p.H * g.stats_rows + stat] = there ? r : 0.0f;
         else
-            g.delta[stat] = delta + r;
+            g.delta[stat] = there ? delta + r : 0.0f;
     }
 }
 
@@ -284,7 +268,7 @@ __global__ __launch_bounds__(256) void k_attn_delta_join(attn_in p, bwd_in g, in
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < rows; at += (int64_t)gridDim.x * 256) {
         float r = 0.0f;
         for (int s = 0; s < splits; ++s) r += g.row_part[s * rows + at];
-        if (at % g.stats_rows < p.Q) g.delta[at] += r;
+        g.delta[at] += r;
     }
 }
 
@@ -689,18 +673,19 @@ bool takes_8_bytes(const rkb_heads &h, int64_t dim)
 }
 
 struct bwd_memory {
-    size_t stats, norms, dq, rows, dkv, table;
+    size_t stats, norms[2], dq, rows, dkv, table;
     bwd_memory(const attn_bwd_plan &plan, const rkb_attn &a)
     {
         auto up = [](size_t n) { return (size_t)round_up((int64_t)n, 256); };
         stats = up((size_t)a.batch * a.heads * plan.stats_rows * 4);
-        norms = a.dtype == RKB_F16 ? up((size_t)a.batch * a.kv_heads * 8) : 0;
+        norms[0] = a.dtype == RKB_F16 ? up((size_t)a.batch * a.heads * (plan.stats_rows / NORM_ROWS) * 4) : 0;
+        norms[1] = a.dtype == RKB_F16 ? up((size_t)a.batch * a.kv_heads * ((a.k_rows + NORM_ROWS - 1) / NORM_ROWS) * 4) : 0;
         dq = plan.q_splits > 1 ? up((size_t)plan.q_splits * a.batch * a.q_rows * a.heads * a.dim * 4) : 0;
         dkv = plan.k_splits > 1 ? up((size_t)plan.k_splits * a.batch * a.k_rows * a.kv_heads * a.dim * 4) : 0;
         rows = plan.q_splits > 1 ? plan.q_splits * stats : 0;
         table = a.table ? up((size_t)plan.k_blocks * plan.k_splits * (a.heads / a.kv_heads) * a.buckets * 4) : 0;
     }
-    size_t all() const { return 2 * stats + norms + dq + rows + 2 * dkv + table; }
+    size_t all() const { return 2 * stats + norms[0] + norms[1] + dq + rows + 2 * dkv + table; }
 };
 
 }  // namespace
@@ -719,7 +704,8 @@ int run_attn_bwd(const attn_in &p, const rkb_attn &a, const attn_bwd_plan &plan,
     };
     g.delta = (float *)take(mem.stats);
     g.lse2 = (float *)take(mem.stats);
-    g.norms = (uint32_t *)take(mem.norms);
+    g.do_norms = (uint32_t *)take(mem.norms[0]);
+    g.v_norms = (uint32_t *)take(mem.norms[1]);
     g.dq = at_of(gr.dq);
     g.dk = at_of(gr.dk);
     g.dv = at_of(gr.dv);
@@ -733,10 +719,8 @@ int run_attn_bwd(const attn_in &p, const rkb_attn &a, const attn_bwd_plan &plan,
         using T = std::remove_pointer_t<decltype(tp)>;
         int rc = RKB_OK;
         const int64_t rows = a.batch * a.heads, keys = a.batch * a.kv_heads;
-        if (g.norms && keys > 0) rc = launch(k_clear, dim3(1), dim3(256), st, g.norms, (int)(2 * keys));
-        if (rc == RKB_OK && rows * a.q_rows > 0) rc = launch(k_attn_delta<T>, dim3((uint32_t)(rows * (plan.stats_rows / 64))), dim3(256), st, p, g);
-        if (rc == RKB_OK && g.norms && keys * a.k_rows > 0)
-            rc = launch(k_attn_vnorm<T>, dim3((uint32_t)(keys * ((a.k_rows + 255) / 256))), dim3(256), st, p, g);
+        const int64_t chunks = rows * (plan.stats_rows / NORM_ROWS) + keys * ((a.k_rows + NORM_ROWS - 1) / NORM_ROWS);
+        if (std::is_same_v<T, f16> && chunks > 0) rc = launch(k_attn_norms<T>, dim3((uint32_t)chunks), dim3(256), st, p, g);
         if (rc != RKB_OK) return rc;
         return with_width(a.dim, [&](auto dp) {
             constexpr int DP = dp();
