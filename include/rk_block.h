@@ -172,7 +172,8 @@ typedef struct rkb_heads {
  * nb is 2 .. RKB_MAX_BUCKETS (and so is twice nb, where two-sided), e < max_distance <= RKB_MAX_DISTANCE.  An entry of -1e30 or less, -inf
  * among them, hides its keys as a mask does, and its gradient is 0.
  *
- * dtype: RKB_F16 or RKB_BF16; 1 <= dim <= RKB_MAX_DIM; heads a multiple of kv_heads; 0 < scale < inf.
+ * dtype: RKB_F16 or RKB_BF16; 1 <= dim <= RKB_MAX_DIM; heads a multiple of kv_heads; 0 < scale < inf; batch * heads times
+ * q_rows (rounded up to 128) at most 2^28, and for the backward pass batch * kv_heads times k_rows likewise.
  */
 typedef struct rkb_attn {
     int dtype, causal;
@@ -234,9 +235,11 @@ int rkb_attn_fwd(const rkb_attn *a, const rkb_heads *q, const rkb_heads *k, cons
  *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i,
  *   dtable[c, h] = sum of ds_ij over the i, j of bucket c and all sequences,
  * dk and dv summed over the heads that share them too.  p and ds enter the products rounded to dtype; in f16, scaled
- * so that neither overflows nor loses bits that its size would not lose in any type.  Taking o rounded instead of in 32 bits costs about
- * one more rounding of dtype in do_i . o_i, which is seen in a 32-bit dtable only.
- * dq, dk, dv of dtype, each may have p NULL (dk and dv both); dtable of table_dtype, NULL for none.
+ * so that neither overflows nor loses bits that its size would not lose in any type.  do_i . o_i takes over the error of o (its rounding, where o is
+ * not given in 32 bits, and that of the probabilities it was summed from); what a row's ds add up to tells that error, which
+ * is taken out of dk and dtable and stays in dq, about as large there as the rounding of ds.
+ * dq, dk, dv of dtype, each may have p NULL (dk and dv both); dtable of table_dtype, NULL for none.  What q and do hold at
+ * a query without live keys is not looked at, whatever it is; its dq is 0.
  * aligned: as above, of do too.
  */
 int rkb_attn_bwd_workspace(const rkb_attn *a, int again, int aligned, size_t *bytes);

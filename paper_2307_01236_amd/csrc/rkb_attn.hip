@@ -631,36 +631,60 @@ __global__ __launch_bounds__((DP == 256 ? 2 : 4) * WAVE, (FEW_BLOCKS<DP, CACHE, 
 template <class T>
 __global__ __launch_bounds__(256) void k_attn_join(attn_in p, attn_out out, int splits)
 {
-    const int quads = (p.D + 3) / 4;
-    const int64_t rows = (int64_t)p.B * p.H * p.Q, at = (int64_t)blockIdx.x * 256 + threadIdx.x, row = at / quads;
+    // a split call has at most 512 x 64 rows or 256 x 128: all of this fits 32 bits
+    const uint32_t quads = (p.D + 3) / 4, rows = (uint32_t)p.B * p.H * p.Q, at = blockIdx.x * 256 + threadIdx.x, row = at / quads;
     const int col = (int)(at - row * quads) * 4;
     if (row >= rows) return;
+    using f32x2 = vec<float, 2>;
+    const f32x2 *const ml = (const f32x2 *)out.part_ml + row;
+    const float *const from = out.part + (int64_t)row * p.D + col;
+    const int64_t size = (int64_t)rows * p.D;
     float top = NEG_INF;
+#pragma unroll 4
     for (int s = 0; s < splits; ++s) {
-        const float *ml = out.part_ml + 2 * (s * rows + row);
-        if (ml[1] != 0.0f) top = fmaxf(top, ml[0]);
+        const f32x2 x = ml[(int64_t)s * rows];
+        top = x[1] != 0.0f ? fmaxf(top, x[0]) : top;
     }
     const float base = top == NEG_INF ? 0.0f : top;
-    float l = 0.0f, v[4] = {};
+    float l = 0.0f;
+    f32x4 v = {};
+    const bool whole = p.D % 4 == 0;
+#pragma unroll 4
     for (int s = 0; s < splits; ++s) {
-        const float *ml = out.part_ml + 2 * (s * rows + row), *from = out.part + (s * rows + row) * p.D + col;
-        if (ml[1] == 0.0f) continue;
-        const float f = __builtin_amdgcn_exp2f(ml[0] - base);
-        l += ml[1] * f;
+        const f32x2 x = ml[(int64_t)s * rows];
+        f32x4 part = {};
+        if (whole) {
+            part = *(const f32x4 *)(from + s * size);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (col + e < p.D) v[e] = __builtin_fmaf(from[e], f, v[e]);
+            for (int e = 0; e < 4; ++e)
+                if (col + e < p.D) part[e] = from[s * size + e];
+        }
+        const bool any = x[1] != 0.0f;
+        const float f = any ? __builtin_amdgcn_exp2f(x[0] - base) : 0.0f;
+        l += x[1] * f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = any ? __builtin_fmaf(part[e], f, v[e]) : v[e];
     }
     const float times = l == 0.0f ? 0.0f : 1.0f / l;
-    const int i = (int)(row % p.Q), h = (int)(row / p.Q % p.H), b = (int)(row / p.Q / p.H);
+    const uint32_t bh = row / p.Q, i = row - bh * p.Q, b = bh / p.H, h = bh - b * p.H;
     T *to = out.o.p ? out.o.at<T>(b, i, h) : nullptr;
     float *to32 = out.o32 ? out.o32 + (((int64_t)b * p.Q + i) * p.H + h) * p.D : nullptr;
+    v *= times;
+    if (out.wide) {
+        vec<T, 4> x;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (col + e < p.D) {
-            if (to) to[col + e] = (T)settled<T>(v[e] * times);
-            if (to32) to32[col + e] = v[e] * times;
-        }
+        for (int e = 0; e < 4; ++e) x[e] = (T)settled<T>(v[e]);
+        if (to) *(vec<T, 4> *)(to + col) = x;
+        if (to32) *(f32x4 *)(to32 + col) = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + e < p.D) {
+                if (to) to[col + e] = (T)settled<T>(v[e]);
+                if (to32) to32[col + e] = v[e];
+            }
+    }
     if (out.lse && col == 0) out.lse[row] = l == 0.0f ? NEG_INF : (base + __builtin_amdgcn_logf(l)) * LN2;
 }
 

@@ -9,7 +9,7 @@
 namespace rkb {
 namespace {
 
-constexpr int64_t MOST_BLOCKS = (int64_t)1 << 22;  // workgroups of a launch
+constexpr int64_t MOST_BLOCKS = (int64_t)1 << 21;  // workgroups of a launch
 constexpr size_t WS_ALIGN_ATTN = 256;
 
 // ------------------------------------------------------------------ checks
@@ -169,12 +169,15 @@ size_t again_bytes(const rkb_attn &a, const attn_plan &plan)
            attn_fwd_parts_bytes(plan, a);
 }
 
-bool fits_launches(const rkb_attn &a)
+// So that no launch has 2^32 lanes, which take at least 128 rows of a head for a workgroup of 256, but two such workgroups of heads of more than 128
+// columns, and one for 64 rows of queries and keys in the norms' kernel.
+bool fits_launches(const rkb_attn &a, bool backward)
 {
-    // 64 bits hold all of these: rows are at most 2^28 each way, batch 2^28, heads 2^16, so divide before multiplying
-    const int64_t q = (a.q_rows + 31) / 32, k = (a.k_rows + 31) / 32;
-    return a.batch == 0 || ((q == 0 || a.batch <= MOST_BLOCKS / q) && (k == 0 || a.batch <= MOST_BLOCKS / k) &&
-                            a.batch * std::max(q, k) * a.heads <= MOST_BLOCKS * 8 && a.batch * a.heads <= MOST_BLOCKS);
+    auto good = [&](int64_t heads, int64_t rows) {
+        const int64_t units = a.batch * heads;
+        return units <= MOST_BLOCKS && units * ((rows + 127) / 128) <= MOST_BLOCKS;
+    };
+    return good(a.heads, a.q_rows) && (!backward || good(a.kv_heads, a.k_rows));
 }
 
 }  // namespace
@@ -193,7 +196,7 @@ attn_plan plan_fwd(const rkb_attn &a)
     plan.few = rows <= 64;
     if (plan.few) {
         plan.blocks = a.batch * a.kv_heads * ((rows + 31) / 32);
-        plan.splits = split_of(plan.blocks, 512, a.k_rows / 1024);
+        plan.splits = split_of(plan.blocks, 512, a.k_rows / 256);
     } else {
         plan.blocks = a.batch * a.heads * ((a.q_rows + 127) / 128);
         plan.splits = split_of(plan.blocks, 512, a.k_rows / 256);
@@ -219,7 +222,7 @@ using namespace rkb;
 
 extern "C" int rkb_attn_fwd_workspace(const rkb_attn *a, int cache, int aligned, size_t *bytes)
 {
-    if (!bytes || !good_attn(a) || !fits_launches(*a)) return RKB_E_INVAL;
+    if (!bytes || !good_attn(a) || !fits_launches(*a, false)) return RKB_E_INVAL;
     *bytes = attn_fwd_parts_bytes(plan_fwd(*a), *a);
     if (!aligned || a->dim % 8)
         *bytes += copy_bytes(a->batch, a->q_rows, a->heads, a->dim) + (cache ? 0 : 2 * copy_bytes(a->batch, a->k_rows, a->kv_heads, a->dim));
@@ -229,7 +232,7 @@ extern "C" int rkb_attn_fwd_workspace(const rkb_attn *a, int cache, int aligned,
 extern "C" int rkb_attn_fwd(const rkb_attn *a, const rkb_heads *q, const rkb_heads *k, const rkb_heads *v, const rkb_kv8 *cache,
                             const rkb_heads *o, float *o32, float *lse, void *workspace, size_t ws_bytes, void *stream)
 {
-    if (!good_attn(a) || !fits_launches(*a) || (cache ? k || v : !k || !v) || !q || !o) return RKB_E_INVAL;
+    if (!good_attn(a) || !fits_launches(*a, false) || (cache ? k || v : !k || !v) || !q || !o) return RKB_E_INVAL;
     const int64_t B = a->batch, Q = a->q_rows, T = a->k_rows, H = a->heads, K = a->kv_heads, D = a->dim;
     rkb_heads qs = settled_heads(q, B, Q, H), ks = settled_heads(k, B, T, K), vs = settled_heads(v, B, T, K), os = settled_heads(o, B, Q, H);
     if (!good_heads_in(qs, B * Q, 2) || !good_heads_out(os, B, Q, H, D, 2) || (uintptr_t)o32 % 16 || (uintptr_t)lse % 4) return RKB_E_INVAL;
@@ -265,7 +268,7 @@ extern "C" int rkb_attn_fwd(const rkb_attn *a, const rkb_heads *q, const rkb_hea
 
 extern "C" int rkb_attn_bwd_workspace(const rkb_attn *a, int again, int aligned, size_t *bytes)
 {
-    if (!bytes || !good_attn(a) || !fits_launches(*a)) return RKB_E_INVAL;
+    if (!bytes || !good_attn(a) || !fits_launches(*a, true)) return RKB_E_INVAL;
     *bytes = attn_bwd_bytes(plan_bwd(*a), *a) + (again ? again_bytes(*a, plan_fwd(*a)) : 0);
     if (!aligned || a->dim % 8) *bytes += 2 * copy_bytes(a->batch, a->q_rows, a->heads, a->dim) + 2 * copy_bytes(a->batch, a->k_rows, a->kv_heads, a->dim);
     return RKB_OK;
@@ -275,7 +278,7 @@ extern "C" int rkb_attn_bwd(const rkb_attn *a, const rkb_heads *d_o, const rkb_h
                             const rkb_heads *o, const float *o32, const float *lse, const rkb_heads *dq, const rkb_heads *dk,
                             const rkb_heads *dv, void *dtable, void *workspace, size_t ws_bytes, void *stream)
 {
-    if (!good_attn(a) || !fits_launches(*a) || !d_o || !q || !k || !v || !dq || !dk || !dv) return RKB_E_INVAL;
+    if (!good_attn(a) || !fits_launches(*a, true) || !d_o || !q || !k || !v || !dq || !dk || !dv) return RKB_E_INVAL;
     const int64_t B = a->batch, Q = a->q_rows, T = a->k_rows, H = a->heads, K = a->kv_heads, D = a->dim;
     rkb_heads ds = settled_heads(d_o, B, Q, H), qs = settled_heads(q, B, Q, H), ks = settled_heads(k, B, T, K), vs = settled_heads(v, B, T, K);
     rkb_heads os = settled_heads(o, B, Q, H), dqs = settled_heads(dq, B, Q, H), dks = settled_heads(dk, B, T, K), dvs = settled_heads(dv, B, T, K);

@@ -18,6 +18,7 @@ struct bwd_in {
     const float *o32, *lse;
     float *delta, *lse2;     // [B, H, stats_rows]: do . o, and -lse in steps of log2 (-inf: a row without keys, or none)
     uint32_t *do_norms, *v_norms;  // f16: bits of the largest |do|^2 and |v|^2 of NORM_ROWS rows: [B, H, stats_rows / NORM_ROWS] and [B, K, ..]
+    uint32_t *seen;          // [B, H, stats_rows / 32]: bit r: row r has keys
     int64_t stats_rows;
     heads_at dq, dk, dv;
     float *dq_part, *dk_part, *dv_part;  // [splits, rows, D] each, where there are several
@@ -52,7 +53,7 @@ constexpr float P_LIFT = std::is_same_v<T, f16> ? 14.0f : 0.0f;
 
 // ------------------------------------------------------------------ norms (f16)
 
-// The largest |do|^2 of NORM_ROWS queries of a head, or |v|^2 of the live ones among as many keys of a key head; 16 lanes a row.
+// The largest |do|^2 of those of NORM_ROWS queries of a head that have keys, or |v|^2 of the live ones among as many keys of a key head; 16 lanes a row.
 template <class T>
 __global__ __launch_bounds__(256) void k_attn_norms(attn_in p, bwd_in g)
 {
@@ -67,7 +68,7 @@ __global__ __launch_bounds__(256) void k_attn_norms(attn_in p, bwd_in g)
     for (int k = 0; k < NORM_ROWS / 16; ++k) {
         const int r = r0 + k * 16 + threadIdx.x / 16;
         float norm = 0.0f;
-        if (r < rows && (!keys || mask_byte(p, b, r, rows))) {
+        if (r < rows && (keys ? mask_byte(p, b, r, rows) != 0 : g.lse[(int64_t)bh * p.Q + r] != NEG_INF)) {
             const T *row = keys ? p.v.at<T>(b, r, h) : g.d_o.at<T>(b, r, h);
             for (int c = lane * 8; c < p.D; c += 128) {
                 float x[8];
@@ -122,7 +123,8 @@ __device__ inline void store_grad(T *to, float *part, bool wide, int width, cons
 
 // ------------------------------------------------------------------ dq
 //
-// A row's delta = do . o and -lse are formed here, where its do is in registers, and left for dk and dv.  delta comes from an o that was summed from rounded probabilities (and may be rounded itself), so ds of a row adds up to some r
+// A row's delta = do . o and -lse are formed here, where its do is in registers, and left for dk and dv.  delta comes from an o that
+// was summed from rounded probabilities (and may be rounded itself), so ds of a row adds up to some r
 // instead of 0.  Then delta + r is what delta should have been, to 32 bits: it is left for dk, dv and the bias's gradient, which
 // are formed from it afterwards; dq keeps an error of r (p k), about as large as the rounding of ds.
 template <class T, int DP>
@@ -173,6 +175,8 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
     delta = half_sum(delta);
     if (lse == NEG_INF) delta = 0.0f;
     if (counted && lane < 32 && split == 0) {
+        const uint32_t seen = (uint32_t)__ballot(lse != NEG_INF);
+        if (lane == 0) g.seen[stat / 32] = seen;
         g.lse2[stat] = lse;
         if (g.row_part) g.delta[stat] = delta;
     }
@@ -255,9 +259,9 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
     const float r = half_sum(row_sum[0] + row_sum[1]);
     if (counted && lane < 32) {
         if (g.row_part)
-            g.row_part[(int64_t)split * p.B * p.H * g.stats_rows + stat] = there ? r : 0.0f;
+            g.row_part[(int64_t)split * p.B * p.H * g.stats_rows + stat] = lse == NEG_INF ? 0.0f : r;
         else
-            g.delta[stat] = there ? delta + r : 0.0f;
+            g.delta[stat] = lse == NEG_INF ? 0.0f : delta + r;
     }
 }
 
@@ -354,10 +358,24 @@ __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dk
         copy_d = (const char *)g.d_o.at<T>(b, (int64_t)t * TILE, h);
         copy_s = (lane < 32 ? g.lse2 : g.delta) + ((int64_t)b * p.H + h) * g.stats_rows + t * TILE + lane % 32;  // rows are padded
     };
+    // Queries without keys become zeros: 0 times whatever lies there would not be 0.  Only order, masks and bias leave such queries; whether any
+    // did is looked up once.
+    bool gaps = false;
+    if (of_head && (p.causal || p.mask || FAR > 0)) {
+        const uint32_t *const seen = g.seen + ((int64_t)b * p.H + kv * p.G) * (g.stats_rows / TILE);
+        const int words = (int)(g.stats_rows / TILE), last = p.Q % TILE;
+        const uint32_t of_last = last ? (1u << last) - 1 : ~0u;
+        for (int64_t n = threadIdx.x % WAVE; n < (int64_t)words * p.G; n += WAVE) {
+            const int at = (int)(n % words);
+            gaps |= seen[n] != (at < q_tiles - 1 ? ~0u : at == q_tiles - 1 ? of_last : 0u);
+        }
+        gaps = __any(gaps);
+    }
     auto fetch = [&](char *qto, char *dto, float *sto) __attribute__((always_inline)) {
         const int n = p.Q - copy_t * TILE;
-        const uint64_t live = n >= TILE ? 0xffffffffu : ((uint64_t)1 << n) - 1;
-        const bool whole = n >= TILE && p.D == DP;
+        uint64_t live = n >= TILE ? 0xffffffffu : ((uint64_t)1 << n) - 1;
+        if (gaps) live = g.seen[((int64_t)b * p.H + copy_h) * (g.stats_rows / TILE) + copy_t];
+        const bool whole = (uint32_t)live == ~0u && p.D == DP;
         qc.copy(wave, lane, copy_q, live, whole, (lds_byte *)qto);
         dc.copy(wave, lane, copy_d, live, whole, (lds_byte *)dto);
         __builtin_amdgcn_global_load_lds((global_void *)copy_s, (lds_void *)(lds_byte *)(sto + wave * 64), 4, 0, 0);
@@ -653,17 +671,35 @@ struct grad_join {
     int n, heads;
 };
 
-// A lane has one element; splits are added in order.
+// A lane has 4 columns of a row (with `wide` as one piece); splits are added in order.
 template <class T>
-__global__ __launch_bounds__(256) void k_attn_grads(grad_join j0, grad_join j1, int D, int splits)
+__global__ __launch_bounds__(256) void k_attn_grads(grad_join j0, grad_join j1, int D, int splits, int wide)
 {
     const grad_join &j = blockIdx.y ? j1 : j0;
-    const int64_t size = j.rows * D;
-    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < size; at += (int64_t)gridDim.x * 256) {
-        float sum = 0.0f;
-        for (int s = 0; s < splits; ++s) sum += j.part[s * size + at];
-        const int64_t row = at / D, t = row / j.heads;
-        j.to.at<T>(t / j.n, t % j.n, row % j.heads)[at - row * D] = (T)settled<T>(sum);
+    const uint32_t quads = (D + 3) / 4;
+    const int64_t size = j.rows * D, all = j.rows * quads;
+    const bool small = all >> 31 == 0;  // 64-bit division is slow
+    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
+        const int64_t row = small ? (uint32_t)at / quads : at / quads, t = small ? (uint32_t)row / (uint32_t)j.heads : row / j.heads;
+        const int64_t b = small ? (uint32_t)t / (uint32_t)j.n : t / j.n;
+        const int col = (int)(at - row * quads) * 4;
+        const float *const from = j.part + row * D + col;
+        T *const to = j.to.at<T>(b, t - b * j.n, row - t * j.heads) + col;
+        if (wide) {
+            f32x4 sum = {};
+#pragma unroll 4
+            for (int s = 0; s < splits; ++s) sum += *(const f32x4 *)(from + s * size);
+            vec<T, 4> v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = (T)settled<T>(sum[e]);
+            *(vec<T, 4> *)to = v;
+        } else {
+            for (int e = 0; e < 4 && col + e < D; ++e) {
+                float sum = 0.0f;
+                for (int s = 0; s < splits; ++s) sum += from[s * size + e];
+                to[e] = (T)settled<T>(sum);
+            }
+        }
     }
 }
 
@@ -673,11 +709,12 @@ bool takes_8_bytes(const rkb_heads &h, int64_t dim)
 }
 
 struct bwd_memory {
-    size_t stats, norms[2], dq, rows, dkv, table;
+    size_t stats, seen, norms[2], dq, rows, dkv, table;
     bwd_memory(const attn_bwd_plan &plan, const rkb_attn &a)
     {
         auto up = [](size_t n) { return (size_t)round_up((int64_t)n, 256); };
         stats = up((size_t)a.batch * a.heads * plan.stats_rows * 4);
+        seen = up(stats / 32);
         norms[0] = a.dtype == RKB_F16 ? up((size_t)a.batch * a.heads * (plan.stats_rows / NORM_ROWS) * 4) : 0;
         norms[1] = a.dtype == RKB_F16 ? up((size_t)a.batch * a.kv_heads * ((a.k_rows + NORM_ROWS - 1) / NORM_ROWS) * 4) : 0;
         dq = plan.q_splits > 1 ? up((size_t)plan.q_splits * a.batch * a.q_rows * a.heads * a.dim * 4) : 0;
@@ -685,7 +722,7 @@ struct bwd_memory {
         rows = plan.q_splits > 1 ? plan.q_splits * stats : 0;
         table = a.table ? up((size_t)plan.k_blocks * plan.k_splits * (a.heads / a.kv_heads) * a.buckets * 4) : 0;
     }
-    size_t all() const { return 2 * stats + norms[0] + norms[1] + dq + rows + 2 * dkv + table; }
+    size_t all() const { return 2 * stats + seen + norms[0] + norms[1] + dq + rows + 2 * dkv + table; }
 };
 
 }  // namespace
@@ -704,6 +741,7 @@ int run_attn_bwd(const attn_in &p, const rkb_attn &a, const attn_bwd_plan &plan,
     };
     g.delta = (float *)take(mem.stats);
     g.lse2 = (float *)take(mem.stats);
+    g.seen = (uint32_t *)take(mem.seen);
     g.do_norms = (uint32_t *)take(mem.norms[0]);
     g.v_norms = (uint32_t *)take(mem.norms[1]);
     g.dq = at_of(gr.dq);
@@ -726,9 +764,9 @@ int run_attn_bwd(const attn_in &p, const rkb_attn &a, const attn_bwd_plan &plan,
             constexpr int DP = dp();
             const dim3 q_grid((uint32_t)(plan.q_blocks * plan.q_splits)), k_grid((uint32_t)(plan.k_blocks * plan.k_splits * (DP == 256 ? 2 : 1)));
             int rc = RKB_OK;
-            auto join = [&](const grad_join &x, const grad_join &y, int splits, int jobs) {
-                const int64_t blocks = std::min<int64_t>((x.rows * a.dim + 255) / 256, 1 << 16);
-                return launch(k_attn_grads<T>, dim3((uint32_t)blocks, jobs), dim3(256), st, x, y, (int)a.dim, splits);
+            auto join = [&](const grad_join &x, const grad_join &y, int splits, int jobs, int wide) {
+                const int64_t blocks = std::min<int64_t>((x.rows * ((a.dim + 3) / 4) + 255) / 256, 1 << 16);
+                return launch(k_attn_grads<T>, dim3((uint32_t)blocks, jobs), dim3(256), st, x, y, (int)a.dim, splits, wide);
             };
             if (plan.q_blocks) rc = launch(k_attn_dq<T, DP>, q_grid, dim3(256), st, p, g, plan.q_splits);
             if (rc == RKB_OK && g.row_part && plan.q_blocks)
@@ -736,7 +774,7 @@ int run_attn_bwd(const attn_in &p, const rkb_attn &a, const attn_bwd_plan &plan,
                             plan.q_splits);
             if (rc == RKB_OK && plan.q_splits > 1 && gr.dq.p) {
                 const grad_join j{g.dq_part, g.dq, a.batch * a.q_rows * a.heads, (int)a.q_rows, (int)a.heads};
-                rc = join(j, j, plan.q_splits, 1);
+                rc = join(j, j, plan.q_splits, 1, g.wide & 1);
             }
             if (rc == RKB_OK && plan.k_blocks && (gr.dk.p || gr.dtable)) {
                 if (!p.bias.table)
@@ -751,7 +789,7 @@ int run_attn_bwd(const attn_in &p, const rkb_attn &a, const attn_bwd_plan &plan,
                             a.batch * ((a.k_rows + ROWS - 1) / ROWS) * plan.k_splits, gr.dtable);
             if (rc == RKB_OK && plan.k_splits > 1 && gr.dk.p) {
                 const int64_t n = a.batch * a.k_rows * a.kv_heads;
-                rc = join({g.dk_part, g.dk, n, (int)a.k_rows, (int)a.kv_heads}, {g.dv_part, g.dv, n, (int)a.k_rows, (int)a.kv_heads}, plan.k_splits, 2);
+                rc = join({g.dk_part, g.dk, n, (int)a.k_rows, (int)a.kv_heads}, {g.dv_part, g.dv, n, (int)a.k_rows, (int)a.kv_heads}, plan.k_splits, 2, g.wide >> 1);
             }
             return rc;
         });

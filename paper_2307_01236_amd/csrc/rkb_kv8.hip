@@ -116,18 +116,20 @@ struct kv_load {
     int B, K, D, ld, chunks;
 };
 
-// A lane has 8 columns of a token; neighbouring lanes go on in the columns and then the tokens of a head.
+// A lane has 8 columns of a token.  Neighbouring lanes go on in the columns, then the heads and then the tokens, as k and v lie in most programs:
+// stores are contiguous and a token's codes whole pieces of 64 to 256 bytes.
 template <class T>
 __global__ __launch_bounds__(LANES) void k_kv8_load(kv_load w)
 {
     const int side = blockIdx.y;
     if (!w.p[side]) return;
+    const bool small = w.chunks_all >> 31 == 0;  // 64-bit division is slow
     for (int64_t i = (int64_t)blockIdx.x * LANES + threadIdx.x; i < w.chunks_all; i += (int64_t)gridDim.x * LANES) {
-        int64_t n = w.chunks_all >> 32 ? i / w.chunks : (uint32_t)i / (uint32_t)w.chunks;
+        const int64_t n = small ? (uint32_t)i / (uint32_t)w.chunks : i / w.chunks;
         const int col = (int)(i - n * w.chunks) * 8;
-        const int64_t head = w.chunks_all >> 32 ? n / w.tokens : (uint32_t)n / (uint32_t)w.tokens, t = n - head * w.tokens;
-        const int b = (int)head / w.K, kv = (int)head - b * w.K;
-        const int64_t at = (int64_t)side * w.B * w.K + head;
+        const int64_t bt = small ? (uint32_t)n / (uint32_t)w.K : n / w.K;
+        const int kv = (int)(n - bt * w.K), b = (int)(small ? (uint32_t)bt / (uint32_t)w.tokens : bt / w.tokens);
+        const int64_t t = bt - b * w.tokens, at = ((int64_t)side * w.B + b) * w.K + kv;
         const vec<int8_t, 8> q = *(const vec<int8_t, 8> *)(w.codes + (at * w.room + t) * w.ld + col);
         const uint8_t e = w.exps[at * (w.room / RKB_GROUP) + t / RKB_GROUP];
         const float step = e == 0 ? 0.0f : step_of(e);
@@ -141,7 +143,9 @@ __global__ __launch_bounds__(LANES) void k_kv8_load(kv_load w)
 bool good_kv(int dtype, int64_t batch, int64_t kv_heads, int64_t dim, const rkb_kv8 *c)
 {
     return good_dtype16(dtype) && batch >= 0 && batch <= RKB_MAX_TOKENS && kv_heads >= 1 && kv_heads <= 65536 && dim >= 1 && dim <= RKB_MAX_DIM && c &&
-           c->tokens >= 0 && c->tokens <= RKB_MAX_TOKENS && (batch * c->tokens == 0 || (c->codes && c->exps && (uintptr_t)c->codes % 16 == 0));
+           c->tokens >= 0 && c->tokens <= RKB_MAX_TOKENS &&
+           (double)batch * (double)kv_heads * (double)c->tokens <= (double)((int64_t)1 << 48) &&  // more than any memory holds
+           (batch * c->tokens == 0 || (c->codes && c->exps && (uintptr_t)c->codes % 16 == 0));
 }
 
 bool good_strides(const rkb_heads &h, int64_t batch, int64_t rows, int64_t heads)
@@ -224,7 +228,6 @@ extern "C" int rkb_kv8_load(int dtype, int64_t batch, int64_t kv_heads, int64_t 
     w.D = (int)dim;
     w.ld = (int)round_up(dim, 16);
     w.chunks = (int)((dim + 7) / 8);
-    if (batch * kv_heads > ((int64_t)1 << 30)) return RKB_E_INVAL;
     w.chunks_all = batch * kv_heads * tokens * w.chunks;
     const dim3 grid((uint32_t)std::min<int64_t>((w.chunks_all + LANES - 1) / LANES, 1 << 16), 2);
     return dtype == RKB_F16 ? launch(k_kv8_load<f16>, grid, dim3(LANES), (hipStream_t)stream, w)

@@ -110,6 +110,17 @@ def test_short_workspaces_are_refused():
     assert lib.rkb_attn_bwd_workspace(a, 0, 1, None) == bk.RKB_E_INVAL
 
 
+def test_long_caches_fit_and_more_rows_than_a_launch_takes_do_not():
+    lib, n = bk.load(), C.c_size_t(0)
+    long = dict(batch=256, heads=64, kv_heads=8, q_rows=1, k_rows=1 << 20)
+    assert lib.rkb_attn_fwd_workspace(attn(**long), 1, 1, n) == bk.RKB_OK
+    assert lib.rkb_attn_bwd_workspace(attn(**{**long, "batch": 512}), 0, 1, n) == bk.RKB_E_INVAL
+    for rows, want in ((1 << 28, bk.RKB_OK), ((1 << 28) + 1, bk.RKB_E_INVAL)):
+        assert lib.rkb_attn_fwd_workspace(attn(batch=1, heads=1, kv_heads=1, q_rows=rows), 0, 1, n) == want
+        assert lib.rkb_attn_bwd_workspace(attn(batch=1, heads=1, kv_heads=1, k_rows=rows), 0, 1, n) == want
+    assert lib.rkb_attn_fwd_workspace(attn(batch=2, heads=1, kv_heads=1, q_rows=1 << 28), 0, 1, n) == bk.RKB_E_INVAL
+
+
 WRITE = dict(dtype=bk.RKB_BF16, batch=2, rows=3, kv_heads=2, dim=16, k=heads(3, 2), v=heads(3, 2), first=0, firsts=None, counts=None,
              cache=bk.CKv8(P, P, 40), stream=None)
 LOAD = dict(dtype=bk.RKB_BF16, batch=2, kv_heads=2, dim=16, cache=bk.CKv8(P, P, 40), k=heads(40, 2), v=heads(40, 2), stream=None)
@@ -119,7 +130,7 @@ LOAD = dict(dtype=bk.RKB_BF16, batch=2, kv_heads=2, dim=16, cache=bk.CKv8(P, P, 
     dict(dtype=bk.RKB_F32), dict(batch=-1), dict(rows=-1), dict(kv_heads=0), dict(dim=0), dict(dim=257), dict(k=None), dict(v=None), dict(cache=None),
     dict(k=heads(3, 2, p=None)), dict(v=heads(3, 2, p=P + 1)), dict(k=heads(3, 2, row=-2)), dict(first=1 << 41), dict(firsts=P + 1), dict(counts=P + 3),
     dict(cache=bk.CKv8(P, P, -1)), dict(cache=bk.CKv8(P + 4, P, 40)), dict(cache=bk.CKv8(None, P, 40)), dict(cache=bk.CKv8(P, None, 40)),
-    dict(batch=1 << 22, rows=1 << 10),
+    dict(batch=1 << 22, rows=1 << 10), dict(batch=1 << 28, kv_heads=1 << 16, cache=bk.CKv8(P, P, 1 << 28)),
 ], ids=lambda c: ",".join(c))
 def test_bad_writes_are_refused(change):
     assert bk.load().rkb_kv8_write(*{**WRITE, **change}.values()) == bk.RKB_E_INVAL
@@ -128,6 +139,7 @@ def test_bad_writes_are_refused(change):
 @pytest.mark.parametrize("change", [
     dict(dtype=bk.RKB_F32), dict(batch=-1), dict(kv_heads=0), dict(dim=0), dict(dim=300), dict(k=None), dict(v=None), dict(cache=None),
     dict(k=heads(40, 2, p=P + 1)), dict(v=heads(40, 2, head=15)), dict(k=heads(40, 2, row=16)), dict(cache=bk.CKv8(P, None, 40)),
+    dict(batch=1 << 28, kv_heads=1 << 16, cache=bk.CKv8(P, P, 1 << 28)),
 ], ids=lambda c: ",".join(c))
 def test_bad_loads_are_refused(change):
     assert bk.load().rkb_kv8_load(*{**LOAD, **change}.values()) == bk.RKB_E_INVAL

@@ -166,6 +166,29 @@ def test_dead_places_are_not_looked_at(Q, value):
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and not got[1][dead].any() and not got[2][dead].any()
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("B,Q,T,H,K,D,more", [
+    (2, 70, 70, 4, 2, 64, dict(mask="left", causal=True)), (2, 200, 190, 2, 2, 128, dict(causal=True, firsts=[-40, -300])),
+    (1, 40, 50, 2, 1, 200, dict(causal=True, firsts=-9)), (2, 150, 40, 2, 2, 40, dict(lens=[40, 0], bias=(8, 16, True, FP))),
+    (2, 300, 300, 4, 4, 64, dict(mask="left", causal=True, bias=(32, 128, True, FP)))])
+def test_queries_without_keys_are_not_looked_at(B, Q, T, H, K, D, more, value, dtype):
+    more = dict(more)
+    left = more.pop("mask", None)
+    (q, k, v, do), how, _ = problem(B, Q, T, H, K, D, dtype, **more)
+    if left:
+        how["mask"] = torch.arange(T, device="cuda") >= torch.tensor([[37], [5]], device="cuda")
+    o, kept = bk.rkb_attn_fwd(q, k, v, keep="full", **how)
+    dead = (kept[1] == -math.inf).permute(0, 2, 1)  # [B, Q, H]
+    assert dead.any() and not dead.all()
+    want = bk.rkb_attn_bwd(do.masked_fill(dead[..., None], 0), q.masked_fill(dead[..., None], 0), k, v, kept, **how)
+    q, do = q.masked_fill(dead[..., None], value), do.masked_fill(dead[..., None], value)
+    o2, kept2 = bk.rkb_attn_fwd(q, k, v, keep="full", **how)
+    assert torch.equal(o, o2) and torch.equal(kept[1], kept2[1])
+    for a, b in zip(want, bk.rkb_attn_bwd(do, q, k, v, kept, **how)):
+        assert (a is None and b is None) or (torch.equal(a, b) and bool(a.isfinite().all()))
+
+
 def test_bad_values_stay_in_their_row_and_head():
     (q, k, v, do), _, _ = problem(2, 100, 90, 4, 4, 64, BF)
     o, kept = bk.rkb_attn_fwd(q, k, v, keep="16bit")
