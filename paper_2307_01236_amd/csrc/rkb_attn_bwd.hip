@@ -456,18 +456,18 @@ __global__ __launch_bounds__(256, DP == 64 && FAR <= 128 ? 2 : 1) void k_attn_dk
                 sums[wave][2 * far] = ahead;
             }
             __syncthreads();
-            const int count = p.bias.count, buckets = count * p.bias.sides, c = threadIdx.x;
-            if (c < buckets && a0 == 0) {
-                const int side = c / count, n = c % count;
-                const int lo = n == 0 ? 0 : p.bias.border[n - 1], hi = n == count - 1 ? far : p.bias.border[n] - 1;
+            // a wave adds up a bucket, 64 distances at a time
+            const int count = p.bias.count, buckets = count * p.bias.sides;
+            const int64_t of_head = (int64_t)p.B * k_tiles * splits, me = ((int64_t)b * k_tiles + kt) * splits + split;
+            for (int c = wave; c < buckets && a0 == 0; c += WAVES) {
+                const int side = c / count, n = c - side * count;
+                const int lo = n == 0 ? side : p.bias.border[n - 1], hi = n == count - 1 ? far : p.bias.border[n] - 1;
+                // the positions in sums; of a one-sided bias, keys ahead count as distance 0
+                const int from = side ? far + lo : far - hi, to = side ? far + hi : p.bias.sides == 1 && n == 0 ? 2 * far : far - lo;
                 float sum = 0.0f;
-                for (int wv = 0; wv < WAVES; ++wv) {
-                    for (int dist = side ? max(lo, 1) : lo; dist <= hi; ++dist) sum += sums[wv][side ? far + dist : far - dist];
-                    if (p.bias.sides == 1 && n == 0)
-                        for (int at = far + 1; at <= 2 * far; ++at) sum += sums[wv][at];
-                }
-                const int64_t of_head = (int64_t)p.B * k_tiles * splits, me = ((int64_t)b * k_tiles + kt) * splits + split;
-                g.table_part[(h * of_head + me) * buckets + c] = sum * __builtin_amdgcn_exp2f(-P_LIFT<T>);
+                for (int at = from + lane; at <= to; at += WAVE) sum += (sums[0][at] + sums[1][at]) + (sums[2][at] + sums[3][at]);
+                sum = lane_sum<64>(sum);
+                if (lane == 0) g.table_part[(h * of_head + me) * buckets + c] = sum * __builtin_amdgcn_exp2f(-P_LIFT<T>);
             }
             __syncthreads();
             for (int n = lane; n <= 2 * far; n += WAVE) sums[wave][n] = 0.0f;
