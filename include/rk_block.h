@@ -235,9 +235,9 @@ int rkb_attn_fwd(const rkb_attn *a, const rkb_heads *q, const rkb_heads *k, cons
  *   dq_i = scale sum_j ds_ij k_j,  dk_j = scale sum_i ds_ij q_i,  dv_j = sum_i p_ij do_i,
  *   dtable[c, h] = sum of ds_ij over the i, j of bucket c and all sequences,
  * dk and dv summed over the heads that share them too.  p and ds enter the products rounded to dtype; in f16, scaled
- * so that neither overflows nor loses bits that its size would not lose in any type.  do_i . o_i takes over the error of o (its rounding, where o is
- * not given in 32 bits, and that of the probabilities it was summed from); what a row's ds add up to tells that error, which
- * is taken out of dk and dtable and stays in dq, about as large there as the rounding of ds.
+ * so that neither overflows nor loses bits that its size would not lose in any type.  do_i . o_i would take over the error of o (its rounding, where o is
+ * not given in 32 bits, and that of the probabilities it was summed from); what a row's ds add up to, 0 otherwise, tells that error, which
+ * is taken out of all of them.
  * dq, dk, dv of dtype, each may have p NULL (dk and dv both); dtable of table_dtype, NULL for none.  What q and do hold at
  * a query without live keys is not looked at, whatever it is; its dq is 0.
  * aligned: as above, of do too.

@@ -21,7 +21,7 @@ struct bwd_in {
     uint32_t *seen;          // [B, H, stats_rows / 32]: bit r: row r has keys
     int64_t stats_rows;
     heads_at dq, dk, dv;
-    float *dq_part, *dk_part, *dv_part;  // [splits, rows, D] each, where there are several
+    float *dq_part, *pk_part, *dk_part, *dv_part;  // [splits, rows, D] each, where there are several; pk: of sum p k
     float *row_part;         // [splits, B, H, stats_rows]: parts of the sums of ds, where there are several
     float *table_part;       // [H, B key tiles splits, buckets]
     int wide;                // bit 0: dq, 1: dk and dv take 8-byte stores
@@ -126,17 +126,22 @@ __device__ inline void store_grad(T *to, float *part, bool wide, int width, cons
 // A row's delta = do . o and -lse are formed here, where its do is in registers, and left for dk and dv.  delta comes from an o that
 // was summed from rounded probabilities (and may be rounded itself), so ds of a row adds up to some r
 // instead of 0.  Then delta + r is what delta should have been, to 32 bits: it is left for dk, dv and the bias's gradient, which
-// are formed from it afterwards; dq keeps an error of r (p k), about as large as the rounding of ds.
+// are formed from it afterwards.  dq itself is sum ds k - r sum p k, whose second product shares the keys' fragments with the first.
+// Heads of more than 128 columns are two workgroups', each with half of dq's columns.
 template <class T, int DP>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, bwd_in g, int splits)
 {
     using L = lay<DP>;
-    constexpr int TILE = DP == 256 ? 32 : 64, N = TILE / 32, BYTES = TILE * DP * 2, C = DP / 16, A = DP / 32;
+    constexpr bool DO_LDS = DP == 128;  // a wave's do lies in LDS: two waves of a unit leave it 256 registers, of which the sums take 128
+    constexpr int TILE = DP >= 128 ? 32 : 64, N = TILE / 32, BYTES = TILE * DP * 2, C = DP / 16, HALVES = DP == 256 ? 2 : 1, A = DP / 32 / HALVES;
     __shared__ __align__(16) char k0[BYTES], k1[BYTES], v0[BYTES], v1[BYTES];
+    __shared__ __align__(16) char own_do[DO_LDS ? WAVES * 32 * DP * 2 : 16];
     __shared__ float by_distance[2 * (MAX_FAR + PAD) + 1];
     const int lane = threadIdx.x % WAVE, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / WAVE);
     const int q_tiles = (p.Q + ROWS - 1) / ROWS;
-    int w = unit_order(blockIdx.x, p.B * p.K, p.G * splits * q_tiles);
+    int w = unit_order(blockIdx.x, p.B * p.K, p.G * splits * q_tiles * HALVES);
+    const int a0 = w % HALVES * A;  // the first of this workgroup's column blocks of 32
+    w /= HALVES;
     const int qt = q_tiles - 1 - w % q_tiles;
     w /= q_tiles;
     const int split = w % splits, bh = w / splits, b = bh / p.H, h = bh - b * p.H, kv = h / p.G;
@@ -152,7 +157,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
     frag<T> q[C], d[C];
     load_stationary<T, DP>(q, p.q.at<T>(b, min(i, p.Q - 1), h), lane, p.D, there);
     load_stationary<T, DP>(d, g.d_o.at<T>(b, min(i, p.Q - 1), h), lane, p.D, there);
-    const bool counted = i < g.stats_rows;  // rows past the last query are left as rows without keys, for tiles that reach there
+    const bool counted = i < g.stats_rows && a0 == 0;  // rows past the last query are left as rows without keys, for tiles that reach there
     const int64_t stat = (int64_t)bh * g.stats_rows + i;
     float lse = NEG_INF, delta = 0.0f;
     if (there) {
@@ -182,6 +187,12 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
     }
     const float lift = ds_scale<T>(g, p, b, kv);
     const int far = p.bias.far;
+    lds_byte *const my_do = (lds_byte *)own_do + wave * 32 * L::PITCH;
+    if constexpr (DO_LDS) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) *(__attribute__((address_space(3))) frag<T> *)(my_do + (L::rows_place(lane) ^ c * 32)) = d[c];
+        asm volatile("" ::: "memory");
+    }
     if (p.bias.table) fill_bias<T>(by_distance, p, h, threadIdx.x, 256);
 
     tile_copy<DP, TILE, WAVES> kc, vc;
@@ -196,9 +207,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
         vc.copy(wave, lane, (const char *)(vp + key * p.v.t), live, all, vto);
     };
 
-    f32x16 acc[A] = {};
+    f32x16 acc[A] = {}, pk[A] = {};
     const int place = L::rows_place(lane), cols[2] = {L::cols_place(lane, 0), L::cols_place(lane, 1)};
     float row_sum[2] = {0.0f, 0.0f};
+    const float lifted = lse + P_LIFT<T>, drop = __builtin_amdgcn_exp2f(-P_LIFT<T>), ds_times = lift * drop;
     auto compute = [&](int t, uint64_t live, lds_byte *kt, lds_byte *vt) __attribute__((always_inline)) {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
@@ -207,7 +219,10 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 s = mma32(L::template rows<T>(kt, place, c, n * 32), q[c], s);
-                dp = mma32(L::template rows<T>(vt, place, c, n * 32), d[c], dp);
+                if constexpr (DO_LDS)
+                    dp = mma32(L::template rows<T>(vt, place, c, n * 32), L::template rows<T>(my_do, place, c, 0), dp);
+                else
+                    dp = mma32(L::template rows<T>(vt, place, c, n * 32), d[c], dp);
             }
             float by = p.c;
             if (p.bias.table) {
@@ -216,16 +231,22 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
             }
             kill_dead(s, (uint32_t)(live >> n * 32), p.causal ? pos - key0 : INT_MAX, lane, NEG_INF);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], by, lse)) * (dp[r] - delta);
-                row_sum[r % 2] += s[r];
-            }
-            if constexpr (std::is_same_v<T, f16>) s *= lift;
-#pragma unroll
             for (int half = 0; half < 2; ++half) {
-                const frag<T> f = to_frag<T>(s, half);
+                frag<T> fp, fd;
 #pragma unroll
-                for (int a = 0; a < A; ++a) acc[a] = mma32(L::template cols<T>(kt, cols, a, n * 32 + half * 16), f, acc[a]);
+                for (int e = 0; e < 8; ++e) {
+                    const int r = half * 8 + e;
+                    const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], by, lifted)), ds = x * (dp[r] - delta);
+                    row_sum[r % 2] += ds;
+                    fp[e] = (T)x;
+                    fd[e] = (T)(std::is_same_v<T, f16> ? ds * ds_times : ds);
+                }
+#pragma unroll
+                for (int a = 0; a < A; ++a) {
+                    const frag<T> keys = L::template cols<T>(kt, cols, a0 + a, n * 32 + half * 16);
+                    acc[a] = mma32(keys, fd, acc[a]);
+                    pk[a] = mma32(keys, fp, pk[a]);
+                }
             }
         }
     };
@@ -251,12 +272,21 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
             if (t + 1 < t1) step(t + 1, k1, v1, k0, v0);
         }
     }
+    const float r = half_sum(row_sum[0] + row_sum[1]) * drop;
     if (there && g.dq.p) {
-        const int64_t row = ((int64_t)b * p.Q + i) * p.H + h, rows = (int64_t)p.B * p.Q * p.H;
-        store_grad<T, A>(g.dq.at<T>(b, i, h), g.dq_part ? g.dq_part + (split * rows + row) * p.D : nullptr, g.wide & 1, p.D,
-                         acc, p.scale / lift, lse == NEG_INF, lane);
+        const int64_t row = ((int64_t)b * p.Q + i) * p.H + h, rows = (int64_t)p.B * p.Q * p.H, part = (split * rows + row) * p.D + a0 * 32;
+        const float times = p.scale / lift;
+        if (g.dq_part) {
+            store_grad<T, A>(nullptr, g.pk_part + part, false, p.D - a0 * 32, pk, p.scale * drop, lse == NEG_INF, lane);
+        } else {
+            const float less = r * lift * drop;
+#pragma unroll
+            for (int a = 0; a < A; ++a)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[a][e] = __builtin_fmaf(-less, pk[a][e], acc[a][e]);
+        }
+        store_grad<T, A>(g.dq.at<T>(b, i, h) + a0 * 32, g.dq_part ? g.dq_part + part : nullptr, g.wide & 1, p.D - a0 * 32, acc, times, lse == NEG_INF, lane);
     }
-    const float r = half_sum(row_sum[0] + row_sum[1]);
     if (counted && lane < 32) {
         if (g.row_part)
             g.row_part[(int64_t)split * p.B * p.H * g.stats_rows + stat] = lse == NEG_INF ? 0.0f : r;
@@ -265,13 +295,14 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
     }
 }
 
-// delta + r where splits of the keys left parts of r.
+// delta + r where splits of the keys left parts of r, which become their sum.
 __global__ __launch_bounds__(256) void k_attn_delta_join(attn_in p, bwd_in g, int splits)
 {
     const int64_t rows = (int64_t)p.B * p.H * g.stats_rows;
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < rows; at += (int64_t)gridDim.x * 256) {
         float r = 0.0f;
         for (int s = 0; s < splits; ++s) r += g.row_part[s * rows + at];
+        g.row_part[at] = r;
         g.delta[at] += r;
     }
 }
@@ -669,6 +700,8 @@ struct grad_join {
     heads_at to;
     int64_t rows;  // batch * n * heads
     int n, heads;
+    const float *less, *by;  // dq: parts of sum p k, taken r times ([batch, heads, by_rows]); else NULL
+    int64_t by_rows;
 };
 
 // A lane has 4 columns of a row (with `wide` as one piece); splits are added in order.
@@ -683,12 +716,19 @@ __global__ __launch_bounds__(256) void k_attn_grads(grad_join j0, grad_join j1, 
         const int64_t row = small ? (uint32_t)at / quads : at / quads, t = small ? (uint32_t)row / (uint32_t)j.heads : row / j.heads;
         const int64_t b = small ? (uint32_t)t / (uint32_t)j.n : t / j.n;
         const int col = (int)(at - row * quads) * 4;
-        const float *const from = j.part + row * D + col;
+        const float *const from = j.part + row * D + col, *const less = j.less + row * D + col;
+        const float r = j.less ? -j.by[(b * j.heads + (row - t * j.heads)) * j.by_rows + (t - b * j.n)] : 0.0f;
         T *const to = j.to.at<T>(b, t - b * j.n, row - t * j.heads) + col;
         if (wide) {
             f32x4 sum = {};
 #pragma unroll 4
             for (int s = 0; s < splits; ++s) sum += *(const f32x4 *)(from + s * size);
+            if (j.less) {
+                f32x4 pk = {};
+#pragma unroll 4
+                for (int s = 0; s < splits; ++s) pk += *(const f32x4 *)(less + s * size);
+                sum += pk * r;
+            }
             vec<T, 4> v;
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[e] = (T)settled<T>(sum[e]);
@@ -697,6 +737,11 @@ __global__ __launch_bounds__(256) void k_attn_grads(grad_join j0, grad_join j1, 
             for (int e = 0; e < 4 && col + e < D; ++e) {
                 float sum = 0.0f;
                 for (int s = 0; s < splits; ++s) sum += from[s * size + e];
+                if (j.less) {
+                    float pk = 0.0f;
+                    for (int s = 0; s < splits; ++s) pk += less[s * size + e];
+                    sum = __builtin_fmaf(pk, r, sum);
+                }
                 to[e] = (T)settled<T>(sum);
             }
         }
@@ -722,7 +767,7 @@ struct bwd_memory {
         rows = plan.q_splits > 1 ? plan.q_splits * stats : 0;
         table = a.table ? up((size_t)plan.k_blocks * plan.k_splits * (a.heads / a.kv_heads) * a.buckets * 4) : 0;
     }
-    size_t all() const { return 2 * stats + seen + norms[0] + norms[1] + dq + rows + 2 * dkv + table; }
+    size_t all() const { return 2 * stats + seen + norms[0] + norms[1] + 2 * dq + rows + 2 * dkv + table; }
 };
 
 }  // namespace
@@ -748,6 +793,7 @@ int run_attn_bwd(const attn_in &p, const rkb_attn &a, const attn_bwd_plan &plan,
     g.dk = at_of(gr.dk);
     g.dv = at_of(gr.dv);
     g.dq_part = (float *)take(mem.dq);
+    g.pk_part = (float *)take(mem.dq);
     g.row_part = (float *)take(mem.rows);
     g.dk_part = (float *)take(mem.dkv);
     g.dv_part = (float *)take(mem.dkv);
@@ -762,7 +808,7 @@ int run_attn_bwd(const attn_in &p, const rkb_attn &a, const attn_bwd_plan &plan,
         if (rc != RKB_OK) return rc;
         return with_width(a.dim, [&](auto dp) {
             constexpr int DP = dp();
-            const dim3 q_grid((uint32_t)(plan.q_blocks * plan.q_splits)), k_grid((uint32_t)(plan.k_blocks * plan.k_splits * (DP == 256 ? 2 : 1)));
+            const dim3 q_grid((uint32_t)(plan.q_blocks * plan.q_splits * (DP == 256 ? 2 : 1))), k_grid((uint32_t)(plan.k_blocks * plan.k_splits * (DP == 256 ? 2 : 1)));
             int rc = RKB_OK;
             auto join = [&](const grad_join &x, const grad_join &y, int splits, int jobs, int wide) {
                 const int64_t blocks = std::min<int64_t>((x.rows * ((a.dim + 3) / 4) + 255) / 256, 1 << 16);
@@ -773,7 +819,7 @@ int run_attn_bwd(const attn_in &p, const rkb_attn &a, const attn_bwd_plan &plan,
                 rc = launch(k_attn_delta_join, dim3((uint32_t)std::min<int64_t>((rows * plan.stats_rows + 255) / 256, 1 << 16)), dim3(256), st, p, g,
                             plan.q_splits);
             if (rc == RKB_OK && plan.q_splits > 1 && gr.dq.p) {
-                const grad_join j{g.dq_part, g.dq, a.batch * a.q_rows * a.heads, (int)a.q_rows, (int)a.heads};
+                const grad_join j{g.dq_part, g.dq, a.batch * a.q_rows * a.heads, (int)a.q_rows, (int)a.heads, g.pk_part, g.row_part, g.stats_rows};
                 rc = join(j, j, plan.q_splits, 1, g.wide & 1);
             }
             if (rc == RKB_OK && plan.k_blocks && (gr.dk.p || gr.dtable)) {
@@ -789,7 +835,7 @@ int run_attn_bwd(const attn_in &p, const rkb_attn &a, const attn_bwd_plan &plan,
                             a.batch * ((a.k_rows + ROWS - 1) / ROWS) * plan.k_splits, gr.dtable);
             if (rc == RKB_OK && plan.k_splits > 1 && gr.dk.p) {
                 const int64_t n = a.batch * a.k_rows * a.kv_heads;
-                rc = join({g.dk_part, g.dk, n, (int)a.k_rows, (int)a.kv_heads}, {g.dv_part, g.dv, n, (int)a.k_rows, (int)a.kv_heads}, plan.k_splits, 2, g.wide >> 1);
+                rc = join({g.dk_part, g.dk, n, (int)a.k_rows, (int)a.kv_heads, nullptr, nullptr, 0}, {g.dv_part, g.dv, n, (int)a.k_rows, (int)a.kv_heads, nullptr, nullptr, 0}, plan.k_splits, 2, g.wide >> 1);
             }
             return rc;
         });

@@ -173,10 +173,12 @@ class Case:
         alive = torch.where(self.live, 1.0, 0.0)
         rounded = lambda e: e + u * (ds.abs() + e) + lost * alive  # noqa: E731
         group = lambda x: x.view(self.B, self.K, -1, self.T, self.D).sum(2).permute(0, 2, 1, 3)  # noqa: E731
-        b_dq = self.scale * (rounded(e1) @ self.ks.abs() + (self.T + 16) * U32 * (ds.abs() @ self.ks.abs())).permute(0, 2, 1, 3)
+        # dq: ds is rounded with the error of delta in it, which is then taken out with rounded probabilities
+        dropped = 2.0 ** -38 if dtype == torch.float16 else 0.0
+        in_dq = e2 + u * (ds.abs() + e1) + (p * (u + rel) * (1 + u) + dropped * alive) * e_kept + lost * alive
+        b_dq = self.scale * (in_dq @ self.ks.abs() + (self.T + 16) * U32 * ((ds.abs() + e1 + p * e_kept) @ self.ks.abs())).permute(0, 2, 1, 3)
         n = self.Q * (self.H // self.K)
         b_dk = group(self.scale * (rounded(e2).transpose(2, 3) @ self.qs.abs() + (n + 16) * U32 * (ds.abs().transpose(2, 3) @ self.qs.abs())))
-        dropped = 2.0 ** -38 if dtype == torch.float16 else 0.0
         b_dv = group((p * (u + rel) * (1 + u) + dropped * alive).transpose(2, 3) @ dos.abs() + (n + 16) * U32 * (p.transpose(2, 3) @ dos.abs()))
         out = [b_dq * 1.01 + rounding(dq, dtype), b_dk * 1.01 + rounding(dk, dtype), b_dv * 1.01 + rounding(dv, dtype), None]
         if dtable is not None:
