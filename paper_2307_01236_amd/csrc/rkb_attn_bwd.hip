@@ -299,14 +299,13 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
     }
 }
 
-// delta + r where splits of the keys left parts of r, which become their sum.
+// delta + r where splits of the keys left parts of r, and no dq is asked for (else k_attn_grads does it).
 __global__ __launch_bounds__(256) void k_attn_delta_join(attn_in p, bwd_in g, int splits)
 {
     const int64_t rows = (int64_t)p.B * p.H * g.stats_rows;
     for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < rows; at += (int64_t)gridDim.x * 256) {
         float r = 0.0f;
         for (int s = 0; s < splits; ++s) r += g.row_part[s * rows + at];
-        g.row_part[at] = r;
         g.delta[at] += r;
     }
 }
@@ -707,8 +706,10 @@ struct grad_join {
     heads_at to;
     int64_t rows;  // batch * n * heads
     int n, heads;
-    const float *less, *by;  // dq: parts of sum p k, taken r times ([batch, heads, by_rows]); else NULL
-    int64_t by_rows;
+    // dq: parts of sum p k, taken r times, whose parts are [splits, batch, heads, stats_rows] and which is added to delta; else NULL
+    const float *less, *by;
+    float *delta;
+    int64_t stats_rows, by_size;
 };
 
 // A lane has 4 columns of a row (with `wide` as one piece); splits are added in order.  Mostly a launch's latency: 5 to 6 us.
@@ -724,7 +725,13 @@ __global__ __launch_bounds__(256) void k_attn_grads(grad_join j0, grad_join j1, 
         const int64_t b = small ? (uint32_t)t / (uint32_t)j.n : t / j.n;
         const int col = (int)(at - row * quads) * 4;
         const float *const from = j.part + row * D + col, *const less = j.less + row * D + col;
-        const float r = j.less ? -j.by[(b * j.heads + (row - t * j.heads)) * j.by_rows + (t - b * j.n)] : 0.0f;
+        float r = 0.0f;
+        if (j.less) {
+            const int64_t stat = (b * j.heads + (row - t * j.heads)) * j.stats_rows + (t - b * j.n);
+            for (int s = 0; s < splits; ++s) r += j.by[s * j.by_size + stat];
+            if (col == 0) j.delta[stat] += r;
+            r = -r;
+        }
         T *const to = j.to.at<T>(b, t - b * j.n, row - t * j.heads) + col;
         if (wide) {
             f32x4 sum = {};
@@ -822,11 +829,12 @@ int run_attn_bwd(const attn_in &p, const rkb_attn &a, const attn_bwd_plan &plan,
                 return launch(k_attn_grads<T>, dim3((uint32_t)blocks, jobs), dim3(256), st, x, y, (int)a.dim, splits, wide);
             };
             if (plan.q_blocks) rc = launch(k_attn_dq<T, DP>, q_grid, dim3(256), st, p, g, plan.q_splits);
-            if (rc == RKB_OK && g.row_part && plan.q_blocks)
+            if (rc == RKB_OK && g.row_part && plan.q_blocks && !gr.dq.p)
                 rc = launch(k_attn_delta_join, dim3((uint32_t)std::min<int64_t>((rows * plan.stats_rows + 255) / 256, 1 << 16)), dim3(256), st, p, g,
                             plan.q_splits);
             if (rc == RKB_OK && plan.q_splits > 1 && gr.dq.p) {
-                const grad_join j{g.dq_part, g.dq, a.batch * a.q_rows * a.heads, (int)a.q_rows, (int)a.heads, g.pk_part, g.row_part, g.stats_rows};
+                const grad_join j{g.dq_part, g.dq, a.batch * a.q_rows * a.heads, (int)a.q_rows, (int)a.heads,
+                                  g.pk_part, g.row_part, g.delta, g.stats_rows, rows * g.stats_rows};
                 rc = join(j, j, plan.q_splits, 1, g.wide & 1);
             }
             if (rc == RKB_OK && plan.k_blocks && (gr.dk.p || gr.dtable)) {
@@ -842,7 +850,7 @@ int run_attn_bwd(const attn_in &p, const rkb_attn &a, const attn_bwd_plan &plan,
                             a.batch * ((a.k_rows + ROWS - 1) / ROWS) * plan.k_splits, gr.dtable);
             if (rc == RKB_OK && plan.k_splits > 1 && gr.dk.p) {
                 const int64_t n = a.batch * a.k_rows * a.kv_heads;
-                rc = join({g.dk_part, g.dk, n, (int)a.k_rows, (int)a.kv_heads, nullptr, nullptr, 0}, {g.dv_part, g.dv, n, (int)a.k_rows, (int)a.kv_heads, nullptr, nullptr, 0}, plan.k_splits, 2, g.wide >> 1);
+                rc = join({g.dk_part, g.dk, n, (int)a.k_rows, (int)a.kv_heads}, {g.dv_part, g.dv, n, (int)a.k_rows, (int)a.kv_heads}, plan.k_splits, 2, g.wide >> 1);
             }
             return rc;
         });

@@ -601,7 +601,7 @@ struct attn_args {
         a.kv_heads = kv_heads;
         a.dim = q.size(3);
         if (o[0] == Py_None) {
-            a.scale = a.dim > 0 ? 1.0f / std::sqrt((float)a.dim) : 1.0f;
+            a.scale = a.dim > 0 ? (float)(1.0 / std::sqrt((double)a.dim)) : 1.0f;
         } else {
             const double s = PyFloat_AsDouble(o[0]);
             if (s == -1.0 && PyErr_Occurred()) throw refused();

@@ -5,7 +5,7 @@
 // result does not depend on their order.
 //
 // Both are bound by memory and, when small, by a launch: 100 rows into 8 caches of 8 heads of 128 take 6 us, all 8 x 1024 tokens out again 14 us
-// (50 MB, 3.6 TB/s).
+// (50 MB; about 4 of it are the launch).
 #include <algorithm>
 
 #include "rkb_common.h"

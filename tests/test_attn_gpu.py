@@ -303,6 +303,31 @@ def test_outputs_into_a_wider_tensor():
     assert all(torch.equal(x[1], w) for x, w in zip(outs, want))
 
 
+@pytest.mark.parametrize("dtype", [BF, HF])
+def test_gradients_one_at_a_time(dtype):
+    """At the C interface, of a call whose keys are split: each alone is what it is with the others."""
+    lib, st = bk.load(), torch.cuda.current_stream().cuda_stream
+    (q, k, v, do), how, _ = problem(1, 70, 1100, 4, 2, 72, dtype, lens=[1030], bias=(8, 20, True, FP))
+    o, kept = bk.rkb_attn_fwd(q, k, v, keep="16bit", **how)
+    want = bk.rkb_attn_bwd(do, q, k, v, kept, **how)
+    table = how["bias"].table
+    a = bk.CAttn(bk.RKB_BF16 if dtype == BF else bk.RKB_F16, 0, 1, 70, 1100, 4, 2, 72, 72 ** -0.5, 0, None, how["lens"].data_ptr(), None, 0,
+                 table.data_ptr(), bk.RKB_F32, 8, 20, 1)
+
+    def at(t):
+        return bk.CHeads(t.data_ptr(), *t.stride()[:3])
+
+    n, none = ctypes.c_size_t(0), bk.CHeads(None, 0, 0, 0)
+    assert lib.rkb_attn_bwd_workspace(a, 0, 1, n) == 0
+    ws = torch.empty(n.value, dtype=torch.uint8, device="cuda")
+    for asked in ((0,), (1, 2), (3,), (0, 3), (0, 1, 2)):
+        got = [torch.empty_like(w) for w in want]
+        outs = [at(got[i]) if i in asked else none for i in range(3)]
+        assert lib.rkb_attn_bwd(a, at(do), at(q), at(k), at(v), at(o), None, kept[1].data_ptr(), *outs, got[3].data_ptr() if 3 in asked else None,
+                                ws.data_ptr(), n.value, st) == 0
+        assert all(torch.equal(got[i], want[i]) for i in asked), asked
+
+
 def test_empty_tensors():
     q, k = rand(0, 5, 2, 16, dtype=BF), rand(0, 7, 2, 16, dtype=BF)
     assert bk.rkb_attn_fwd(q, k, k)[0].shape == q.shape
