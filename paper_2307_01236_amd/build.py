@@ -22,8 +22,8 @@ BLOCK_LIB = os.path.join(PKG, "librkblock.so")
 BLOCK_SOURCES = ["rkb_norm.hip", "rkb_ckpt.hip", "rkb_gemm.hip", "rkb_attn.hip", "rkb_attn_bwd.hip", "rkb_attn_api.hip",
                  "rkb_kv8.hip"]
 # Sums of the attention kernels stay in vector registers past 256 of them, where vector instructions reach them: kept in the
-# accumulation registers, they are copied to and fro.  Heads of 256 columns gain most (one query over
-# 16 x 4096 tokens of 4 key heads 60 us instead of 195, a step of 2 x 2048 tokens 741 instead of 858), the others the same.
+# accumulation registers, they are copied to and fro.  Heads of 256 columns gain most (one query over 16 x 4096 tokens of 4 key
+# heads takes 60 us instead of 195), the others are the same or a few percent faster.
 SOURCE_FLAGS = {s: ["-mllvm", "-amdgpu-mfma-vgpr-form=1"] for s in ("rkb_attn.hip", "rkb_attn_bwd.hip")}
 BIND_LIB = os.path.join(PKG, "_rkblock.so")
 BIND_SOURCE = "rkb_bind.cpp"

@@ -157,7 +157,7 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
 
     const int i = q0 + wave * 32 + lane % 32;
     const bool there = i < p.Q;
-    const int pos = first + i, pos_lo = first + q0 + wave * 32, pos_hi = pos_lo + 31;
+    const int pos_lo = first + q0 + wave * 32, pos_hi = pos_lo + 31;
     frag<T> q[C], d[C];
     load_stationary<T, DP>(q, p.q.at<T>(b, min(i, p.Q - 1), h), lane, p.D, there);
     load_stationary<T, DP>(d, g.d_o.at<T>(b, min(i, p.Q - 1), h), lane, p.D, there);
@@ -220,20 +220,24 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
         for (int n = 0; n < N; ++n) {
             const int key0 = t * TILE + n * 32;
             f32x16 s = {}, dp = {};
+            int own = place;
+            asm volatile("" : "+v"(own));  // places in do are worked out each time, too
 #pragma unroll
             for (int c = 0; c < C; ++c) {
                 s = mma32(L::template rows<T>(kt, place, c, n * 32), q[c], s);
                 if constexpr (DO_LDS)
-                    dp = mma32(L::template rows<T>(vt, place, c, n * 32), L::template rows<T>(my_do, place, c, 0), dp);
+                    dp = mma32(L::template rows<T>(vt, place, c, n * 32), L::template rows<T>(my_do, own, c, 0), dp);
                 else
                     dp = mma32(L::template rows<T>(vt, place, c, n * 32), d[c], dp);
             }
             float by = p.c;
+            int me = lane;
+            asm volatile("" : "+v"(me));  // nothing of this is worked out ahead of the loop: it would hold registers in every turn
             if (p.bias.table) {
                 by = 1.0f;
-                add_bias(s, p.c, by_distance, far, key0, pos, pos_lo, pos_hi, lane);
+                add_bias(s, p.c, by_distance, far, key0, pos_lo + me % 32, pos_lo, pos_hi, me);
             }
-            kill_dead(s, (uint32_t)(live >> n * 32), p.causal ? pos - key0 : INT_MAX, lane, NEG_INF);
+            kill_dead(s, (uint32_t)(live >> n * 32), p.causal ? pos_lo + me % 32 - key0 : INT_MAX, me, NEG_INF);
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 frag<T> fp, fd;
@@ -276,12 +280,17 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
             if (t + 1 < t1) step(t + 1, k1, v1, k0, v0);
         }
     }
+    // places are worked out again, so that they hold no registers in the loop
+    int me = threadIdx.x % WAVE;
+    asm volatile("" : "+v"(me));
+    const int row_i = q0 + wave * 32 + me % 32;
+    const bool none = lifted == NEG_INF, stored = row_i < p.Q;
     const float r = half_sum(row_sum[0] + row_sum[1]) * drop;
-    if (there && g.dq.p) {
-        const int64_t row = ((int64_t)b * p.Q + i) * p.H + h, rows = (int64_t)p.B * p.Q * p.H, part = (split * rows + row) * p.D + a0 * 32;
+    if (stored && g.dq.p) {
+        const int64_t row = ((int64_t)b * p.Q + row_i) * p.H + h, rows = (int64_t)p.B * p.Q * p.H, part = (split * rows + row) * p.D + a0 * 32;
         const float times = p.scale / lift;
         if (g.dq_part) {
-            store_grad<T, A>(nullptr, g.pk_part + part, false, p.D - a0 * 32, pk, p.scale * drop, lse == NEG_INF, lane);
+            store_grad<T, A>(nullptr, g.pk_part + part, false, p.D - a0 * 32, pk, p.scale * drop, none, me);
         } else {
             const float less = r * lift * drop;
 #pragma unroll
@@ -289,13 +298,14 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, b
 #pragma unroll
                 for (int e = 0; e < 16; ++e) acc[a][e] = __builtin_fmaf(-less, pk[a][e], acc[a][e]);
         }
-        store_grad<T, A>(g.dq.at<T>(b, i, h) + a0 * 32, g.dq_part ? g.dq_part + part : nullptr, g.wide & 1, p.D - a0 * 32, acc, times, lse == NEG_INF, lane);
+        store_grad<T, A>(g.dq.at<T>(b, row_i, h) + a0 * 32, g.dq_part ? g.dq_part + part : nullptr, g.wide & 1, p.D - a0 * 32, acc, times, none, me);
     }
-    if (counted && lane < 32) {
+    if (row_i < g.stats_rows && a0 == 0 && me < 32) {
+        const int64_t at = (int64_t)bh * g.stats_rows + row_i;
         if (g.row_part)
-            g.row_part[(int64_t)split * p.B * p.H * g.stats_rows + stat] = lse == NEG_INF ? 0.0f : r;
+            g.row_part[(int64_t)split * p.B * p.H * g.stats_rows + at] = none ? 0.0f : r;
         else
-            g.delta[stat] = lse == NEG_INF ? 0.0f : delta + r;
+            g.delta[at] = none ? 0.0f : delta + r;
     }
 }
 
