@@ -426,9 +426,10 @@ __global__ __launch_bounds__((DP == 256 ? 2 : 4) * WAVE, (FEW_BLOCKS<DP, CACHE, 
     const int buckets = p.bias.sides * p.bias.count, far = p.bias.far;
     if constexpr (BIAS) {
         for (int n = threadIdx.x; n <= 2 * far; n += W * WAVE) bucket[n] = (uint8_t)bucket_of(p.bias, n - far);
+        // A row that does not exist sees no key: its maximum would else move when the others' sums are scaled, and with that their bits.
         for (int n = threadIdx.x; n < 32 * buckets; n += W * WAVE) {
             const int row = r0 + n % 32;
-            if (row < rows) table[n % 32 * (buckets + 1) + n / 32] = table_value<T>(p, n / 32, kv * p.G + row % p.G);
+            table[n % 32 * (buckets + 1) + n / 32] = row < rows ? table_value<T>(p, n / 32, kv * p.G + row % p.G) : NEG_INF;
         }
         __syncthreads();
     }
