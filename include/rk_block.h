@@ -208,6 +208,8 @@ typedef struct rkb_kv8 {
  * tokens before the first one written keeps them: where the new ones need a larger step, 2^e', their codes become
  * round-half-even(code 2^(e - e')).  What a block held from the first token written on is dropped: the places behind the
  * last one written are zeros.  Other blocks stay as they were.
+ * At most 2^22 blocks of all sequences and heads may be touched by a call: batch * kv_heads times the lesser of
+ * (rows + 62) / 32, rounded down (what rows tokens touch wherever they begin, and whatever counts says), and a head's blocks.
  */
 int rkb_kv8_write(int dtype, int64_t batch, int64_t rows, int64_t kv_heads, int64_t dim, const rkb_heads *k, const rkb_heads *v,
                   int64_t first, const int32_t *firsts, const int32_t *counts, const rkb_kv8 *cache, void *stream);
