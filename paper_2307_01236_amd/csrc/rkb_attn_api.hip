@@ -44,22 +44,9 @@ bool good_heads_in(const rkb_heads &h, int64_t elements, int size)
     return elements == 0 || (h.p && (uintptr_t)h.p % size == 0 && good(h.batch) && good(h.row) && good(h.head));
 }
 
-// An output's elements must not overlap: of its dimensions in order of their strides, each starts behind all of the one before.
 bool good_heads_out(const rkb_heads &h, int64_t batch, int64_t rows, int64_t heads, int64_t dim, int size)
 {
-    if (batch * rows == 0) return true;
-    if (!good_heads_in(h, 1, size)) return false;
-    int64_t stride[3] = {h.batch, h.row, h.head}, n[3] = {batch, rows, heads}, end = dim;
-    for (int k = 0; k < 3; ++k) {
-        int least = -1;
-        for (int i = 0; i < 3; ++i)
-            if (n[i] > 1 && (least < 0 || stride[i] < stride[least])) least = i;
-        if (least < 0) break;
-        if (stride[least] < end) return false;
-        end += stride[least] * (n[least] - 1);
-        n[least] = 1;
-    }
-    return true;
+    return batch * rows == 0 || (good_heads_in(h, 1, size) && elements_apart(h, batch, rows, heads, dim));
 }
 
 bool aligned_heads(const rkb_heads &h, int64_t dim)

@@ -221,6 +221,23 @@ inline bool good_output(const void *p, int64_t rows, int64_t cols, int64_t strid
     return good_input(p, rows, stride, size) && (rows <= 1 || stride >= cols);
 }
 
+// Whether no two elements of a [batch, rows, heads, dim] output share a place: of its dimensions in order of their strides (0 to 2^40 where the
+// size is over 1), each starts behind all of the one before.  An extent of 2^62 elements and more is no memory's, and 64 bits hold any
+// below it.
+inline bool elements_apart(const rkb_heads &h, int64_t batch, int64_t rows, int64_t heads, int64_t dim)
+{
+    int64_t stride[3] = {h.batch, h.row, h.head}, n[3] = {batch, rows, heads}, end = dim;
+    for (;;) {
+        int least = -1;
+        for (int i = 0; i < 3; ++i)
+            if (n[i] > 1 && (least < 0 || stride[i] < stride[least])) least = i;
+        if (least < 0) return true;
+        if (stride[least] < end || stride[least] > (((int64_t)1 << 62) - end) / (n[least] - 1)) return false;
+        end += stride[least] * (n[least] - 1);
+        n[least] = 1;
+    }
+}
+
 inline int64_t round_up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 inline int64_t code_ld(int64_t cols) { return round_up(cols, GROUP); }
 

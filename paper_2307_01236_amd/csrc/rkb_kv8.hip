@@ -205,18 +205,7 @@ extern "C" int rkb_kv8_load(int dtype, int64_t batch, int64_t kv_heads, int64_t 
     const rkb_heads *out[2] = {k, v};
     for (int i = 0; i < 2; ++i) {
         if (!out[i]->p) continue;
-        if (!good_strides(*out[i], batch, tokens, kv_heads)) return RKB_E_INVAL;
-        // elements must not overlap: of the dimensions in order of their strides, each starts behind all of the one before
-        int64_t stride[3] = {out[i]->batch, out[i]->row, out[i]->head}, n[3] = {batch, tokens, kv_heads}, end = dim;
-        for (;;) {
-            int least = -1;
-            for (int j = 0; j < 3; ++j)
-                if (n[j] > 1 && (least < 0 || stride[j] < stride[least])) least = j;
-            if (least < 0) break;
-            if (stride[least] < end) return RKB_E_INVAL;
-            end += stride[least] * (n[least] - 1);
-            n[least] = 1;
-        }
+        if (!good_strides(*out[i], batch, tokens, kv_heads) || !elements_apart(*out[i], batch, tokens, kv_heads, dim)) return RKB_E_INVAL;
         w.p[i] = (char *)out[i]->p;
         w.b[i] = batch > 1 ? out[i]->batch : 0;
         w.t[i] = tokens > 1 ? out[i]->row : 0;
