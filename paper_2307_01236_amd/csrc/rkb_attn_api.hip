@@ -20,7 +20,7 @@ bool good_attn(const rkb_attn *a)
     if (a->batch < 0 || a->q_rows < 0 || a->k_rows < 0 || a->batch > RKB_MAX_TOKENS || a->q_rows > RKB_MAX_TOKENS || a->k_rows > RKB_MAX_TOKENS)
         return false;
     if (a->kv_heads < 1 || a->heads < 1 || a->heads > 65536 || a->heads % a->kv_heads || a->dim < 1 || a->dim > RKB_MAX_DIM) return false;
-    if (!(a->scale > 0.0f) || !std::isfinite(a->scale)) return false;
+    if (!(a->scale > 0.0f) || !std::isfinite(a->scale * LOG2E)) return false;  // else a score of 0 is NaN in steps of log2
     if (a->first < -((int64_t)1 << 40) || a->first > (int64_t)1 << 40) return false;
     if ((uintptr_t)a->firsts % 4 || (uintptr_t)a->lens % 4) return false;
     if (a->mask && a->batch > 1 && (a->mask_stride < 0 || a->mask_stride > (int64_t)1 << 40)) return false;
