@@ -639,7 +639,7 @@ __global__ __launch_bounds__((DP == 256 ? 2 : 4) * WAVE, (FEW_BLOCKS<DP, CACHE, 
 template <class T>
 __global__ __launch_bounds__(256) void k_attn_join(attn_in p, attn_out out, int splits)
 {
-    // a split call has at most 512 x 64 rows or 256 x 128: all of this fits 32 bits
+    // keys are split for up to 256 workgroups, of up to 128 rows each: all of this fits 32 bits
     const uint32_t quads = (p.D + 3) / 4, rows = (uint32_t)p.B * p.H * p.Q, at = blockIdx.x * 256 + threadIdx.x, row = at / quads;
     const int col = (int)(at - row * quads) * 4;
     if (row >= rows) return;

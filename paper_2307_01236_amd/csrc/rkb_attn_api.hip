@@ -4,6 +4,7 @@
 
 #include "rkb_attn.h"
 #include "rkb_attn_args.h"
+#include "rkb_attn_cut.h"
 #include "rkb_buckets.h"
 
 namespace rkb {
@@ -176,16 +177,13 @@ static int split_of(int64_t blocks, int64_t want, int64_t most)
     return blocks == 0 ? 1 : (int)std::max<int64_t>(1, std::min({want / blocks, most, (int64_t)64}));
 }
 
-// Up to 64 rows of a key head (queries and the heads that share it) go by k_attn_few, which reads keys once for all of them, more by k_attn, which reads
-// them once for 128 queries of a head.  Over 16 x 4096 tokens, 4 key heads of 128, in us, few / many: 1 query of 16 heads 35 / 63 (of a cache 29 / 93), 16 of 16
-// 38 / 65 (35 / 93), 24 of 16 53 / 65, 64 of 4 38 / 33, 96 of 4 54 / 40: past 64 rows, heads that are not shared lose.
 // Keys are split, for 512 workgroups, into parts of at least 256: one token over 1024 cached ones takes 20 us so, 22 by 128, 25 without
 // splits; 6 x 199 queries over 777 keys, forward and backward, 131 by 256 and 142 by 1024.
 attn_plan plan_fwd(const rkb_attn &a)
 {
     const int64_t rows = a.q_rows * (a.heads / a.kv_heads);
     attn_plan plan{};
-    plan.few = rows <= 64;
+    plan.few = few_queries_win(a.q_rows, a.dim, a.table != nullptr);
     plan.blocks = plan.few ? a.batch * a.kv_heads * ((rows + 31) / 32) : a.batch * a.heads * ((a.q_rows + 127) / 128);
     plan.splits = split_of(plan.blocks, 512, a.k_rows / 256);
     return plan;
