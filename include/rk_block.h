@@ -170,7 +170,7 @@ typedef struct rkb_heads {
  * for the distance max(-n, 0).  Of nb buckets of a side the first e = nb / 2 (rounded down) are one distance each; from e on,
  * the bucket is e + floor((nb - e) ln(d / e) / ln(max_distance / e)), at most nb - 1, as exact arithmetic has it.
  * nb is 2 .. RKB_MAX_BUCKETS (and so is twice nb, where two-sided), e < max_distance <= RKB_MAX_DISTANCE.  An entry of -1e30 or less, -inf
- * among them, hides its keys as a mask does, and its gradient is 0.
+ * among them, hides its keys as a mask does, and its gradient is 0; one of 2^127 or more may count as an infinity, whose rows are NaN.
  *
  * dtype: RKB_F16 or RKB_BF16; 1 <= dim <= RKB_MAX_DIM; heads a multiple of kv_heads; 0 < scale, and scale / ln 2 finite in 32 bits; batch * heads times
  * q_rows (rounded up to 128) at most 2^28, and for the backward pass batch * kv_heads times k_rows likewise.

@@ -141,9 +141,9 @@ __device__ inline int keys_end(const attn_in &p, int len, int last_pos)
 // share, two tiles of keys and values in LDS in turn.  While the matrix units form the scores of the next 32 keys and add
 // these ones' values, the vector units make probabilities of these keys' scores.
 //
-// 4 x 2048 queries of 32 heads of 128 over 4096 keys of 8 (some padded): 360 to 390 us, 0.9 to 1.0 PFLOP/s (a large product by the library 1.13).  Between two
-// barriers each wave has 64 matrix instructions, which take 16 ns each by themselves; the exponentials and conversions beside them are nearly as
-// long, and what is not hidden is a wave's own order.  64 columns: 0.79 PFLOP/s, half the products per probability.
+// 4 x 2048 queries of 32 heads of 128 over 4096 keys of 8 (some padded): 360 to 390 us, 0.9 to 1.0 PFLOP/s (a large product by the library 1.4 to 1.6).  Between two
+// barriers each wave has 64 matrix instructions, which take 16 ns each by themselves; exponentials and conversions beside them keep the issue
+// busy 87 % of the time, the matrix units 53 %.  64 columns: 0.79 PFLOP/s, half the products per probability, the issue busy 90 %.
 template <class T, int DP, bool CACHE>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn(attn_in p, attn_out out, int splits)
 {
@@ -378,13 +378,13 @@ __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn(attn_in p, attn
 
 // ------------------------------------------------------------------ few rows
 //
-// A workgroup has up to 32 rows of one key head: queries and the heads that share it, queries first.  Each wave takes keys of its
+// Up to 32 or 64 queries (rkb_attn_cut.h).  A workgroup has up to 32 rows of one key head: queries and the heads that share it, queries first.  Each wave takes keys of its
 // own, in tiles of 32 that no other wave waits for, and the waves' sums are joined at the end.  A cache's keys go from
 // memory to the matrix units' registers (a lane has 16 neighbouring columns of a key, and all keys' and queries' columns are taken in that
 // order), its values through LDS, to be read by columns; two tiles of both wait in registers until they are due.
 //
-// Bound by memory: 64 sequences of up to 1500 keys of 16 heads of 64 take 55 us (5.4 TB/s), 16 caches of up to 32768 tokens, 64 heads on 8
-// of 128, 161 us (4.9 TB/s; through LDS both ways and one tile ahead it was 457).  One token over 1024 cached ones takes 14 us, all latency.
+// Bound by memory: 64 sequences of up to 1500 keys of 16 heads of 64 take 55 to 57 us (5.2 to 5.4 TB/s), 16 caches of up to 32768 tokens, 64 heads on 8
+// of 128, 159 to 162 us (4.9 TB/s; through LDS both ways and one tile ahead it was 457).  One token over 1024 cached ones takes 13 to 15 us, all latency.
 template <int DP, bool CACHE, bool BIAS>
 constexpr int FEW_BLOCKS = (DP == 256 ? 2 : 4) * 32 * DP * 2 * (CACHE ? 2 : 4) + (BIAS ? 32 * (MAX_BUCKETS + 1) * 4 + 2 * MAX_FAR + 1 : 0) + 2048 <=
                                    80 * 1024 && DP < 256 ? 2 : 1;  // workgroups of a compute unit, by LDS

@@ -1,6 +1,6 @@
 // Attention backward (rk_block.h).  Probabilities are made again from the row sums that the forward left: dq by a kernel like the
 // forward, with queries stationary, dk and dv by one with keys stationary, so that every sum has one owner and a
-// fixed order.  That makes the scores and dp twice, 7 products instead of 5, and needs no atomics and no [queries, keys] matrix.
+// fixed order.  That makes the scores and dp twice and, with dq's correction, 8 products instead of 5; it needs no atomics and no [queries, keys] matrix.
 #include <algorithm>
 #include <climits>
 
@@ -130,8 +130,9 @@ __device__ inline void store_grad(T *to, float *part, bool wide, int width, cons
 // are formed from it afterwards.  dq itself is sum ds k - r sum p k, whose second product shares the keys' fragments with the first.
 // Heads of more than 128 columns are two workgroups', each with half of dq's columns.
 //
-// 4 x 2048 queries of 32 heads of 128 over 4096 keys of 8: 680 to 730 us, 1.0 PFLOP/s with four products; without sum p k 527 to 540.  Two waves of a
-// unit hide each other's waits; one wave with twice the registers, which then need not keep do in LDS, took 800.
+// 4 x 2048 queries of 32 heads of 128 over 4096 keys of 8 (some padded): 670 to 730 us, 1.0 to 1.1 PFLOP/s with four products; without sum p k 527 to 540.  Two
+// waves of a unit hide part of each other's waits: each waits 41 % of its time, and the matrix units are busy 53 %.  One wave with twice the registers,
+// which then need not keep do in LDS, took 800.
 template <class T, int DP>
 __global__ __launch_bounds__(256, DP == 256 ? 1 : 2) void k_attn_dq(attn_in p, bwd_in g, int splits)
 {
@@ -343,8 +344,10 @@ __global__ __launch_bounds__(WAVE) void k_attn_dtable(attn_in p, const float *pa
 // then enter dv and dk.  Heads of more than 128 columns are two workgroups', each with half of dk's and dv's columns: all of them do not fit
 // into registers.
 //
-// 4 x 2048 queries of 32 heads of 128 over 4096 keys of 8: 890 us, 0.81 PFLOP/s with four products.  A wave has a unit's registers to itself, so nothing
-// but its own order hides the reads from LDS, 32 KB for 32 matrix instructions.  With a bias, 16 x 512 x 512, 12 heads of 64: 82 us.
+// 4 x 2048 queries of 32 heads of 128 over 4096 keys of 8 (some padded): 880 to 910 us, 0.8 PFLOP/s with four products.  A wave has a unit's registers to
+// itself, so nothing but its own order hides what it waits for: it waits 30 % of its time and issues in half of it, while the matrix units are busy
+// 42 % and LDS 26 %.  With a bias, 16 x 512 x 512, 12 heads of 64: 82 us; its two waves of a unit wait 45 % of their time
+// each, and the issue is busy 60 %.
 //
 // FAR: the largest distance that the bias looks up (0: no bias).  Its gradient, ds by buckets, is summed over diagonals: a wave lays the
 // queries x 32 keys of some registers into LDS at (query, key - query), whose columns are diagonals, and a lane adds up a column.  What no

@@ -12,6 +12,7 @@ namespace rkb {
 //   128                          1         34/29    35/30    35/30     35/31     38/32     39/34
 //   128                          4         35/68    35/67    38/67     54/68     84/71     89/75
 //   128                         16        35/220   54/225   84/232   165/232   207/240   329/249
+//   128, over a cache            1         29/34    30/33    30/34     31/35     33/35     33/37
 //   128, over a cache            4         29/92    31/94    33/93     51/93     80/97     82/97
 //   128, over a cache           16        30/329   51/330   82/328   157/331   192/332   297/334
 //   128, a bias                  4         42/70    43/70    49/70     71/72    102/75    107/78
