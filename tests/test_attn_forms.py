@@ -72,3 +72,15 @@ def test_both_forms_next_to_the_border_agree(columns):
     for n in (border, border + 1):
         o = bk.rkb_attn_fwd(q[:, :n].cuda(), k.cuda(), v.cuda())[0]
         assert ao.worst(o, want[:, :n], bound[:, :n]) <= 1.0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Q", [31, 32, 33, 50, 64, 65])
+def test_a_cache_takes_the_form_that_its_values_take(Q, D):
+    """The same bits over a cache and over what it stands for, on both sides of the rule's borders."""
+    gen = torch.Generator().manual_seed(2)
+    r = lambda *s: torch.randn(*s, generator=gen).to(BF).cuda()  # noqa: E731
+    q, cache = r(2, Q, 4, D), bk.Kv8.zeros(2, 300, 4, D)
+    bk.rkb_kv8_write(cache, r(2, 300, 4, D), r(2, 300, 4, D))
+    assert torch.equal(bk.rkb_attn_fwd(q, cache)[0], bk.rkb_attn_fwd(q, *bk.rkb_kv8_load(cache))[0])
